@@ -67,7 +67,13 @@ enum {
 };
 
 /* Device status bits (first int32 of the workspace). */
-enum { HSPEC_DEV_BAD_PAGE = 1, HSPEC_DEV_BAD_CTX_LEN = 2, HSPEC_DEV_BAD_TOKEN = 4, HSPEC_DEV_NONFINITE = 8 };
+enum {
+  HSPEC_DEV_BAD_PAGE = 1,
+  HSPEC_DEV_BAD_CTX_LEN = 2,
+  HSPEC_DEV_BAD_TOKEN = 4,
+  HSPEC_DEV_NONFINITE = 8,
+  HSPEC_DEV_BAD_ROWS = 16
+};
 
 /*
  * Mamba layer configuration (Sec. 3.3.1; sizes of App. B.1 "Mamba").
@@ -413,6 +419,102 @@ hspec_status hspec_gather_slots(int B, int max_pages, int page_size, int num_pag
 hspec_status hspec_linear(hspec_dtype dtype, int M, int N, int K, const void* A, const void* W,
                           const float* R, float* C, void* workspace, size_t ws_bytes, void* stream);
 size_t hspec_linear_workspace(hspec_dtype dtype, int M, int N, int K);
+
+/* ------------------------------------------------------- the target's side of a step */
+
+/*
+ * A step of the target model over a ragged batch of new tokens: the prompt of a request, part of
+ * it, one token, or the last committed token and its drafts.  Request b has rows cu_new[b] ..
+ * cu_new[b+1]-1 of every [T, ..] array (cu_new [B+1] device int32, cu_new[0] = 0, rising; a
+ * request may have none), and row i of it is the token at position ctx_lens[b] + i, where
+ * ctx_lens[b] counts the positions that were cached before.  Rows past cu_new[B] belong to no
+ * request: they are read by nothing and their outputs are left as they were.
+ *   append:  q, k of the rows get their norm and RoPE, k and v go into the pages, q out
+ *   attend:  every row attends to its request's positions up to its own
+ *   verify:  the drafts that the target's logits let stand, and the next token
+ * The arrays describing the batch are checked on the device: a row range outside [0, T], falling,
+ * or longer than max_new is clamped and sets HSPEC_DEV_BAD_ROWS; a length below 0, or with the new
+ * tokens above the positions there are (max_pages * page_size, and max_len where it is given), is
+ * clamped and sets HSPEC_DEV_BAD_CTX_LEN.  Data tensors are 16-byte aligned, else
+ * HSPEC_ERR_UNSUPPORTED.  Outputs of append and attention are in the storage dtype (what the next
+ * projection and the cache take), unlike those of the drafting calls.
+ *
+ *   B requests (at most 32767), T rows, max_new: host upper bound of one request's new tokens, Hq
+ *   query and Hkv KV heads (query head q reads KV head q / (Hq/Hkv)), D head dim (64 or 128),
+ *   caches [num_pages, page_size, Hkv, D] through page_table [B, max_pages] as in
+ *   hspec_attn_cfg, T * Hq <= 2^28, Hq <= 4096.  window > 0: a row sees the last `window` positions,
+ *   its own included (pages that no row sees are not read, and may be unmapped).  scale: 0 =
+ *   1/sqrt(D).
+ */
+typedef struct {
+  int B, T, max_new, Hq, Hkv, D, page_size, max_pages, num_pages, window;
+  hspec_dtype dtype;
+  float eps, scale;
+  double rope_theta;
+} hspec_chunk_cfg;
+
+/*
+ * qkv [T, (Hq + 2 Hkv) D], rows [q heads | k heads | v heads] of a fused projection, fp32 (as
+ * hspec_linear writes it) or bf16 by qkv_dtype:
+ *   q = RoPE(RMSNorm_D(q) q_norm_w), k = RoPE(RMSNorm_D(k) k_norm_w)
+ * with rotate-half pairing at the row's position (no norm where q_norm_w and k_norm_w [D] are
+ * both NULL).  q [T, Hq, D] out; k and v are written at slot(position) of k_cache and v_cache, in
+ * place.  A position whose page id is outside the pool sets HSPEC_DEV_BAD_PAGE and is not written.
+ * Which of two rows stays is undefined where a page is mapped for both.
+ */
+hspec_status hspec_chunk_append(const hspec_chunk_cfg* cfg, hspec_dtype qkv_dtype, const void* qkv,
+                                const float* q_norm_w, const float* k_norm_w, const int32_t* cu_new,
+                                const int32_t* ctx_lens, void* q, void* k_cache, void* v_cache,
+                                const int32_t* page_table, void* workspace, size_t ws_bytes, void* stream);
+size_t hspec_chunk_append_workspace(const hspec_chunk_cfg* cfg);
+
+/*
+ * o[r, h] = softmax over the visible positions s <= ctx_len + i of scale q[r, h] . K[s], times V:
+ * q, o [T, Hq, D], the caches hold the new tokens' K and V already (hspec_chunk_append).  max_len:
+ * host upper bound of ctx_lens[b] + new tokens of b (bounds the split of long caches).  A slot that
+ * a row does not see never changes it, whatever it holds (NaN and infinities included); pages
+ * outside the pool read as zeros and set HSPEC_DEV_BAD_PAGE; a row that sees no position is zero.
+ * Results are bitwise reproducible and independent of where pages live.  o must not lie over q.
+ */
+hspec_status hspec_chunk_attn(const hspec_chunk_cfg* cfg, const void* q, const int32_t* cu_new, const void* k_cache,
+                              const void* v_cache, const int32_t* page_table, const int32_t* ctx_lens, int max_len,
+                              void* o, void* workspace, size_t ws_bytes, void* stream);
+size_t hspec_chunk_attn_workspace(const hspec_chunk_cfg* cfg, int max_len);
+
+/*
+ * Verification of drafted tokens (speculative sampling): request b has n drafts and n + 1 rows of
+ * target logits, row j after j drafts; rows cu_rows[b] .. cu_rows[b+1]-1 of target_logits [rows,
+ * vocab] (storage dtype), or b (k+1) .. with cu_rows NULL (rows = B (k+1), n = k).  n <= k; a
+ * request without rows gets n_accepted 0 and no token.
+ *   draft_tokens [B, k] int32, ids of the drafter's vocabulary (hspec_draft_head); d2t [draft_vocab]
+ *   int32 gives their target ids and t2d [vocab] the way back (-1: not in the drafter's
+ *   vocabulary); NULL where draft id = target id.
+ * Sampling (u [B, k] in [0, 1) and gumbel [B, vocab] fp32 from the caller):
+ *   p_j = softmax(target row j / temperature); q_j = softmax(draft_logits[b, j] /
+ *   draft_temperature) (draft_logits [B, k, draft_vocab] fp32 as hspec_draft_head writes them), or
+ *   all on the drafted token with draft_logits NULL (a greedy drafter);
+ *   draft j stands if u[b, j] q_j(t_j) < p_j(t_j); a = the first that does not, or n;
+ *   next = argmax_v log max(p_a(v) - q_a(v), 0) + gumbel[b, v], q = 0 for a = n (p_a alone where no
+ *   difference is positive).
+ * Greedy (u and gumbel NULL, draft_logits NULL): draft j stands while it is the argmax of row j;
+ *   next = argmax of row a.  A tie goes to the lowest id.
+ * tokens [B, k+1] int32: the a drafts that stand (target ids), next, then -1; n_accepted [B] = a.
+ * NaN logits count as -inf and +inf as the largest float; they, a NaN of gumbel and a row of nothing but
+ * -inf set HSPEC_DEV_NONFINITE (rows up to a are looked at); a draft id outside [0, draft_vocab)
+ * or a mapped id out of range does not stand (or counts as -1) and sets HSPEC_DEV_BAD_TOKEN;
+ * HSPEC_DEV_BAD_ROWS as above, with max_new = k + 1.
+ */
+typedef struct {
+  int B, k, rows, vocab, draft_vocab;
+  hspec_dtype dtype;
+  float temperature, draft_temperature;
+} hspec_verify_cfg;
+
+hspec_status hspec_verify(const hspec_verify_cfg* cfg, const void* target_logits, const float* draft_logits,
+                          const int32_t* draft_tokens, const int32_t* cu_rows, const int32_t* d2t, const int32_t* t2d,
+                          const float* u, const float* gumbel, int32_t* tokens, int32_t* n_accepted, void* workspace,
+                          size_t ws_bytes, void* stream);
+size_t hspec_verify_workspace(const hspec_verify_cfg* cfg);
 
 /* ------------------------------------------------------------------------- utilities */
 

@@ -159,6 +159,15 @@ __device__ __forceinline__ void touch_args() {
   for (int i = 0; i <= BYTES / 64; ++i) asm volatile("" ::"s"(v[i]));
 }
 
+// Order-preserving map of a float that is no NaN to uint32 (larger float, larger key, never 0).
+__device__ __forceinline__ unsigned score_ord(float s) {
+  const unsigned u = __float_as_uint(s);
+  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+__device__ __forceinline__ int key_token(unsigned long long key) {
+  return (int)~(unsigned)(key & 0xffffffffu);
+}
+
 template <int V>
 using Int = std::integral_constant<int, V>;
 

@@ -26,14 +26,6 @@ constexpr int MK_ROWS = 64;    // requests per tile (4 MFMA row blocks)
 constexpr int ST_BAD_TOKEN = 4;
 constexpr int ST_NONFINITE = 8;
 
-// Order-preserving map of a float that is no NaN to uint32 (larger float, larger key, never 0).
-__device__ __forceinline__ unsigned score_ord(float s) {
-  const unsigned u = __float_as_uint(s);
-  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-}
-__device__ __forceinline__ int key_token(unsigned long long key) {
-  return (int)~(unsigned)(key & 0xffffffffu);
-}
 // Best key of a position over its slots.
 __device__ __forceinline__ unsigned long long best_key(const unsigned long long* keys) {
   unsigned long long m = keys[0];

@@ -22,7 +22,7 @@ BLOCK_CAUSAL = 1
 ATTN_PRECISE_IO = 2
 W_DS_PACKED = 1
 MAMBA_PRECISE_IO = 2
-DEV_BAD_PAGE, DEV_BAD_CTX_LEN, DEV_BAD_TOKEN, DEV_NONFINITE = 1, 2, 4, 8
+DEV_BAD_PAGE, DEV_BAD_CTX_LEN, DEV_BAD_TOKEN, DEV_NONFINITE, DEV_BAD_ROWS = 1, 2, 4, 8, 16
 STATUS = {0: "HSPEC_OK", 1: "HSPEC_ERR_NULL", 2: "HSPEC_ERR_SHAPE", 3: "HSPEC_ERR_DTYPE",
           4: "HSPEC_ERR_UNSUPPORTED", 5: "HSPEC_ERR_WORKSPACE", 6: "HSPEC_ERR_LAUNCH"}
 
@@ -61,6 +61,17 @@ class HeadCfg(C.Structure):
 
 class HeadW(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("norm_f_w", "W_lm", "E_M", "U_M")]
+
+
+class ChunkCfg(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("B", "T", "max_new", "Hq", "Hkv", "D", "page_size", "max_pages", "num_pages",
+                                        "window")] + [
+        ("dtype", C.c_int), ("eps", C.c_float), ("scale", C.c_float), ("rope_theta", C.c_double)]
+
+
+class VerifyCfg(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("B", "k", "rows", "vocab", "draft_vocab")] + [
+        ("dtype", C.c_int), ("temperature", C.c_float), ("draft_temperature", C.c_float)]
 
 
 class HspecError(RuntimeError):
@@ -109,6 +120,13 @@ EXPORTS = {
     "hspec_draft_head": (C.c_int, [C.POINTER(HeadCfg), C.POINTER(HeadW)] + [C.c_void_p] * 7 + [C.c_size_t,
                                                                                           C.c_void_p]),
     "hspec_draft_head_workspace": (C.c_size_t, [C.POINTER(HeadCfg)]),
+    "hspec_chunk_append": (C.c_int, [C.POINTER(ChunkCfg), C.c_int] + [C.c_void_p] * 10 + [C.c_size_t, C.c_void_p]),
+    "hspec_chunk_append_workspace": (C.c_size_t, [C.POINTER(ChunkCfg)]),
+    "hspec_chunk_attn": (C.c_int, [C.POINTER(ChunkCfg)] + [C.c_void_p] * 6 + [C.c_int, C.c_void_p, C.c_void_p, C.c_size_t,
+                                                                          C.c_void_p]),
+    "hspec_chunk_attn_workspace": (C.c_size_t, [C.POINTER(ChunkCfg), C.c_int]),
+    "hspec_verify": (C.c_int, [C.POINTER(VerifyCfg)] + [C.c_void_p] * 11 + [C.c_size_t, C.c_void_p]),
+    "hspec_verify_workspace": (C.c_size_t, [C.POINTER(VerifyCfg)]),
     "hspec_pack_w_ds_bytes": (C.c_size_t, [C.c_int, C.c_int]),
     "hspec_pack_w_ds": (C.c_int, [C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p]),
     "hspec_read_status": (C.c_int, [C.c_void_p, C.POINTER(C.c_int32), C.c_void_p]),
@@ -401,3 +419,92 @@ def kv_inject(cfg, IW: dict, h_new, caches: list, page_table, ctx_lens, ws):
                                  arr([w["W_v"] for w in L]), arr([w["k_norm_w"] for w in L]),
                                  arr([c["k_cache"] for c in caches]), arr([c["v_cache"] for c in caches]),
                                  ptr(page_table), ptr(ctx_lens), ptr(ws), ws.numel(), stream_ptr()))
+
+
+# ----------------------------------------------------------------- the target's side of a step
+
+def _args(want: dict, **tensors):
+    """Pointers of device tensors on the current device, of the type and shape each has to have
+    (want: name -> (dtype, shape); None passes through where the C call allows it)."""
+    torch = _torch()
+    dev = torch.cuda.current_device()
+    out = []
+    for name, t in tensors.items():
+        if t is None:
+            out.append(None)
+            continue
+        dt, shape = want[name]
+        if not (t.is_cuda and t.device.index == dev and t.is_contiguous()):
+            raise ValueError(f"{name}: expected a contiguous tensor on the current device")
+        if t.dtype != dt or tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{name}: expected {dt} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+        out.append(C.c_void_p(t.data_ptr()))
+    return out
+
+
+def _storage(dtype: int):
+    torch = _torch()
+    return torch.float32 if dtype == F32 else torch.bfloat16
+
+
+def chunk_cfg(B, T, max_new, Hq, Hkv, D, page_size, max_pages, num_pages, dtype=BF16, window=0, eps=1e-6, scale=0.0,
+              rope_theta=1e6) -> ChunkCfg:
+    """A ragged batch of new tokens over a paged cache (hspec_chunk_cfg)."""
+    return ChunkCfg(B, T, max_new, Hq, Hkv, D, page_size, max_pages, num_pages, window, dtype, eps, scale, rope_theta)
+
+
+def _chunk_want(cc: ChunkCfg) -> dict:
+    torch = _torch()
+    st, i32 = _storage(cc.dtype), torch.int32
+    pool = (cc.num_pages, cc.page_size, cc.Hkv, cc.D)
+    return dict(q=(st, (cc.T, cc.Hq, cc.D)), o=(st, (cc.T, cc.Hq, cc.D)), k_cache=(st, pool), v_cache=(st, pool),
+                cu_new=(i32, (cc.B + 1,)), ctx_lens=(i32, (cc.B,)), page_table=(i32, (cc.B, cc.max_pages)),
+                q_norm_w=(torch.float32, (cc.D,)), k_norm_w=(torch.float32, (cc.D,)))
+
+
+def chunk_append_workspace(cc: ChunkCfg) -> int:
+    return lib().hspec_chunk_append_workspace(C.byref(cc))
+
+
+def chunk_append(cc: ChunkCfg, qkv, cu_new, ctx_lens, q, k_cache, v_cache, page_table, ws, q_norm_w=None, k_norm_w=None):
+    """Norm and RoPE of the new tokens' q and k; q out, K and V into the pages (hspec_chunk_append)."""
+    torch = _torch()
+    want = _chunk_want(cc)
+    code = F32 if qkv.dtype == torch.float32 else BF16
+    want["qkv"] = (_storage(code), (cc.T, (cc.Hq + 2 * cc.Hkv) * cc.D))
+    a = _args(want, qkv=qkv, q_norm_w=q_norm_w, k_norm_w=k_norm_w, cu_new=cu_new, ctx_lens=ctx_lens, q=q,
+              k_cache=k_cache, v_cache=v_cache, page_table=page_table)
+    _check(lib().hspec_chunk_append(C.byref(cc), code, *a, ptr(ws), ws.numel(), stream_ptr()))
+
+
+def chunk_attn_workspace(cc: ChunkCfg, max_len: int) -> int:
+    return lib().hspec_chunk_attn_workspace(C.byref(cc), int(max_len))
+
+
+def chunk_attn(cc: ChunkCfg, q, cu_new, k_cache, v_cache, page_table, ctx_lens, max_len: int, o, ws):
+    """o [T, Hq, D] = causal attention of the new tokens over the paged cache (hspec_chunk_attn)."""
+    a = _args(_chunk_want(cc), q=q, cu_new=cu_new, k_cache=k_cache, v_cache=v_cache, page_table=page_table,
+              ctx_lens=ctx_lens, o=o)
+    _check(lib().hspec_chunk_attn(C.byref(cc), *a[:6], int(max_len), a[6], ptr(ws), ws.numel(), stream_ptr()))
+
+
+def verify_cfg(B, k, rows, vocab, draft_vocab, dtype=BF16, temperature=1.0, draft_temperature=1.0) -> VerifyCfg:
+    return VerifyCfg(B, k, rows, vocab, draft_vocab, dtype, temperature, draft_temperature)
+
+
+def verify_workspace(vc: VerifyCfg) -> int:
+    return lib().hspec_verify_workspace(C.byref(vc))
+
+
+def verify(vc: VerifyCfg, target_logits, draft_tokens, tokens, n_accepted, ws, draft_logits=None, cu_rows=None, d2t=None,
+           t2d=None, u=None, gumbel=None):
+    """tokens [B, k+1], n_accepted [B] = which drafts stand against the target (hspec_verify)."""
+    torch = _torch()
+    f32, i32 = torch.float32, torch.int32
+    want = dict(target_logits=(_storage(vc.dtype), (vc.rows, vc.vocab)), draft_logits=(f32, (vc.B, vc.k, vc.draft_vocab)),
+                draft_tokens=(i32, (vc.B, vc.k)), cu_rows=(i32, (vc.B + 1,)), d2t=(i32, (vc.draft_vocab,)),
+                t2d=(i32, (vc.vocab,)), u=(f32, (vc.B, vc.k)), gumbel=(f32, (vc.B, vc.vocab)),
+                tokens=(i32, (vc.B, vc.k + 1)), n_accepted=(i32, (vc.B,)))
+    a = _args(want, target_logits=target_logits, draft_logits=draft_logits, draft_tokens=draft_tokens, cu_rows=cu_rows,
+              d2t=d2t, t2d=t2d, u=u, gumbel=gumbel, tokens=tokens, n_accepted=n_accepted)
+    _check(lib().hspec_verify(C.byref(vc), *a, ptr(ws), ws.numel(), stream_ptr()))

@@ -1,0 +1,201 @@
+"""hspec_chunk_attn against a plain float64 attention: ragged batches, head layouts, windows, page sizes, both
+types, split and unsplit caches, what masked slots hold, bad arguments on the device, graphs and streams."""
+import pytest
+
+from paper_2609_24197_amd import hspec
+
+pytestmark = pytest.mark.gpu
+
+HEADS = [(4, 1, 64), (32, 8, 128), (8, 8, 128), (15, 5, 64), (7, 1, 128)]
+
+
+def _u():
+    import target_util
+    return target_util
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Hq,Hkv,D", HEADS)
+@pytest.mark.parametrize("ctx,new", [([0], [1]), ([63], [1]), ([0, 5, 300, 64], [1, 1, 1, 1]), ([0, 17, 200], [7, 16, 3]),
+                                     ([0, 1, 500], [33, 0, 64]), ([0, 129], [130, 77])])
+def test_shapes(Hq, Hkv, D, ctx, new, dtype):
+    u = _u()
+    _, ws = u.check_attend(u.batch(ctx, new, Hq, Hkv, D, dtype=dtype, seed=len(ctx) + new[0]))
+    assert hspec.read_status(ws) == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("window", [1, 2, 15, 16, 17, 64, 100, 1000])
+@pytest.mark.parametrize("ctx,new", [([0, 40], [50, 1]), ([700, 333, 0], [1, 17, 2])])
+def test_windows(ctx, new, window, dtype):
+    u = _u()
+    x = u.batch(ctx, new, 8, 2, 128 if window % 2 else 64, window=window, dtype=dtype, seed=window)
+    # pages that no row sees are gone from the table
+    for b, L in enumerate(ctx):
+        x["table"][b, :max(0, L - window + 1) // x["ps"]] = -1
+    full = u.batch(ctx, new, 8, 2, 128 if window % 2 else 64, window=window, dtype=dtype, seed=window)
+    o, ws = u.attend(x)
+    ref, tol = u.attend_ref(full)
+    N = sum(new)
+    assert ((o.double() - ref).abs() <= tol)[:N].all()
+    assert hspec.read_status(ws) == 0
+
+
+@pytest.mark.parametrize("ps", [16, 32, 64, 128, 1024])
+def test_page_sizes(ps):
+    u = _u()
+    u.check_attend(u.batch([0, 1000, 77], [20, 5, 1], 16, 4, 128, ps=ps, seed=ps))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [1, 5, 40])
+def test_long_caches_are_split(n, dtype):
+    u = _u()
+    u.check_attend(u.batch([20011, 3, 9000], [n, n, n], 8, 2, 128, dtype=dtype, seed=n))
+
+
+def test_many_requests():
+    import torch
+    u = _u()
+    r = torch.Generator().manual_seed(3)
+    B = 1500                                            # more than one round of the plan's 1024
+    ctx = torch.randint(0, 60, (B,), generator=r).tolist()
+    new = torch.randint(0, 4, (B,), generator=r).tolist()
+    u.check_attend(u.batch(ctx, new, 4, 2, 64, seed=9))
+
+
+def test_prompt_of_many_tiles():
+    u = _u()
+    u.check_attend(u.batch([0, 100], [1500, 611], 16, 4, 128, seed=5))
+
+
+def test_scale_and_large_scores():
+    u = _u()
+    x = u.batch([100, 3], [9, 30], 8, 2, 128, scale=0.7, seed=8)       # scores up to tens: one key takes nearly all
+    u.check_attend(x)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("what", [float("nan"), float("inf"), -float("inf")])
+def test_later_tokens_never_change_a_row(dtype, what):
+    """Values of keys a row does not see reach no output, whatever they are; rows that see them show them."""
+    import torch
+    u = _u()
+    ctx, new = [37, 0], [70, 21]
+    x = u.batch(ctx, new, 8, 2, 128, dtype=dtype, seed=4)
+    clean, _ = u.attend(x)
+    b, i = 0, 41                                          # token 41 of request 0 goes bad
+    pos = ctx[b] + i
+    slot = int(x["table"][b, pos // 16]), pos % 16
+    x["v_cache"][slot[0], slot[1], 1, 5] = what
+    o, _ = u.attend(x)
+    g = 4
+    assert torch.equal(o[:i], clean[:i]) and torch.equal(o[new[0]:], clean[new[0]:])
+    seen = o[i:new[0], g:, 5]                             # the heads that read KV head 1
+    assert (torch.isnan(seen) if what != what else seen == what).all()
+    same = torch.ones_like(o, dtype=torch.bool)
+    same[i:new[0], g:, 5] = False
+    assert torch.equal(o[same], clean[same])
+    x["k_cache"][slot[0], slot[1], 0, :] = float("nan")
+    o, _ = u.attend(x)
+    assert torch.equal(o[:i], clean[:i]) and torch.isnan(o[i:new[0], :g].float()).all()
+
+
+def test_bad_pages_read_as_zeros():
+    import torch
+    u = _u()
+    x = u.batch([100], [3], 8, 2, 128, seed=1)
+    page = int(x["table"][0, 2])
+    y = {**x, "k_cache": x["k_cache"].clone(), "v_cache": x["v_cache"].clone()}
+    y["k_cache"][page] = 0
+    y["v_cache"][page] = 0
+    want, _ = u.attend(y)
+    for bad in (-1, x["pages"], 2 ** 31 - 1):
+        x["table"][0, 2] = bad
+        o, ws = u.attend(x)
+        assert torch.equal(o, want)
+        assert hspec.read_status(ws) == hspec.DEV_BAD_PAGE
+
+
+def test_bad_rows_and_lengths_are_clamped():
+    import torch
+    u = _u()
+    x = u.batch([20, 30], [4, 6], 8, 2, 128, seed=2)
+    for cu, bit in (([0, 11, 10], hspec.DEV_BAD_ROWS), ([0, 4, 2 ** 30], hspec.DEV_BAD_ROWS), ([-5, 4, 10], hspec.DEV_BAD_ROWS),
+                    ([0, 10, 10], hspec.DEV_BAD_ROWS), ([2, 4, 10], hspec.DEV_BAD_ROWS)):
+        y = {**x, "cu": torch.tensor(cu, dtype=torch.int32, device="cuda")}
+        o, ws = u.attend(y)
+        assert hspec.read_status(ws) & bit, cu
+    for lens in ([-1, 30], [20, 2 ** 31 - 1], [20, 31]):
+        y = {**x, "lens": torch.tensor(lens, dtype=torch.int32, device="cuda")}
+        o, ws = u.attend(y)
+        assert hspec.read_status(ws) & hspec.DEV_BAD_CTX_LEN, lens
+    good, ws = u.attend(x)
+    assert hspec.read_status(ws) == 0
+
+
+def test_a_request_longer_than_the_positions_there_are():
+    import torch
+    u = _u()
+    x = u.batch([0], [40], 4, 1, 64, seed=2, window=4)
+    o, ws = u.attend(x, max_len=16)                       # rows past position 16 + 3 see nothing: zeros
+    assert hspec.read_status(ws) == hspec.DEV_BAD_CTX_LEN
+    ref, tol = u.attend_ref(x)
+    assert ((o.double() - ref).abs() <= tol)[:16].all()
+    assert torch.count_nonzero(o[20:40]) == 0
+
+
+def test_same_bits_every_time_and_wherever_pages_live():
+    import torch
+    u = _u()
+    x = u.batch([5000, 300, 0], [3, 1, 200], 16, 4, 128, seed=6)
+    a, ws = u.attend(x)
+    for _ in range(3):
+        b, _ = u.attend(x, ws=ws)
+        assert torch.equal(a, b)
+    perm = torch.randperm(x["pages"], device="cuda")
+    y = dict(x)
+    y["k_cache"], y["v_cache"] = x["k_cache"][perm].contiguous(), x["v_cache"][perm].contiguous()
+    back = torch.empty_like(perm)
+    back[perm] = torch.arange(x["pages"], device="cuda")
+    y["table"] = torch.where(x["table"] >= 0, back[x["table"].clamp(min=0).long()].int(), x["table"])
+    c, _ = u.attend(y)
+    assert torch.equal(a, c)
+
+
+def test_a_row_does_not_depend_on_its_batch():
+    """The same request alone: close, not equal (its cache may be split elsewhere)."""
+    u = _u()
+    x = u.batch([900, 4000], [17, 17], 8, 2, 128, seed=3)
+    o, _ = u.check_attend(x)
+    y = u.batch([900], [17], 8, 2, 128, seed=3)
+    u.check_attend(y)
+
+
+def test_graph_and_streams():
+    import torch
+    u = _u()
+    x, y = u.batch([300, 0], [17, 60], 8, 2, 128, seed=1), u.batch([4000], [5], 8, 2, 128, seed=2)
+    want_x, ws_x = u.attend(x)
+    want_y, ws_y = u.attend(y)
+    ox, oy = torch.zeros_like(x["q"]), torch.zeros_like(y["q"])
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(5):                                    # two calls at once, a workspace each
+        with torch.cuda.stream(s1):
+            u.attend(x, ws=ws_x, o=ox)
+        with torch.cuda.stream(s2):
+            u.attend(y, ws=ws_y, o=oy)
+    torch.cuda.synchronize()
+    N, M = 77, 5
+    assert torch.equal(ox[:N], want_x[:N]) and torch.equal(oy[:M], want_y[:M])
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        u.attend(x, ws=ws_x, o=ox)
+        u.attend(y, ws=ws_y, o=oy)
+    for i in range(4):
+        x["q"].normal_(generator=torch.Generator(device="cuda").manual_seed(i))
+        g.replay()
+        torch.cuda.synchronize()
+        want, _ = u.attend(x)
+        assert torch.equal(ox[:N], want[:N]) and torch.equal(oy[:M], want_y[:M])
