@@ -12,8 +12,9 @@
 // any order serves).  K and V tiles stream into LDS by direct DMA, the next tile while one is multiplied; in a page
 // a wave's 16 rows are consecutive, so a tile costs a wave one page id.
 //
-// Three kernels: the plan (one workgroup: checks, list of units with the longest first, clears), the units, and
-// the merge of rows whose keys were split.  Few rows and long caches are split over keys so that the chip is full;
+// Kernels: the plan (one workgroup: checks, list of units with the longest first, clears), the units, those of
+// them with values that are not finite once more where requests can have several new tokens, and the merge of rows
+// whose keys were split.  Few rows and long caches are split over keys so that the chip is full;
 // pieces are merged in key order, so results do not depend on timing.
 //
 // fp32 storage takes the fp32 matrix products (32 x 32 x 2), so nothing is rounded below 32 bits.
@@ -41,8 +42,15 @@ static __device__ __align__(16) const unsigned char zero_row[512] = {};
 // many powers of two; probabilities then stay below 2^8.
 constexpr float CHUNK_SLACK = 8.f;
 
-template <class T, int D, int NW, int KT>
+// NW waves, KT keys per tile.  ONCE: a request's rows
+// fit one tile, so its K and V are read once: non-temporal loads, and a die takes all heads of its units, so that it
+// reads whole rows of the cache; otherwise a die keeps to its KV heads, whose K and V the tiles of a request share
+// in its L2.
+template <class T_, int D_, int NW_, int KT_, bool ONCE_>
 struct Chunk {
+  typedef T_ T;
+  static constexpr int D = D_, NW = NW_, KT = KT_, AUX = ONCE_ ? 2 : 0;
+  static constexpr bool ONCE = ONCE_;
   static constexpr int NT = 64 * NW;
   static constexpr int ROWS = 32 * NW;
   static constexpr int EPC = 16 / sizeof(T);       // elements per 16-byte piece
@@ -54,7 +62,11 @@ struct Chunk {
   static constexpr int GR = WROWS < 16 ? WROWS : 16;   // of them in one page for certain
   static constexpr int NG = WROWS / GR;
   static constexpr int NI = GR * CPR / 64;         // DMA instructions per group and tensor
+  static constexpr int WPE = sizeof(T) == 4 && D == 128 ? 1 : 2;   // waves per SIMD the registers are sized for
   static_assert(KT % 32 == 0 && GR * CPR % 64 == 0 && WROWS % GR == 0, "tile shape");
+  // workgroups that fit a compute unit: 128 pieces of 1280 bytes of LDS, WPE waves on each of four SIMDs
+  static constexpr int LDS = (4 * TILE * (int)sizeof(T) + 8 + 1279) / 1280;
+  static constexpr int PER_CU = 128 / LDS < 4 * WPE / NW ? 128 / LDS : 4 * WPE / NW;
 };
 
 // Element offset of (row, column d) in a K/V tile: 16-byte piece c of row r lives at piece c ^ f(r).  f makes the
@@ -96,26 +108,15 @@ __device__ __forceinline__ bf16x8 v_frag(const bf16* sV, int s, int db, int lane
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// Whether any of n values in LDS is infinite or NaN (the whole wave gets the answer).
-template <class T>
-__device__ __forceinline__ bool tile_odd(const T* t, int n, int lane) {
-  bool bad = false;
-#pragma unroll 4
-  for (int i = lane * (16 / (int)sizeof(T)); i < n; i += 64 * (16 / (int)sizeof(T))) {
-    const u32x4 x = *reinterpret_cast<const u32x4*>(t + i);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      bad |= (x[e] & 0x7f800000u) == 0x7f800000u;
-      if constexpr (sizeof(T) == 2) bad |= (x[e] & 0x7f80u) == 0x7f80u;
-    }
-  }
-  return __any(bad);
-}
-
-// One unit's rows of one KV head.
-template <class T, int D, int NW, int KT>
-__device__ __forceinline__ void chunk_unit(const ChunkAttnArgs& a, const ChunkUnit& u, int h, T* st0, T* st1) {
-  using C = Chunk<T, D, NW, KT>;
+// One unit's rows of one KV head.  Returns whether this lane's row came out with a value that is not finite.
+// ODD: a key that a row does not see has weight 0 in the second product, and where its V is infinite or NaN, 0 x V
+// would reach the row all the same.  So in partly masked tiles such values are taken out of the product and added
+// to the rows that see them, as sums that overflow (a NaN as +inf and -inf).
+template <class C, bool ODD>
+__device__ __forceinline__ bool chunk_unit(const ChunkAttnArgs& a, const ChunkUnit& u, int h, typename C::T* st0,
+                                           typename C::T* st1) {
+  typedef typename C::T T;
+  constexpr int D = C::D, KT = C::KT;
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int NQ = F32 ? D / 8 : D / 16;        // 16-byte pieces of a row per lane
   typedef typename std::conditional<F32, f32x4, bf16x8>::type Frag;
@@ -140,7 +141,8 @@ __device__ __forceinline__ void chunk_unit(const ChunkAttnArgs& a, const ChunkUn
   const int back = a.window > 0 ? a.window - 1 : INT_MAX;   // (positions are far below 2^31)
   auto sees_from = [&](int tok) { return max(u.L + tok - back, 0); };
   auto sees_to = [&](int tok) { return min(min(u.L + tok + 1, a.cap), u.k1); };
-  const int lo = sees_from(i_tok), hi = real ? sees_to(i_tok) : INT_MIN;
+  const int lo = sees_from(i_tok), hi = real ? sees_to(i_tok) : 0;
+  const unsigned span = (unsigned)max(hi - lo, 0);
   const int any_lo = sees_from(t_first), any_hi = sees_to(t_last);
   const int all_lo = sees_from(t_last), all_hi = sees_to(t_first);
   // first key any row of the unit sees: rows before it in the tile are not read
@@ -160,39 +162,68 @@ __device__ __forceinline__ void chunk_unit(const ChunkAttnArgs& a, const ChunkUn
 
   const int ntiles = u.k1 > u.k0 ? (u.k1 - u.k0 + KT - 1) / KT : 0;
   const int32_t* ptab = a.page_table + (size_t)u.b * a.max_pages;
-  // page ids of this wave's row groups of tile ti (loaded a tile ahead of their use)
-  auto load_pids = [&](int ti, int (&pid)[C::NG]) {
-#pragma unroll
-    for (int n = 0; n < C::NG; ++n) {
-      const int key = u.k0 + ti * KT + wave * C::WROWS + n * C::GR;
-      const bool any = key + C::GR > k_min && key < u.k1;
-      pid[n] = any ? ptab[key >> lps] : -1;
-    }
+  // Page ids [pg0, pg0 + 256) of the table, lane by lane in four registers (-1 past the unit's last page): a tile's
+  // ids cost no load of their own, which would have to wait for the DMA that went out before it.
+  int pg0 = 0, id0, id1, id2, id3;
+  const int pg_end = u.k1 > u.k0 ? ((u.k1 - 1) >> lps) + 1 : 0;
+  auto load_ids = [&](int pg) {
+    pg0 = pg;
+    const int e = pg + lane;
+    id0 = e < pg_end ? ptab[e] : -1;
+    id1 = e + 64 < pg_end ? ptab[e + 64] : -1;
+    id2 = e + 128 < pg_end ? ptab[e + 128] : -1;
+    id3 = e + 192 < pg_end ? ptab[e + 192] : -1;
   };
+  load_ids(k_min >> lps);
+  auto page_id = [&](int pg) -> int {
+    const int e = pg - pg0;
+    const int v0 = __builtin_amdgcn_readlane(id0, e & 63), v1 = __builtin_amdgcn_readlane(id1, e & 63);
+    const int v2 = __builtin_amdgcn_readlane(id2, e & 63), v3 = __builtin_amdgcn_readlane(id3, e & 63);
+    return e < 128 ? (e < 64 ? v0 : v1) : (e < 192 ? v2 : v3);
+  };
+  // this lane's row and 16-byte piece of each DMA instruction of a group (the same in every group), and its offset
+  unsigned at[C::NI];
+  int rr[C::NI], piece[C::NI];
+#pragma unroll
+  for (int i = 0; i < C::NI; ++i) {
+    rr[i] = (i * 64 + lane) / C::CPR;
+    const int r = wave * C::WROWS + rr[i];
+    piece[i] = kv_off<T, C::CPR>(r, (i * 64 + lane) % C::CPR * C::EPC) - r * D;   // stored at this lane's place
+    at[i] = (unsigned)(rr[i] * row_elems + piece[i]) * (unsigned)sizeof(T);
+  }
   // DMA of tile ti into a stage: K rows, then V rows
-  auto issue = [&](int ti, T* sb, const int (&pids)[C::NG]) {
+  auto issue = [&](int ti, T* sb) {
 #pragma unroll
     for (int n = 0; n < C::NG; ++n) {
       const int r0 = wave * C::WROWS + n * C::GR;
       const int key0 = u.k0 + ti * KT + r0;
-      const int pid = __builtin_amdgcn_readfirstlane(pids[n]);
-      const bool any = key0 + C::GR > k_min && key0 < u.k1;
-      const bool good = any && pid >= 0 && pid < a.num_pages;
-      if (any && !good && lane == 0) set_status(a.status, ST_BAD_PAGE);
-      const size_t base = good ? (((size_t)pid << lps) + (key0 & (a.ps - 1))) * row_elems + h * D : 0;
-      const T* kp = good ? Kc + base : reinterpret_cast<const T*>(zero_row);
-      const T* vp = good ? Vc + base : reinterpret_cast<const T*>(zero_row);
-      const int stride = good ? row_elems : 0;
-      // rows outside the visible range repeat one inside it (they are masked, and a stale slot may hold NaN)
-      const int first = max(k_min - key0, 0), last = max(min(u.k1 - key0, C::GR) - 1, 0);
+      const bool any = key0 + C::GR > k_min && key0 < u.k1;   // a group with nothing visible has no page
+      if (any && (key0 >> lps) >= pg0 + 256) load_ids(key0 >> lps);
+      const int pid = any ? page_id(key0 >> lps) : -1;
+      const bool good = (unsigned)pid < (unsigned)a.num_pages;
+      const size_t base = (((size_t)(good ? pid : 0) << lps) + (key0 & (a.ps - 1))) * row_elems + h * D;
+      const char* kp = reinterpret_cast<const char*>(Kc + base);
+      const char* vp = reinterpret_cast<const char*>(Vc + base);
+      unsigned off[C::NI];
+#pragma unroll
+      for (int i = 0; i < C::NI; ++i) off[i] = at[i];
+      if (!good || key0 < k_min || key0 + C::GR > u.k1) {
+        // Rows outside the visible range repeat one inside it (they are masked, and a stale slot may hold NaN);
+        // rows of a page outside the pool, and groups with nothing visible, are zeros.
+        if (any && !good && lane == 0) set_status(a.status, ST_BAD_PAGE);
+        const int first = max(k_min - key0, 0), last = max(min(u.k1 - key0, C::GR) - 1, 0);
+        if (!good) kp = vp = reinterpret_cast<const char*>(zero_row);
+#pragma unroll
+        for (int i = 0; i < C::NI; ++i)
+          off[i] = (unsigned)((good ? min(max(rr[i], first), last) * row_elems : 0) + piece[i]) * (unsigned)sizeof(T);
+      }
+      int to = r0 * D;
+      asm volatile("" : "+s"(to));   // (else the LDS address of every instruction and stage takes a register of its own)
 #pragma unroll
       for (int i = 0; i < C::NI; ++i) {
-        const int rr = (i * 64 + lane) / C::CPR, slot = (i * 64 + lane) % C::CPR;
-        const int piece = kv_off<T, C::CPR>(r0 + rr, slot * C::EPC) / C::EPC - (r0 + rr) * C::CPR;   // stored here
-        const int off = min(max(rr, first), last) * stride + piece * C::EPC;
-        T* dst = sb + r0 * D + i * 64 * C::EPC;
-        __builtin_amdgcn_global_load_lds((const GLB_AS void*)(kp + off), (LDS_AS void*)dst, 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((const GLB_AS void*)(vp + off), (LDS_AS void*)(dst + C::TILE), 16, 0, 0);
+        T* dst = sb + to + i * 64 * C::EPC;
+        __builtin_amdgcn_global_load_lds((const GLB_AS void*)(kp + off[i]), (LDS_AS void*)dst, 16, 0, C::AUX);
+        __builtin_amdgcn_global_load_lds((const GLB_AS void*)(vp + off[i]), (LDS_AS void*)(dst + C::TILE), 16, 0, C::AUX);
       }
     }
   };
@@ -210,35 +241,38 @@ __device__ __forceinline__ void chunk_unit(const ChunkAttnArgs& a, const ChunkUn
     f32x16 st[C::NB];
 #pragma unroll
     for (int kb = 0; kb < C::NB; ++kb) st[kb] = zero16();
+    {
+      // every K fragment first, then the products interleaved across key blocks
+      Frag kf[C::NB][NQ];
 #pragma unroll
-    for (int s = 0; s < NQ; ++s)
+      for (int s = 0; s < NQ; ++s)
 #pragma unroll
-      for (int kb = 0; kb < C::NB; ++kb) {
-        const Frag kf = *reinterpret_cast<const Frag*>(
-            sK + kv_off<T, C::CPR>(kb * 32 + l32, F32 ? 8 * s + 4 * hf : 16 * s + 8 * hf));
-        if constexpr (F32) {
+        for (int kb = 0; kb < C::NB; ++kb)
+          kf[kb][s] = *reinterpret_cast<const Frag*>(
+              sK + kv_off<T, C::CPR>(kb * 32 + l32, F32 ? 8 * s + 4 * hf : 16 * s + 8 * hf));
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            st[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], qf[s][e], st[kb], 0, 0, 0);
-        } else {
-          st[kb] = mma32(kf, qf[s], st[kb]);
+      for (int s = 0; s < NQ; ++s)
+#pragma unroll
+        for (int kb = 0; kb < C::NB; ++kb) {
+          if constexpr (F32) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              st[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[kb][s][e], qf[s][e], st[kb], 0, 0, 0);
+          } else {
+            st[kb] = mma32(kf[kb][s], qf[s], st[kb]);
+          }
         }
-      }
+    }
 
     const bool full = base + KT <= all_hi && base >= all_lo;
-    bool odd = false;
     if (!full) {
 #pragma unroll
       for (int kb = 0; kb < C::NB; ++kb)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int key = base + kb * 32 + 8 * (i / 4) + 4 * hf + i % 4;
-          if (key < lo || key >= hi) st[kb][i] = -INFINITY;
+          if ((unsigned)(key - lo) >= span) st[kb][i] = -INFINITY;
         }
-      // Values of V that are not finite: a key that a row does not see has weight 0 in the product, and 0 x NaN
-      // would reach the row all the same.  Here they are taken out of the product and added to the rows that see
-      // them, as sums that overflow (a NaN as +inf and -inf).
-      odd = tile_odd(sV, C::TILE, lane);
     }
     float mx = -INFINITY;
 #pragma unroll
@@ -264,66 +298,71 @@ __device__ __forceinline__ void chunk_unit(const ChunkAttnArgs& a, const ChunkUn
         l_run += e;
       }
 
-    if constexpr (F32) {
+    // O^T += V^T P^T.  P enters as bf16 with bf16 storage (2^-9 relative to each weight, like the V it multiplies);
+    // the sum above takes the unrounded weights.
+    auto add_values = [&](auto masked_) {
+      constexpr bool FIX = ODD && decltype(masked_)::value;
+      if constexpr (F32) {
 #pragma unroll
-      for (int kb = 0; kb < C::NB; ++kb)
+        for (int kb = 0; kb < C::NB; ++kb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int row = kb * 32 + 8 * (i / 4) + 4 * hf + i % 4;
+          for (int i = 0; i < 16; ++i) {
+            const int row = kb * 32 + 8 * (i / 4) + 4 * hf + i % 4;
+#pragma unroll
+            for (int db = 0; db < C::NDB; ++db) {
+              float v = sV[kv_off<T, C::CPR>(row, db * 32 + l32)];
+              if constexpr (FIX) {
+                const float sees = base + row >= lo && base + row < hi ? FLT_MAX : 0.f;
+                const bool fin = fabsf(v) < INFINITY;
+                o[db] += __builtin_amdgcn_mfma_f32_32x32x2f32(fin || v < 0.f ? 0.f : FLT_MAX, sees, zero16(), 0, 0, 0);
+                o[db] += __builtin_amdgcn_mfma_f32_32x32x2f32(fin || v > 0.f ? 0.f : -FLT_MAX, sees, zero16(), 0, 0, 0);
+                if (!fin) v = 0.f;
+                }
+              o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, st[kb][i], o[db], 0, 0, 0);
+            }
+          }
+      } else {
+#pragma unroll
+        for (int s = 0; s < 2 * C::NB; ++s) {
+          bf16x8 pf;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) pf[j] = f2bf(st[s / 2][8 * (s & 1) + j]);
 #pragma unroll
           for (int db = 0; db < C::NDB; ++db) {
-            float v = sV[kv_off<T, C::CPR>(row, db * 32 + l32)];
-            if (odd) {
-              const float sees = base + row >= lo && base + row < hi ? FLT_MAX : 0.f;
-              const bool fin = fabsf(v) < INFINITY;
-              o[db] += __builtin_amdgcn_mfma_f32_32x32x2f32(fin || v < 0.f ? 0.f : FLT_MAX, sees, zero16(), 0, 0, 0);
-              o[db] += __builtin_amdgcn_mfma_f32_32x32x2f32(fin || v > 0.f ? 0.f : -FLT_MAX, sees, zero16(), 0, 0, 0);
-              if (!fin) v = 0.f;
+            bf16x8 vf = v_frag<C::CPR>(sV, s, db, lane);
+            if constexpr (FIX) {
+              s16x8 bits = __builtin_bit_cast(s16x8, vf), up, dn, sees;
+#pragma unroll
+              for (int j = 0; j < 8; ++j) {
+                const bool fin = (bits[j] & 0x7f80) != 0x7f80, nan = !fin && (bits[j] & 0x7f);
+                const int key = base + 16 * s + 8 * (j / 4) + 4 * hf + j % 4;
+                up[j] = (short)(!fin && (nan || bits[j] >= 0) ? 0x7f7f : 0);   // the largest bf16
+                dn[j] = (short)(!fin && (nan || bits[j] < 0) ? 0xff7f : 0);
+                sees[j] = (short)(key >= lo && key < hi ? 0x7f7f : 0);
+                if (!fin) bits[j] = 0;
+              }
+              o[db] += mma32(__builtin_bit_cast(bf16x8, up), __builtin_bit_cast(bf16x8, sees), zero16());
+              o[db] += mma32(__builtin_bit_cast(bf16x8, dn), __builtin_bit_cast(bf16x8, sees), zero16());
+              vf = __builtin_bit_cast(bf16x8, bits);
             }
-            o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, st[kb][i], o[db], 0, 0, 0);
+            o[db] = mma32(vf, pf, o[db]);
           }
-        }
-    } else {
-      // P enters the second product as bf16 (2^-9 relative to each weight, like the V it multiplies); the sum above
-      // takes the unrounded weights
-#pragma unroll
-      for (int s = 0; s < 2 * C::NB; ++s) {
-        bf16x8 pf;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) pf[j] = f2bf(st[s / 2][8 * (s & 1) + j]);
-#pragma unroll
-        for (int db = 0; db < C::NDB; ++db) {
-          bf16x8 vf = v_frag<C::CPR>(sV, s, db, lane);
-          if (odd) {
-            s16x8 bits = __builtin_bit_cast(s16x8, vf), up, dn, sees;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const bool fin = (bits[j] & 0x7f80) != 0x7f80, nan = !fin && (bits[j] & 0x7f);
-              const int key = base + 16 * s + 8 * (j / 4) + 4 * hf + j % 4;
-              up[j] = (short)(!fin && (nan || bits[j] >= 0) ? 0x7f7f : 0);   // the largest bf16
-              dn[j] = (short)(!fin && (nan || bits[j] < 0) ? 0xff7f : 0);
-              sees[j] = (short)(key >= lo && key < hi ? 0x7f7f : 0);
-              if (!fin) bits[j] = 0;
-            }
-            o[db] += mma32(__builtin_bit_cast(bf16x8, up), __builtin_bit_cast(bf16x8, sees), zero16());
-            o[db] += mma32(__builtin_bit_cast(bf16x8, dn), __builtin_bit_cast(bf16x8, sees), zero16());
-            vf = __builtin_bit_cast(bf16x8, bits);
-          }
-          o[db] = mma32(vf, pf, o[db]);
         }
       }
+    };
+    if constexpr (ODD) {
+      if (!full) add_values(std::true_type{});
+      else add_values(std::false_type{});
+    } else {
+      add_values(std::false_type{});
     }
   };
 
-  int pids[C::NG];
-  load_pids(0, pids);
-  if (ntiles > 0) issue(0, st0, pids);
-  if (ntiles > 1) load_pids(1, pids);
+  if (ntiles > 0) issue(0, st0);
   auto step = [&](int ti, T* mine, T* other) {
     wait_vmcnt<0>();
     wg_barrier();   // every wave's part of tile ti has landed, and every wave has left the other stage
-    if (ti + 1 < ntiles) issue(ti + 1, other, pids);
-    if (ti + 2 < ntiles) load_pids(ti + 2, pids);
+    if (ti + 1 < ntiles) issue(ti + 1, other);
     compute(ti, mine);
   };
   for (int t0 = 0; t0 < ntiles; t0 += 2) {
@@ -333,7 +372,14 @@ __device__ __forceinline__ void chunk_unit(const ChunkAttnArgs& a, const ChunkUn
 
   // lane holds O[row l32][d = 32 db + 8 (i / 4) + 4 hf + i % 4]
   const float l = half_sum(l_run);
-  if (!real) return;
+  bool bad = false;
+  if constexpr (!ODD) {
+#pragma unroll
+    for (int db = 0; db < C::NDB; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) bad |= !(fabsf(o[db][i]) < INFINITY);
+  }
+  if (!real) return false;
   if (u.slot < 0) {
     const float inv = hi > lo ? 1.f / l : 0.f;   // (a row that sees no key is zero)
     T* dst = static_cast<T*>(a.o) + q_off + 4 * hf;
@@ -357,57 +403,93 @@ __device__ __forceinline__ void chunk_unit(const ChunkAttnArgs& a, const ChunkUn
             f32x4{o[db][4 * q], o[db][4 * q + 1], o[db][4 * q + 2], o[db][4 * q + 3]};
     if (hf == 0) *reinterpret_cast<float2*>(a.part_ml + pr * 2) = float2{m_run, l};
   }
+  return bad;
 }
 
-template <class T, int D, int NW, int KT>
-__global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2)))
+template <class C>
+// (256 threads for every NW: with fewer the compiler counts on one wave per SIMD and puts O into accumulation
+// registers, which costs a copy of it both ways in every tile)
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(C::WPE)))
 chunk_attn_kernel(ChunkAttnArgs a) {
-  using C = Chunk<T, D, NW, KT>;
-  __shared__ __align__(16) T st0[2 * C::TILE];   // two stages, so that the compiler can tell the one being read
-  __shared__ __align__(16) T st1[2 * C::TILE];   // from the one whose DMA is in flight
+  // one LDS object per stage, so that the compiler can tell the one being read from the one whose DMA is in flight
+  __shared__ __align__(16) typename C::T st0[2 * C::TILE];
+  __shared__ __align__(16) typename C::T st1[2 * C::TILE];
   __shared__ int s_item[2];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int n_items = min(a.status[1], a.max_units) * a.Hkv;
-  // Items go by class (item mod 8): a class's items share KV heads and its workgroups a die's L2.  A workgroup's
-  // first item is its own index; the next come from its class's counter, then from the other classes'.
-  // Each claim goes out at the start of an item and is looked at at its end.
-  const int grid = gridDim.x;
-  const int cls = blockIdx.x % kChunkClasses;
-  auto item_of = [&](int c, int ticket) -> int {
-    const long long it = ((long long)ticket + (grid - c + kChunkClasses - 1) / kChunkClasses) * kChunkClasses + c;
-    return it < n_items ? (int)it : -1;
+  // Work goes by class, one per die (workgroups go to the dies in turn): unit v of head h is in class v mod 8, or
+  // (v Hkv + h) mod 8.  A workgroup's first ticket is its place in its class; the next come from the class's
+  // counter, then from the other classes'.  Each claim goes out at the start of an item and is looked at at its end.
+  const int n_units = min(a.status[1], a.max_units);
+  const int grid = gridDim.x;   // a multiple of the classes
+  const int cls = blockIdx.x % kChunkClasses, own = grid / kChunkClasses;
+  auto tickets = [&](int c) {   // of a class
+    return C::ONCE ? (n_units - c + kChunkClasses - 1) / kChunkClasses * a.Hkv
+                   : (n_units * a.Hkv - c + kChunkClasses - 1) / kChunkClasses;
   };
+  const bool one_each = tickets(0) <= own;
   auto counter = [&](int c) { return a.queue + c * kChunkQueueStride; };
+  auto item_of = [&](int c, int t) {
+    if (t >= tickets(c)) return -1;
+    return C::ONCE ? (t / a.Hkv * kChunkClasses + c) * a.Hkv + t % a.Hkv : t * kChunkClasses + c;
+  };
   // lanes of wave 0: an item of any class, or -1
   auto steal = [&]() -> int {
     for (;;) {
-      int c = (cls + lane) % kChunkClasses, t = INT_MAX - grid;
-      if (lane < kChunkClasses) t = __hip_atomic_load(counter(c), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      const unsigned long long some = __ballot(lane < kChunkClasses && item_of(c, t) >= 0);
+      int c = (cls + lane) % kChunkClasses, t = 0;
+      if (lane < kChunkClasses) t = own + __hip_atomic_load(counter(c), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      const unsigned long long some = __ballot(lane < kChunkClasses && t < tickets(c));
       if (!some) return -1;
       c = (cls + __builtin_ctzll(some)) % kChunkClasses;
       int got = 0;
       if (lane == 0) got = atomicAdd(counter(c), 1);
-      const int it = item_of(c, __builtin_amdgcn_readfirstlane(got));
+      const int it = item_of(c, own + __builtin_amdgcn_readfirstlane(got));
       if (it >= 0) return it;
     }
   };
-  int item = blockIdx.x < n_items ? (int)blockIdx.x : -1;
-  for (int turn = 0; item >= 0; turn ^= 1) {
+  int turn = 0;
+  auto shared = [&](int it) -> int {   // wave 0's item, for all
+    if (tid == 0) s_item[turn] = it;
+    __syncthreads();   // (and every wave is done with the last one)
+    it = __builtin_amdgcn_readfirstlane(s_item[turn]);
+    turn ^= 1;
+    return it;
+  };
+  int item = item_of(cls, blockIdx.x / kChunkClasses);
+  if (item < 0 && !one_each) item = shared(wave == 0 ? steal() : 0);   // (uniform) fewer units in the class than workgroups
+  while (item >= 0) {
     int ticket = 0;
-    if (tid == 0 && n_items > grid) ticket = atomicAdd(counter(cls), 1);
+    if (tid == 0 && !one_each) ticket = atomicAdd(counter(cls), 1);
     const ChunkUnit u = a.units[item / a.Hkv];
     const int h = item % a.Hkv;
-    chunk_unit<T, D, NW, KT>(a, u, h, st0, st1);
-    if (n_items <= grid) break;
-    if (wave == 0) {
-      int it = item_of(cls, __builtin_amdgcn_readfirstlane(ticket));
-      if (it < 0) it = steal();
-      if (lane == 0) s_item[turn] = it;
+    const bool bad = chunk_unit<C, false>(a, u, h, st0, st1);
+    // (one entry a wave at most: the same item twice is done twice, with the same result)
+    if (a.redo && __any(bad) && lane == 0) {
+      const int at = atomicAdd(a.status + 3, 1);
+      if (at < a.max_redo) a.redo[at] = item;
     }
-    __syncthreads();   // the next item is known; every wave is done with this one
-    item = __builtin_amdgcn_readfirstlane(s_item[turn]);
+    if (one_each) break;
+    int it = 0;
+    if (wave == 0) {
+      it = item_of(cls, own + __builtin_amdgcn_readfirstlane(ticket));
+      if (it < 0) it = steal();
+    }
+    item = shared(it);
+  }
+}
+
+// The units some row of which came out infinite or NaN, once more with masked values kept apart (rare: the list is
+// empty where V is finite and nothing overflows).
+template <class C>
+__global__ void __launch_bounds__(C::NT) chunk_redo_kernel(ChunkAttnArgs a) {
+  __shared__ __align__(16) typename C::T st0[2 * C::TILE];
+  __shared__ __align__(16) typename C::T st1[2 * C::TILE];
+  const int n = min(a.status[3], a.max_redo);
+  for (int i = blockIdx.x; i < n; i += gridDim.x) {
+    const int item = a.redo[i];
+    const ChunkUnit u = a.units[item / a.Hkv];
+    chunk_unit<C, true>(a, u, item % a.Hkv, st0, st1);
+    __syncthreads();
   }
 }
 
@@ -437,10 +519,10 @@ __device__ __forceinline__ TileKeys tile_keys(const ChunkAttnArgs& a, int g, int
   return r;
 }
 
-// One workgroup lists the units.  Every tile of rows has len keys; tiles longer than S = max(min_split, all keys
-// x Hkv / target) are cut into ceil(len / S) even pieces, so the pieces of all tiles number at most target / Hkv
-// more than the tiles, and the split ones twice that (what the workspace holds).  Units are written longest first
-// (64 classes of length), which keeps the queue's tail short.
+// One workgroup lists the units.  Every tile of rows has len keys; tiles longer than S >= keys of all tiles x Hkv /
+// target are cut into ceil(len / S) even pieces, so the pieces of all tiles number at most target / Hkv more than the
+// tiles, and the split ones twice that (what the workspace holds).  Units are written longest first (64 classes of
+// length), which keeps the queue's tail short.
 __global__ void __launch_bounds__(PL_THREADS) chunk_plan(ChunkAttnArgs a) {
   __shared__ PlanLds s;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -492,19 +574,37 @@ __global__ void __launch_bounds__(PL_THREADS) chunk_plan(ChunkAttnArgs a) {
     return lo;
   };
   const int chunks = (a.B + PL_THREADS - 1) / PL_THREADS;
-  int tiles = 0;
+  int tiles = 0, all_tiles = 0;
+  struct Tile {
+    int r, tile, k0, len;
+  };
+  Tile mine{0, 0, 0, 0};   // this thread's first tile, where there is one chunk
+  auto tile_of = [&](int t) -> Tile {
+    const int r = request_of(t), tile = t - s.first[r];
+    const TileKeys k = tile_keys(a, g, tile, s.n[r], s.L[r]);
+    return Tile{r, tile, k.k0, max(k.k1 - k.k0, 0)};
+  };
+  auto each = [&](bool again, auto f) {
+    for (int c = 0; c < chunks; ++c) {
+      if (chunks > 1 || !again) tiles = load(c * PL_THREADS);
+      if (!again) all_tiles += tiles;
+      for (int t = tid; t < tiles; t += PL_THREADS) {
+        if (t == tid && again && chunks == 1) {
+          f(c * PL_THREADS, mine);
+          continue;
+        }
+        const Tile x = tile_of(t);
+        if (t == tid) mine = x;
+        f(c * PL_THREADS, x);
+      }
+    }
+  };
   unsigned long long keys = 0;
   int longest = 0;
-  for (int c = 0; c < chunks; ++c) {
-    tiles = load(c * PL_THREADS);
-    for (int t = tid; t < tiles; t += PL_THREADS) {
-      const int r = request_of(t);
-      const TileKeys k = tile_keys(a, g, t - s.first[r], s.n[r], s.L[r]);
-      const int len = max(k.k1 - k.k0, 0);
-      keys += len;
-      longest = max(longest, len);
-    }
-  }
+  each(false, [&](int, const Tile& x) {
+    keys += x.len;
+    longest = max(longest, x.len);
+  });
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
     keys += __shfl_xor(keys, o);
@@ -515,37 +615,27 @@ __global__ void __launch_bounds__(PL_THREADS) chunk_plan(ChunkAttnArgs a) {
     atomicMax(&s.longest, longest);
   }
   __syncthreads();
-  // keys per unit, in whole key tiles
-  const unsigned long long per = (s.keys * a.Hkv + a.target - 1) / a.target;
-  const int S = (int)(((per < (unsigned long long)a.min_split ? (unsigned long long)a.min_split
-                                                              : min(per, 1ull << 30)) + a.key_tile - 1) / a.key_tile * a.key_tile);
-  const int top = min(S, s.longest) + 1;
-  auto pieces_of = [&](int len, int& q) -> int {
-    if (len <= S) {
-      q = max(len, 1);
-      return 1;
-    }
-    const int p = (int)(((long long)len + S - 1) / S);
-    q = ((len + p - 1) / p + a.key_tile - 1) / a.key_tile * a.key_tile;
-    return (len + q - 1) / q;
+  // Keys per unit, in whole key tiles: where the tiles leave most of the chip free, what makes one round of units
+  // (so every piece starts at once: 1 request of 32768 tokens 53 us, 79 in two short rounds), else 13/8 rounds, which
+  // the queue evens out.  (The factor covers the float roundings.)
+  const float spare = (float)a.slots - (float)all_tiles * (float)a.Hkv;
+  const float units = spare * 4.f >= (float)a.slots * 3.f ? spare : (float)a.target;
+  const float per = (float)s.keys * (float)a.Hkv / units * 1.0001f;
+  const int S = ((int)fminf(fmaxf(per, (float)a.min_split), 1e9f) + a.key_tile) / a.key_tile * a.key_tile;
+  const int shift = max(26 - __builtin_clz(min(S, s.longest) | 1), 0);   // lengths >> shift are below 64
+  auto bucket = [&](int len) -> int { return PL_BUCKETS - 1 - min(len >> shift, PL_BUCKETS - 1); };
+  auto pieces_of = [&](int len, int& q) -> int {   // pieces, and the length of all but the last
+    q = max(len, 1);
+    if (len <= S) return 1;
+    const unsigned p = ((unsigned)len + S - 1) / (unsigned)S;
+    q = (((unsigned)len + p - 1) / p + a.key_tile - 1) / a.key_tile * a.key_tile;
+    return ((unsigned)len + q - 1) / (unsigned)q;
   };
-  auto bucket = [&](int len) -> int { return PL_BUCKETS - 1 - (int)((long long)min(len, top - 1) * PL_BUCKETS / top); };
-  auto each = [&](auto f) {
-    for (int c = 0; c < chunks; ++c) {
-      if (chunks > 1) tiles = load(c * PL_THREADS);
-      for (int t = tid; t < tiles; t += PL_THREADS) {
-        const int r = request_of(t), tile = t - s.first[r];
-        const TileKeys k = tile_keys(a, g, tile, s.n[r], s.L[r]);
-        int q;
-        const int p = pieces_of(max(k.k1 - k.k0, 0), q);
-        f(c * PL_THREADS + r, r, tile, k, q, p);
-      }
-    }
-  };
-  each([&](int, int, int, const TileKeys& k, int q, int p) {
-    const int len = max(k.k1 - k.k0, 0);
+  each(true, [&](int, const Tile& x) {
+    int q;
+    const int p = pieces_of(x.len, q);
     if (p > 1) atomicAdd(&s.hist[bucket(q)], p - 1);
-    atomicAdd(&s.hist[bucket(len - (p - 1) * q)], 1);
+    atomicAdd(&s.hist[bucket(x.len - (p - 1) * q)], 1);
   });
   __syncthreads();
   if (wave == 0) {   // exclusive prefix of the 64 buckets
@@ -560,30 +650,33 @@ __global__ void __launch_bounds__(PL_THREADS) chunk_plan(ChunkAttnArgs a) {
     if (lane == 63) a.status[1] = v;
   }
   __syncthreads();
-  each([&](int b, int r, int tile, const TileKeys& k, int q, int p) {
-    const int len = max(k.k1 - k.k0, 0);
+  each(true, [&](int b0, const Tile& x) {
+    int q;
+    const int p = pieces_of(x.len, q), b = b0 + x.r;
+    const int row0 = s.row0[x.r], n = s.n[x.r], L = s.L[x.r];
     int slot = -1;
     if (p > 1) {
       slot = atomicAdd(&s.slots, p);
       const int e = atomicAdd(&s.n_splits, 1);
       if (slot + p <= a.max_slots && e < a.max_splits)
-        a.splits[e] = ChunkSplit{b, tile, slot, p, s.row0[r], s.n[r], s.L[r], 0};
+        a.splits[e] = ChunkSplit{b, x.tile, slot, p, row0, n, L, 0};
       else   // (cu that divides the rows cannot need more than the workspace holds)
         slot = INT_MIN;
     }
     for (int i = 0; i < p; ++i) {
       const bool whole = slot == INT_MIN && i == 0;   // (then the other pieces are empty)
-      const int k0 = k.k0 + i * q, k1 = whole || i == p - 1 ? k.k1 : k0 + q;
-      const int at = atomicAdd(&s.hist[bucket(i == p - 1 ? len - i * q : q)], 1);
+      const int at0 = i * q, at1 = whole || i == p - 1 ? x.len : at0 + q;
+      const int at = atomicAdd(&s.hist[bucket(i == p - 1 ? x.len - at0 : q)], 1);
       if (at >= a.max_units) continue;
       if (slot == INT_MIN && !whole) a.units[at] = ChunkUnit{b, 0, 0, 0, -1, 0, 0, 0};
-      else a.units[at] = ChunkUnit{b, tile, k0, k1, slot < 0 ? -1 : slot + i, s.row0[r], s.n[r], s.L[r]};
+      else a.units[at] = ChunkUnit{b, x.tile, x.k0 + at0, x.k0 + at1, slot < 0 ? -1 : slot + i, row0, n, L};
     }
   });
   __syncthreads();
   if (tid == 0) {
     a.status[0] = s.bits;
     a.status[2] = min(s.n_splits, a.max_splits);
+    a.status[3] = 0;
   }
 }
 
@@ -591,9 +684,29 @@ __global__ void __launch_bounds__(PL_THREADS) chunk_plan(ChunkAttnArgs a) {
 
 constexpr int MG_THREADS = 256;
 
-// o = sum_i O_i 2^(m_i - m*) / sum_i l_i 2^(m_i - m*) over the pieces in key order; a thread takes four dims of a row.
+// o = sum_i O_i 2^(m_i - m*) / sum_i l_i 2^(m_i - m*) over a row's pieces, in an order of their own (not of time).
+// Bound by the round trips of a row's loads: a workgroup takes one row, with its pieces spread over groups of D / 4
+// threads, where that makes few workgroups (few rows, so perhaps many pieces each: 1 request of 32768 tokens, 128
+// pieces, 77 us for the whole call with a thread for all of a row's pieces, now 48), else 1024 / D rows.
+constexpr int MG_FEW = 4096;   // workgroups up to which each takes one row
+
 template <class T, int D>
-__global__ void __launch_bounds__(MG_THREADS) chunk_merge(ChunkAttnArgs a, int blocks) {
+__device__ __forceinline__ void merge_store(const ChunkAttnArgs& a, const ChunkSplit& s, int h, int c, int d, f32x4 acc, float l) {
+  const int g = a.Hq / a.Hkv, tok = c / g;
+  const long long pos = (long long)s.L + tok;
+  const long long lo = a.window > 0 ? pos - a.window + 1 : 0;
+  acc *= min(pos + 1, (long long)a.cap) > lo ? 1.f / l : 0.f;   // (a row that sees no key is zero)
+  T* dst = static_cast<T*>(a.o) + ((size_t)(s.row0 + tok) * a.Hq + h * g + (c - tok * g)) * D + d;
+  if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(dst) = acc;
+  else *reinterpret_cast<bf16x4*>(dst) = bf16x4{f2bf(acc[0]), f2bf(acc[1]), f2bf(acc[2]), f2bf(acc[3])};
+}
+// Weight of a piece: 0 where the row sees nothing of it.
+__device__ __forceinline__ float piece_weight(float2 ml, float m_use) {
+  return ml.x == -INFINITY && ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - m_use);
+}
+
+template <class T, int D>
+__global__ void __launch_bounds__(MG_THREADS) chunk_merge_rows(ChunkAttnArgs a, int blocks) {
   constexpr int PR = MG_THREADS * 4 / D;   // rows per workgroup
   constexpr int U = 4;
   const int g = a.Hq / a.Hkv;
@@ -628,28 +741,86 @@ __global__ void __launch_bounds__(MG_THREADS) chunk_merge(ChunkAttnArgs a, int b
       }
 #pragma unroll
       for (int x = 0; x < U; ++x) {
-        if (i + x >= s.pieces) break;
-        if (ml[x].x == -INFINITY && ml[x].y == 0.f) continue;   // a piece the row sees nothing of
-        const float f = __builtin_amdgcn_exp2f(ml[x].x - m_use);
+        const float f = i + x < s.pieces ? piece_weight(ml[x], m_use) : 0.f;
+        if (f == 0.f) continue;   // (an O of 0 x infinity stays out)
         l += ml[x].y * f;
         acc += o[x] * f;
       }
     }
-    const int tok = c / g;
-    const long long pos = (long long)s.L + tok;
-    const long long lo = a.window > 0 ? pos - a.window + 1 : 0;
-    const float inv = min(pos + 1, (long long)a.cap) > lo ? 1.f / l : 0.f;
-    acc *= inv;
-    T* dst = static_cast<T*>(a.o) + ((size_t)(s.row0 + tok) * a.Hq + h * g + (c - tok * g)) * D + d;
-    if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(dst) = acc;
-    else *reinterpret_cast<bf16x4*>(dst) = bf16x4{f2bf(acc[0]), f2bf(acc[1]), f2bf(acc[2]), f2bf(acc[3])};
+    merge_store<T, D>(a, s, h, c, d, acc, l);
+  }
+}
+
+template <class T, int D>
+__global__ void __launch_bounds__(MG_THREADS) chunk_merge_row(ChunkAttnArgs a, int rows) {
+  constexpr int TPR = D / 4, G = MG_THREADS / TPR;   // threads of a row, groups of pieces
+  constexpr int U = 4, CH = MG_THREADS;              // pieces in flight per group, pieces per round
+  __shared__ float s_w[CH], s_m[MG_THREADS / 64], s_l[MG_THREADS / 64];
+  __shared__ __align__(16) f32x4 s_o[MG_THREADS];
+  const int g = a.Hq / a.Hkv, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int n = a.status[2] * a.Hkv * rows;
+  for (int w = blockIdx.x; w < n; w += gridDim.x) {
+    const int e = w / (a.Hkv * rows), h = w / rows % a.Hkv, rr = w % rows;
+    const ChunkSplit s = a.splits[e];
+    const int c = s.tile * a.tile_rows + rr;
+    if (c >= s.n * g) continue;   // (uniform)
+    const size_t p0 = ((size_t)s.slot * a.Hkv + h) * a.tile_rows + rr, step = (size_t)a.Hkv * a.tile_rows;
+    const int grp = tid / TPR, d = tid % TPR * 4;
+    auto piece_o = [&](int i) { return *reinterpret_cast<const f32x4*>(a.part_o + (p0 + min(i, s.pieces - 1) * step) * D + d); };
+    f32x4 o[U];   // the first pieces' O on its way beside the maxima
+#pragma unroll
+    for (int x = 0; x < U; ++x) o[x] = piece_o(grp + x * G);
+    float m = -INFINITY;
+    for (int i = tid; i < s.pieces; i += CH) m = fmaxf(m, a.part_ml[(p0 + i * step) * 2]);
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
+    if (lane == 0) s_m[wave] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
+    const float m_use = m == -INFINITY ? 0.f : m;
+    float l = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int c0 = 0; c0 < s.pieces; c0 += CH) {
+      if (c0) __syncthreads();   // the last round's weights are read
+      float f = 0.f;
+      if (c0 + tid < s.pieces) {
+        const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (p0 + (c0 + tid) * step) * 2);
+        f = piece_weight(ml, m_use);
+        if (f != 0.f) l += ml.y * f;
+      }
+      s_w[tid] = f;
+      __syncthreads();
+      const int top = min(CH, s.pieces - c0);
+      for (int i = grp; i < top; i += U * G) {
+        if (c0 || i != grp) {
+#pragma unroll
+          for (int x = 0; x < U; ++x) o[x] = piece_o(c0 + i + x * G);
+        }
+#pragma unroll
+        for (int x = 0; x < U; ++x) {
+          const float v = i + x * G < top ? s_w[i + x * G] : 0.f;
+          if (v != 0.f) acc += o[x] * v;   // (an O of 0 x infinity stays out)
+        }
+      }
+    }
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) l += __shfl_xor(l, x);
+    if (lane == 0) s_l[wave] = l;
+    s_o[tid] = acc;
+    __syncthreads();
+    if (grp == 0) {
+#pragma unroll
+      for (int x = 1; x < G; ++x) acc += s_o[x * TPR + tid];
+      merge_store<T, D>(a, s, h, c, d, acc, (s_l[0] + s_l[1]) + (s_l[2] + s_l[3]));
+    }
+    __syncthreads();   // s_m, s_l and s_o are filled again
   }
 }
 
 // ----------------------------------------------------------------------------- launch
 
-// Tile of the units: rows per wave are 32; one, two or four waves by the rows a request can have (n g), so that a
-// workgroup of few rows is not mostly idle waves.  Tiles of 32 keys where one wave or fp32 rows would make 64 too large.
+// Tile of the units: 32 rows per wave; one, two or four waves by the rows a request can have (n g), so that a
+// workgroup of few rows is not mostly idle waves.
 template <class F>
 auto with_variant(const ChunkAttnArgs& a, F f) {
   const long long R = (long long)a.max_new * (a.Hq / a.Hkv);
@@ -657,27 +828,28 @@ auto with_variant(const ChunkAttnArgs& a, F f) {
     typedef typename decltype(t)::type T;
     constexpr int D = decltype(d)::value;
     constexpr int KT = sizeof(T) == 4 ? 32 : 64;
-    if (R <= 32) return f(t, d, Int<1>{}, Int<32>{});
-    if (R <= 64) return f(t, d, Int<2>{}, Int<KT>{});
-    return f(t, d, Int<4>{}, Int<KT>{});
+    if (R <= 32) return f(Chunk<T, D, 1, 32, true>{});
+    if (R <= 64) return f(Chunk<T, D, 2, KT, true>{});
+    if (R <= 128) return f(Chunk<T, D, 4, KT, true>{});
+    return f(Chunk<T, D, 4, KT, false>{});
   };
   if (a.f32) return a.D == 128 ? by_rows(std::common_type<float>{}, Int<128>{}) : by_rows(std::common_type<float>{}, Int<64>{});
   return a.D == 128 ? by_rows(std::common_type<bf16>{}, Int<128>{}) : by_rows(std::common_type<bf16>{}, Int<64>{});
 }
 
-constexpr int CHUNK_TARGET = 1024;    // units (x KV heads) that splitting aims for
-constexpr int CHUNK_MIN_SPLIT = 256;  // keys a piece has at least
+constexpr int CHUNK_MIN_SPLIT = 64;   // keys a piece has at least
 
 }  // namespace
 
 void chunk_bounds(ChunkAttnArgs& a) {
-  with_variant(a, [&](auto, auto, auto nw, auto kt) {
-    a.tile_rows = 32 * decltype(nw)::value;
-    a.key_tile = decltype(kt)::value;
+  with_variant(a, [&](auto c) {
+    a.tile_rows = decltype(c)::ROWS;
+    a.key_tile = decltype(c)::KT;
+    a.slots = decltype(c)::PER_CU * 256;
     return 0;
   });
   a.min_split = CHUNK_MIN_SPLIT;
-  a.target = CHUNK_TARGET;
+  a.target = a.slots * 13 / 8;
   const long long g = a.Hq / a.Hkv;
   const long long per_req = ((long long)a.max_new * g + a.tile_rows - 1) / a.tile_rows;
   const long long tiles = std::min((long long)a.T * g / a.tile_rows + a.B, per_req * a.B);
@@ -688,15 +860,16 @@ void chunk_bounds(ChunkAttnArgs& a) {
   a.max_units = (int)std::min(tiles * cuts, tiles + extra);
   a.max_slots = cuts > 1 ? (int)std::min(tiles * cuts, 2 * extra) : 0;
   a.max_splits = (int)std::min(tiles, (long long)a.max_slots / 2);
+  a.max_redo = a.max_units * a.Hkv * (a.tile_rows / 32);   // an entry for every wave
 }
 
 hipError_t launch_chunk_attn(const ChunkAttnArgs& a, hipStream_t s) {
   hipLaunchKernelGGL(chunk_plan, dim3(1), dim3(PL_THREADS), 0, s, a);
   if (hipError_t e = hipGetLastError()) return e;
-  return with_variant(a, [&](auto t, auto d, auto nw, auto kt) -> hipError_t {
-    typedef typename decltype(t)::type T;
-    constexpr int D = decltype(d)::value, NW = decltype(nw)::value, KT = decltype(kt)::value;
-    constexpr auto kern = chunk_attn_kernel<T, D, NW, KT>;
+  return with_variant(a, [&](auto c) -> hipError_t {
+    using C = decltype(c);
+    constexpr int D = C::D, NW = C::NW;
+    constexpr auto kern = chunk_attn_kernel<C>;
     static int slots_of[64] = {};   // resident workgroups, per device
     int dev = 0;
     if (hipError_t e = hipGetDevice(&dev)) return e;
@@ -708,13 +881,24 @@ hipError_t launch_chunk_attn(const ChunkAttnArgs& a, hipStream_t s) {
       if (e != hipSuccess) return e;
       slots = cus * (per_cu > 0 ? per_cu : 1);
     }
-    const long long items = (long long)a.max_units * a.Hkv;
+    const long long items = (a.max_units + kChunkClasses - 1LL) / kChunkClasses * kChunkClasses * a.Hkv;
+    slots = std::max(slots / kChunkClasses * kChunkClasses, kChunkClasses);
     hipLaunchKernelGGL(kern, dim3((unsigned)std::min(items, (long long)slots)), dim3(64 * NW), 0, s, a);
     if (hipError_t e = hipGetLastError()) return e;
+    if (a.redo) {
+      hipLaunchKernelGGL((chunk_redo_kernel<C>), dim3((unsigned)std::min(items, 64LL)), dim3(64 * NW), 0, s, a);
+      if (hipError_t e = hipGetLastError()) return e;
+    }
     if (a.max_splits > 0) {
-      const int blocks = (a.tile_rows * D / 4 + MG_THREADS - 1) / MG_THREADS;
-      const long long wgs = (long long)a.max_splits * a.Hkv * blocks;
-      hipLaunchKernelGGL((chunk_merge<T, D>), dim3((unsigned)std::min(wgs, 4096LL)), dim3(MG_THREADS), 0, s, a, blocks);
+      const long long rows = std::min((long long)a.tile_rows, (long long)a.max_new * (a.Hq / a.Hkv));
+      const long long singles = (long long)a.max_splits * a.Hkv * rows;
+      if (singles <= MG_FEW) {
+        hipLaunchKernelGGL((chunk_merge_row<typename C::T, D>), dim3((unsigned)singles), dim3(MG_THREADS), 0, s, a, (int)rows);
+      } else {
+        const int blocks = (int)((rows * D / 4 + MG_THREADS - 1) / MG_THREADS);
+        const long long wgs = std::min((long long)a.max_splits * a.Hkv * blocks, 2048LL);
+        hipLaunchKernelGGL((chunk_merge_rows<typename C::T, D>), dim3((unsigned)wgs), dim3(MG_THREADS), 0, s, a, blocks);
+      }
     }
     return hipGetLastError();
   });

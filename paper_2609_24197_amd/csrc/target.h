@@ -49,14 +49,15 @@ struct ChunkAttnArgs {
   int window = 0, f32 = 0;
   int cap = 0;                        // positions a request can have: min(max_len, max_pages ps)
   float scale_log2 = 0.f;
-  int* status = nullptr;              // [0] status, [1] units, [2] split tiles
+  int* status = nullptr;              // [0] status, [1] units, [2] split tiles, [3] items to do again
   int* queue = nullptr;               // [kChunkClasses * kChunkQueueStride]
   ChunkUnit* units = nullptr;
   ChunkSplit* splits = nullptr;
+  int* redo = nullptr;                // items to do again, status[3] of them; null: rows of a request see the same keys
   float* part_o = nullptr;            // [slots][Hkv][tile rows][D]
   float* part_ml = nullptr;           // [slots][Hkv][tile rows][2]
   // filled from chunk_shape / chunk_bounds
-  int tile_rows = 0, key_tile = 0, min_split = 0, target = 0, max_units = 0, max_slots = 0, max_splits = 0;
+  int tile_rows = 0, key_tile = 0, min_split = 0, slots = 0, target = 0, max_units = 0, max_slots = 0, max_splits = 0, max_redo = 0;
 };
 // The tile the launch uses for these arguments, and the most units, partial slots and split tiles it can need.
 void chunk_bounds(ChunkAttnArgs& a);
