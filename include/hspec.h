@@ -502,7 +502,8 @@ size_t hspec_chunk_attn_workspace(const hspec_chunk_cfg* cfg, int max_len);
  * NaN logits count as -inf and +inf as the largest float; they, a NaN of gumbel and a row of nothing but
  * -inf set HSPEC_DEV_NONFINITE (rows up to a are looked at); a draft id outside [0, draft_vocab)
  * or a mapped id out of range does not stand (or counts as -1) and sets HSPEC_DEV_BAD_TOKEN;
- * HSPEC_DEV_BAD_ROWS as above, with max_new = k + 1.
+ * HSPEC_DEV_BAD_ROWS as above, with max_new = k + 1.  B <= 32767, k <= 4096, B (k+1) and rows <= 2^22,
+ * draft_vocab <= vocab <= 2^19.
  */
 typedef struct {
   int B, k, rows, vocab, draft_vocab;

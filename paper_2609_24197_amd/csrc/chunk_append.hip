@@ -41,42 +41,72 @@ __device__ __forceinline__ void store_e(T* p, const float (&v)[E]) {
 #pragma unroll
     for (int i = 0; i < E; i += 4) *reinterpret_cast<f32x4*>(p + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
   } else {
-    static_assert(E == 8, "one 16-byte store");
-    bf16x8 x;
+    typedef bf16 Vec __attribute__((ext_vector_type(E)));
+    Vec x;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = f2bf(v[e]);
-    *reinterpret_cast<bf16x8*>(p) = x;
+    for (int e = 0; e < E; ++e) x[e] = f2bf(v[e]);
+    *reinterpret_cast<Vec*>(p) = x;
   }
 }
 
+// Turns per position of each RoPE pair, theta^(-2p/D) / 2 pi: from the host, since 64-bit powers and divisions on the
+// way to every token's angles sit on the critical path of a call of few tokens.
+struct Turns {
+  double per_pos[64];
+};
+
 // Checks of the whole call by one workgroup, which alone writes the status word: the rows' division, the
-// lengths, and the page of every position written.
+// lengths, and the page of every position written.  A thread takes a request; requests of many pages are left to a
+// wave each.
 __device__ void check_call(const ChunkAppendArgs& a) {
-  __shared__ int s_bits;
-  if (threadIdx.x == 0) s_bits = 0;
-  __syncthreads();
+  __shared__ int s_bits, s_big, s_list[AP_THREADS];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (tid == 0) s_bits = 0;
   int bits = 0;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int b = wave; b < a.B; b += AP_THREADS / 64) {
+  auto page_ok = [&](int b, int pg) {
+    const int id = a.page_table[(size_t)b * a.max_pages + pg];
+    return id >= 0 && id < a.num_pages;
+  };
+  auto pages = [&](int b, int& first, int& last) {   // last < first: none
     const ChunkRows r = chunk_rows(a.cu, b, a.T, a.max_new);
     const ChunkPos p = chunk_pos(a.ctx_lens[b], r.n, a.cap);
-    bits |= (r.ok ? 0 : ST_BAD_ROWS) | (p.ok ? 0 : ST_BAD_CTX_LEN);
-    if (r.n == 0) continue;
-    const int last = (min(p.L + r.n, a.cap) - 1) / a.ps;
-    for (int pg = p.L / a.ps + lane; pg <= last; pg += 64) {
-      const int id = a.page_table[(size_t)b * a.max_pages + pg];
-      if (id < 0 || id >= a.num_pages) bits |= ST_BAD_PAGE;
+    first = p.L / a.ps;
+    last = r.n ? (min(p.L + r.n, a.cap) - 1) / a.ps : -1;
+    return (r.ok ? 0 : ST_BAD_ROWS) | (p.ok ? 0 : ST_BAD_CTX_LEN);
+  };
+  constexpr int OWN = 4;
+  for (int b0 = 0; b0 < a.B; b0 += AP_THREADS) {
+    __syncthreads();
+    if (tid == 0) s_big = 0;
+    __syncthreads();
+    if (b0 + tid < a.B) {
+      int first, last;
+      bits |= pages(b0 + tid, first, last);
+      if (last - first >= OWN) {
+        s_list[atomicAdd(&s_big, 1)] = b0 + tid;
+      } else {
+#pragma unroll
+        for (int i = 0; i < OWN; ++i)
+          if (first + i <= last && !page_ok(b0 + tid, first + i)) bits |= ST_BAD_PAGE;
+      }
+    }
+    __syncthreads();
+    for (int i = wave; i < s_big; i += AP_THREADS / 64) {
+      int first, last;
+      pages(s_list[i], first, last);
+      for (int pg = first + lane; pg <= last; pg += 64)
+        if (!page_ok(s_list[i], pg)) bits |= ST_BAD_PAGE;
     }
   }
   if (bits) atomicOr(&s_bits, bits);
   __syncthreads();
-  if (threadIdx.x == 0) a.status[0] = s_bits;
+  if (tid == 0) a.status[0] = s_bits;
 }
 
 // TB tokens per workgroup.  The last workgroup checks the call (no launch clears the status word).
 template <class Tin, class T, int TB>
-__global__ void __launch_bounds__(AP_THREADS) chunk_append_kernel(ChunkAppendArgs a, double log2_theta) {
-  constexpr int E = sizeof(T) == 2 ? 8 : 4;
+__global__ void __launch_bounds__(AP_THREADS) chunk_append_kernel(ChunkAppendArgs a, Turns turns) {
+  constexpr int E = sizeof(Tin) == 2 && sizeof(T) == 2 ? 8 : 4;   // 16 bytes of the wider side per load or store
   if (blockIdx.x == gridDim.x - 1) {
     check_call(a);
     return;
@@ -87,51 +117,62 @@ __global__ void __launch_bounds__(AP_THREADS) chunk_append_kernel(ChunkAppendArg
   const int tid = threadIdx.x, wave = tid >> 6;
   const int r0 = blockIdx.x * TB;
   const int D = a.D, half = D / 2;
-  for (int t = wave; t < TB; t += AP_THREADS / 64) {
-    const int r = r0 + t;
-    const int b = r < a.T ? row_request(a.cu, a.B, r) : -1;
+  const int lph = half / E, heads = a.Hq + 2 * a.Hkv;   // lanes of a head (a power of two, at most 16)
+  const int work = TB * heads * lph;
+  // Lanes past the end repeat the last (shuffles stay whole).  Elements are on their way a round ahead, the first
+  // while positions, slots and angles are found.
+  auto element = [&](int w, int& t, int& hd, int& i0) {
+    w = min(w, work - 1);
+    i0 = w % lph * E;
+    hd = w / lph % heads;
+    t = w / lph / heads;
+  };
+  float x1[E], x2[E], n1[E], n2[E];
+  auto fetch = [&](int w, float (&v1)[E], float (&v2)[E]) {
+    int t, hd, i0;
+    element(w, t, hd, i0);
+    const Tin* src = static_cast<const Tin*>(a.qkv) + ((size_t)min(r0 + t, a.T - 1) * heads + hd) * D + i0;
+    load_e<Tin, E>(src, v1);
+    load_e<Tin, E>(src + half, v2);
+  };
+  fetch(tid, n1, n2);
+  for (int t = wave; t < TB; t += AP_THREADS / 64) {   // a wave per token: its place, then its angles
+    const int r = r0 + t, lane = tid & 63;
+    const RowPlace at = row_place(a.cu, a.ctx_lens, a.B, a.T, a.max_new, r);
     int pos = -1;
     long long slot = -1;
-    if (b >= 0) {
-      const ChunkRows cr = chunk_rows(a.cu, b, a.T, a.max_new);
-      const int i = r - cr.row0;
-      if (i >= 0 && i < cr.n) {
-        pos = chunk_pos(a.ctx_lens[b], cr.n, a.cap).L + i;
-        const int pg = pos / a.ps;
-        if (pg < a.max_pages) {
-          const int id = a.page_table[(size_t)b * a.max_pages + pg];
-          if (id >= 0 && id < a.num_pages) slot = (long long)id * a.ps + pos % a.ps;
-        }
+    if (at.n > 0) {
+      pos = chunk_pos(at.L, at.n, a.cap).L + at.i;
+      const int pg = pos / a.ps;
+      if (pg < a.max_pages) {
+        const int id = a.page_table[(size_t)at.b * a.max_pages + pg];
+        if (id >= 0 && id < a.num_pages) slot = (long long)id * a.ps + pos % a.ps;
       }
     }
-    if ((tid & 63) == 0) {
+    if (lane == 0) {
       s_pos[t] = pos;
       s_slot[t] = slot;
     }
+    if (lane < half) {
+      double rev = (double)pos * turns.per_pos[lane];
+      rev -= rint(rev);
+      float sn, cs;
+      sincosf((float)(rev * 6.283185307179586476925286766559), &sn, &cs);
+      s_cs[t][lane] = cs;
+      s_sn[t][lane] = sn;
+    }
   }
   __syncthreads();
-  for (int i = tid; i < TB * half; i += AP_THREADS) {
-    const int t = i / half, p = i % half;
-    const double inv = p ? exp2(-2.0 * (double)p / (double)D * log2_theta) : 1.0;   // (0 x log2(inf) is NaN)
-    double phi = (double)s_pos[t] * inv;
-    const double two_pi = 6.283185307179586476925286766559;
-    phi -= two_pi * rint(phi / two_pi);
-    float sn, cs;
-    sincosf((float)phi, &sn, &cs);
-    s_cs[t][p] = cs;
-    s_sn[t][p] = sn;
-  }
-  __syncthreads();
-  const int lph = half / E, heads = a.Hq + 2 * a.Hkv;   // lanes of a head (a power of two, at most 16)
-  const int work = TB * heads * lph;
   for (int w0 = 0; w0 < work; w0 += AP_THREADS) {
-    const int w = min(w0 + tid, work - 1);               // (lanes past the end repeat the last: shuffles stay whole)
-    const int t = w / (heads * lph), hd = w / lph % heads, i0 = w % lph * E;
+    int t, hd, i0;
+    element(w0 + tid, t, hd, i0);
     const int pos = s_pos[t];
-    const Tin* src = static_cast<const Tin*>(a.qkv) + ((size_t)min(r0 + t, a.T - 1) * heads + hd) * D + i0;
-    float x1[E], x2[E];
-    load_e<Tin, E>(src, x1);
-    load_e<Tin, E>(src + half, x2);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      x1[e] = n1[e];
+      x2[e] = n2[e];
+    }
+    if (w0 + AP_THREADS < work) fetch(w0 + AP_THREADS + tid, n1, n2);
     const float* gain = hd < a.Hq ? a.qw : a.kw;
     if (hd < a.Hq + a.Hkv) {
       float f = 1.f;
@@ -168,7 +209,9 @@ __global__ void __launch_bounds__(AP_THREADS) chunk_append_kernel(ChunkAppendArg
 
 template <class Tin, class T>
 hipError_t launch_typed(const ChunkAppendArgs& a, hipStream_t s) {
-  const double lt = log2(a.rope_theta);
+  Turns lt{};
+  for (int p = 0; p < a.D / 2; ++p)   // (pair 0 turns by 1 whatever the base)
+    lt.per_pos[p] = (p ? exp2(-2.0 * p / a.D * log2(a.rope_theta)) : 1.0) / 6.283185307179586476925286766559;
   if (a.T >= 2048)
     hipLaunchKernelGGL((chunk_append_kernel<Tin, T, 4>), dim3((a.T + 3) / 4 + 1), dim3(AP_THREADS), 0, s, a, lt);
   else

@@ -420,19 +420,21 @@ chunk_attn_kernel(ChunkAttnArgs a) {
   // Work goes by class, one per die (workgroups go to the dies in turn): unit v of head h is in class v mod 8, or
   // (v Hkv + h) mod 8.  A workgroup's first ticket is its place in its class; the next come from the class's
   // counter, then from the other classes'.  Each claim goes out at the start of an item and is looked at at its end.
-  const int n_units = min(a.status[1], a.max_units);
   const int grid = gridDim.x;   // a multiple of the classes
   const int cls = blockIdx.x % kChunkClasses, own = grid / kChunkClasses;
+  auto place = [&](int c, int t) {   // item of a ticket
+    return C::ONCE ? (t / a.Hkv * kChunkClasses + c) * a.Hkv + t % a.Hkv : t * kChunkClasses + c;
+  };
+  // the first item's unit, read beside the number of units (what it holds past them is not used)
+  ChunkUnit u = a.units[min(place(cls, blockIdx.x / kChunkClasses) / a.Hkv, a.max_units - 1)];
+  const int n_units = min(a.status[1], a.max_units);
   auto tickets = [&](int c) {   // of a class
     return C::ONCE ? (n_units - c + kChunkClasses - 1) / kChunkClasses * a.Hkv
                    : (n_units * a.Hkv - c + kChunkClasses - 1) / kChunkClasses;
   };
   const bool one_each = tickets(0) <= own;
   auto counter = [&](int c) { return a.queue + c * kChunkQueueStride; };
-  auto item_of = [&](int c, int t) {
-    if (t >= tickets(c)) return -1;
-    return C::ONCE ? (t / a.Hkv * kChunkClasses + c) * a.Hkv + t % a.Hkv : t * kChunkClasses + c;
-  };
+  auto item_of = [&](int c, int t) { return t < tickets(c) ? place(c, t) : -1; };
   // lanes of wave 0: an item of any class, or -1
   auto steal = [&]() -> int {
     for (;;) {
@@ -456,11 +458,13 @@ chunk_attn_kernel(ChunkAttnArgs a) {
     return it;
   };
   int item = item_of(cls, blockIdx.x / kChunkClasses);
-  if (item < 0 && !one_each) item = shared(wave == 0 ? steal() : 0);   // (uniform) fewer units in the class than workgroups
+  if (item < 0 && !one_each) {   // (uniform) fewer units in the class than workgroups
+    item = shared(wave == 0 ? steal() : 0);
+    u = a.units[max(item, 0) / a.Hkv];
+  }
   while (item >= 0) {
     int ticket = 0;
     if (tid == 0 && !one_each) ticket = atomicAdd(counter(cls), 1);
-    const ChunkUnit u = a.units[item / a.Hkv];
     const int h = item % a.Hkv;
     const bool bad = chunk_unit<C, false>(a, u, h, st0, st1);
     // (one entry a wave at most: the same item twice is done twice, with the same result)
@@ -475,6 +479,7 @@ chunk_attn_kernel(ChunkAttnArgs a) {
       if (it < 0) it = steal();
     }
     item = shared(it);
+    u = a.units[max(item, 0) / a.Hkv];
   }
 }
 
@@ -495,7 +500,7 @@ __global__ void __launch_bounds__(C::NT) chunk_redo_kernel(ChunkAttnArgs a) {
 
 // ------------------------------------------------------------------------------- plan
 
-constexpr int PL_THREADS = 1024;
+constexpr int PL_THREADS = 256;
 constexpr int PL_BUCKETS = 64;
 
 struct PlanLds {

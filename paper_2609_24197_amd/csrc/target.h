@@ -64,7 +64,12 @@ void chunk_bounds(ChunkAttnArgs& a);
 hipError_t launch_chunk_attn(const ChunkAttnArgs& a, hipStream_t s);
 
 // ------------------------------------------------------------------------ verification
-constexpr int kVerifyKeys = 2;        // per request: best of the residual, best of the target's own
+// What a finished row leaves for the choice: log2 of its sums of 2^x, status bits, greedy's argmax.
+struct VerifyRow {
+  float lse_p, lse_q;
+  int flags, top;
+};
+constexpr int kVerifyLine = 32;   // ints between counters: a 128-byte line each, so that they are not one line's traffic
 struct VerifyArgs {
   const void* target = nullptr;       // [rows, V]
   const float* draft = nullptr;       // [B, k, Vd] or null
@@ -72,12 +77,16 @@ struct VerifyArgs {
   const float *u = nullptr, *gumbel = nullptr;   // null: greedy
   int32_t *tokens = nullptr, *accepted = nullptr;
   int B = 0, k = 0, rows = 0, V = 0, Vd = 0, f32 = 0;
-  float inv_t = 1.f, inv_td = 1.f;
+  float c_t = 1.f, c_d = 1.f;             // log2(e) / temperature, of the target and of the drafts
   int* status = nullptr;
-  float4* stat_t = nullptr;           // [rows][pieces_t]
-  float4* stat_d = nullptr;           // [B*k][pieces_d]
-  unsigned long long* keys = nullptr; // [B][kVerifyKeys]
-  int* count = nullptr;               // [B] workgroups of a request that are done
+  unsigned long long* stat_t = nullptr;   // [rows][pieces_t]
+  unsigned long long* stat_d = nullptr;   // [B*k][pieces_d]
+  VerifyRow* row = nullptr;               // [B][k + 1]
+  int* count = nullptr;                   // [B][k + 1][kVerifyLine] pieces of a row that are done
+  int* n = nullptr;                       // [B][kVerifyLine] first draft found not to stand
+  int2* req = nullptr;                    // [B] first row, drafts
+  int* done = nullptr;                    // [B][kVerifyLine] workgroups of the choice that are done
+  unsigned long long* keys = nullptr;     // [B][kVerifyLine / 2] best (score, token)
   int pieces_t = 0, pieces_d = 0, pieces_r = 0;
 };
 void verify_bounds(VerifyArgs& a);

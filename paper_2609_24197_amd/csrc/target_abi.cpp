@@ -168,7 +168,7 @@ static hspec_status check_verify(const hspec_verify_cfg* c) {
     return fail(HSPEC_ERR_SHAPE, "non-positive verification dimension");
   if (c->draft_vocab > c->vocab)
     return fail(HSPEC_ERR_SHAPE, "the draft vocabulary (%d) is larger than the target's (%d)", c->draft_vocab, c->vocab);
-  if (c->vocab > (1 << 28) || c->B > 32767 || c->k > 4096 || (long long)c->B * c->k > (1 << 22) || c->rows > (1 << 22))
+  if (c->vocab > (1 << 19) || c->B > 32767 || c->k > 4096 || (long long)c->B * (c->k + 1) > (1 << 22) || c->rows > (1 << 22))
     return fail(HSPEC_ERR_UNSUPPORTED, "verification too large");
   return HSPEC_OK;
 }
@@ -177,10 +177,15 @@ static void plan_verify(Arena& ar, const hspec_verify_cfg& c, hspec::VerifyArgs&
   a.B = c.B; a.k = c.k; a.rows = c.rows; a.V = c.vocab; a.Vd = c.draft_vocab; a.f32 = c.dtype == HSPEC_F32;
   hspec::verify_bounds(a);
   a.status = ar.take<int>(64);
-  a.keys = ar.take<unsigned long long>((size_t)c.B * hspec::kVerifyKeys);
-  a.count = ar.take<int>(c.B);
-  a.stat_t = ar.take<float4>((size_t)c.rows * a.pieces_t);
-  a.stat_d = ar.take<float4>((size_t)c.B * c.k * a.pieces_d);
+  const size_t rows = (size_t)c.B * (c.k + 1);
+  a.keys = ar.take<unsigned long long>((size_t)c.B * hspec::kVerifyLine / 2);
+  a.stat_t = ar.take<unsigned long long>((size_t)c.rows * a.pieces_t);
+  a.stat_d = ar.take<unsigned long long>((size_t)c.B * c.k * a.pieces_d);
+  a.row = ar.take<hspec::VerifyRow>(rows);
+  a.count = ar.take<int>(rows * hspec::kVerifyLine);
+  a.n = ar.take<int>((size_t)c.B * hspec::kVerifyLine);
+  a.req = ar.take<int2>(c.B);
+  a.done = ar.take<int>((size_t)c.B * hspec::kVerifyLine);
 }
 
 HSPEC_API size_t hspec_verify_workspace(const hspec_verify_cfg* cfg) {
@@ -202,20 +207,21 @@ HSPEC_API hspec_status hspec_verify(const hspec_verify_cfg* cfg, const void* tar
   if (!u != !gumbel) return fail(HSPEC_ERR_NULL, "sampling needs both u and gumbel, greedy verification neither");
   if (!u && draft_logits) return fail(HSPEC_ERR_UNSUPPORTED, "greedy verification takes no draft logits");
   if (draft_logits && !d2t != !t2d) return fail(HSPEC_ERR_NULL, "draft logits need both vocabulary maps or neither");
-  if (u && !(cfg->temperature > 0.f && std::isfinite(1.f / cfg->temperature)))
+  if (u && !(cfg->temperature > 0.f && std::isfinite((float)(1.5 / cfg->temperature))))
     return fail(HSPEC_ERR_SHAPE, "sampling needs temperature > 0");
-  if (draft_logits && !(cfg->draft_temperature > 0.f && std::isfinite(1.f / cfg->draft_temperature)))
+  if (draft_logits && !(cfg->draft_temperature > 0.f && std::isfinite((float)(1.5 / cfg->draft_temperature))))
     return fail(HSPEC_ERR_SHAPE, "draft logits need draft_temperature > 0");
   if (!cu_rows && cfg->rows != (long long)cfg->B * (cfg->k + 1))
     return fail(HSPEC_ERR_SHAPE, "without cu_rows, rows must be B * (k + 1)");
   if (hspec_status s = check_ws(workspace, ws_bytes, hspec_verify_workspace(cfg))) return s;
   Arena ar{(char*)workspace};
   hspec::VerifyArgs a;
-  a.u = u;
   plan_verify(ar, *cfg, a);
+  a.u = u;
   a.target = target_logits; a.draft = draft_logits; a.draft_tokens = draft_tokens; a.cu = cu_rows; a.d2t = d2t;
   a.t2d = t2d; a.gumbel = gumbel; a.tokens = tokens; a.accepted = n_accepted;
-  a.inv_t = u ? 1.f / cfg->temperature : 1.f;
-  a.inv_td = draft_logits ? 1.f / cfg->draft_temperature : 1.f;
+  const double log2e = 1.4426950408889634074;
+  a.c_t = u ? (float)(log2e / cfg->temperature) : 1.f;
+  a.c_d = draft_logits ? (float)(log2e / cfg->draft_temperature) : 1.f;
   return launched(hspec::launch_verify(a, (hipStream_t)stream));
 }

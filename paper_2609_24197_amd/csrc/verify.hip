@@ -7,10 +7,15 @@
 // (Gumbel-max over the residual distribution; over p_n where no residual is positive).  Greedy: t_j stands
 // while it is the argmax of l_j, and next = argmax l_n.
 //
-// Bound by reading the logits.  Launch 1 takes pieces of rows to (maximum, sum of exponentials, argmax); launch 2
-// joins them, decides n in every workgroup of a request, and reads row n once more for the choice.
+// Bound by reading the logits.  Rows behind the first draft that does not stand are not needed, and which one that
+// is comes out of the rows before it: the pieces of all rows are taken in the order of j by a grid that holds little
+// more than one j of every request at a time; the workgroup that finishes a row decides its draft, and pieces of rows
+// past a request's decision are left out.  Then row n is read once more for the choice.  64 requests x 16 drafts,
+// 131072 bf16 logits: 162 us when every row was read first, now 74.
 #include <algorithm>
 #include <cfloat>
+#include <climits>
+#include <type_traits>
 
 #include "common.h"
 #include "target.h"
@@ -22,23 +27,27 @@ namespace {
 constexpr int VF_THREADS = 256;
 constexpr int ST_BAD_TOKEN = 4;
 constexpr int ST_NONFINITE = 8;
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr int VF_PIECE = 32768;   // bytes of a row that a workgroup takes at a time, all its loads under way together
+constexpr int VF_GRID = 16384;    // (32768-byte pieces, 4096 workgroups: 90 us at 64 x 16 x 131072; 8192: 76; 16384: 74)
+constexpr float LN2 = 0.6931471805599453f;
 
-// A logit over its temperature.  NaN counts as -inf and +inf (or what overflows) as the largest float; both flag.
-__device__ __forceinline__ float scaled(float l, float inv_t, bool& bad) {
-  const float x = l * inv_t;
-  if (x <= FLT_MAX) return x + 0.f;   // (-0 becomes 0: they tie)
+// Logits are taken in units of log 2: x = l c with c = log2(e) / T.
+
+// One as the definition wants it: NaN counts as -inf and +inf (or what overflows) as the largest float; both flag.
+__device__ __forceinline__ float scaled(float l, float c, bool& bad) {
+  const float x = l * c;
+  if (x <= FLT_MAX) return x;
   bad = true;
   return x == x ? FLT_MAX : -INFINITY;
 }
 
-// (maximum, sum of 2^((x - maximum) log2 e)) of what a lane has seen.
+// (maximum, sum of 2^(x - maximum)).
 struct Lse {
   float m = -INFINITY, s = 0.f;
   __device__ __forceinline__ void join(float m2, float s2) {
     const float mn = fmaxf(m, m2);
     const float ref = mn == -INFINITY ? 0.f : mn;
-    s = s * __builtin_amdgcn_exp2f((m - ref) * LOG2E) + s2 * __builtin_amdgcn_exp2f((m2 - ref) * LOG2E);
+    s = s * __builtin_amdgcn_exp2f(m - ref) + s2 * __builtin_amdgcn_exp2f(m2 - ref);
     m = mn;
   }
 };
@@ -71,327 +80,427 @@ __device__ __forceinline__ void each_piece(const T* row, int e0, int e1, F f) {
   }
 }
 
-// Statistics of elements [e0, e1) of a row over the workgroup; thread 0 has the result.
-template <class T, bool GREEDY>
-__device__ __forceinline__ float4 row_stats(const T* row, int e0, int e1, float inv_t) {
-  __shared__ float4 s_w[VF_THREADS / 64];
-  Lse a;
-  unsigned long long best = 0;
-  bool bad = false;
-  each_piece(row, e0, e1, [&](int e, float* v, auto n) {
-    constexpr int N = decltype(n)::value;
-    float mx = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      v[i] = scaled(v[i], inv_t, bad);
-      mx = fmaxf(mx, v[i]);
-    }
-    if constexpr (GREEDY) {
-      if (mx > a.m || best == 0) {   // (a thread's elements come in rising order: the first maximum stays)
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const unsigned long long key = ((unsigned long long)score_ord(v[i]) << 32) | ~(unsigned)(e + i);
-          best = key > best ? key : best;
-        }
-      }
-      a.m = fmaxf(a.m, mx);
-    } else {
-      float s = 0.f;
-      const float ref = mx == -INFINITY ? 0.f : mx;
-#pragma unroll
-      for (int i = 0; i < N; ++i) s += __builtin_amdgcn_exp2f((v[i] - ref) * LOG2E);
-      a.join(mx, s);
-    }
-  });
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    if constexpr (GREEDY) {
-      const unsigned long long k = ((unsigned long long)__shfl_xor((unsigned)(best >> 32), o) << 32) |
-                                   __shfl_xor((unsigned)best, o);
-      best = k > best ? k : best;
-    } else {
-      const float m2 = __shfl_xor(a.m, o), s2 = __shfl_xor(a.s, o);
-      a.join(m2, s2);
-    }
-  }
-  bad = __any(bad);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if (lane == 0)
-    s_w[wave] = GREEDY ? float4{__uint_as_float((unsigned)(best >> 32)), __uint_as_float((unsigned)best), 0.f, bad ? 1.f : 0.f}
-                       : float4{a.m, a.s, 0.f, bad ? 1.f : 0.f};
-  __syncthreads();
-  float4 r = s_w[0];
-  if (threadIdx.x == 0) {
-    Lse t;
-    unsigned long long top = 0;
-    float flag = 0.f;
-    for (int w = 0; w < VF_THREADS / 64; ++w) {
-      const float4 x = s_w[w];
-      flag = fmaxf(flag, x.w);
-      if constexpr (GREEDY) {
-        const unsigned long long k = ((unsigned long long)__float_as_uint(x.x) << 32) | __float_as_uint(x.y);
-        top = k > top ? k : top;
-      } else {
-        t.join(x.x, x.y);
-      }
-    }
-    r = GREEDY ? float4{__uint_as_float((unsigned)(top >> 32)), __uint_as_float((unsigned)top), 0.f, flag}
-               : float4{t.m, t.s, 0.f, flag};
-  }
-  return r;
-}
-
 __device__ __forceinline__ int2 piece_range(int n, int pieces, int p) {
   const int len = ((n + pieces - 1) / pieces + 255) / 256 * 256;
   return int2{min(n, p * len), min(n, (p + 1) * len)};
 }
 
-template <class T, bool GREEDY>
-__global__ void __launch_bounds__(VF_THREADS) verify_stats(VerifyArgs a) {
-  const int w = blockIdx.x;
-  if (threadIdx.x == 0) {
-    if (w == 0) a.status[0] = 0;
-    for (int b = w; b < a.B; b += gridDim.x) {
-      a.count[b] = 0;
-      for (int i = 0; i < kVerifyKeys; ++i) a.keys[b * kVerifyKeys + i] = 0;
-    }
+// A thread's part of a piece of at most VF_PIECE bytes on its way: 16-byte loads from the first aligned element on, and
+// an element of the ragged ends.
+constexpr int VF_VEC = VF_PIECE / (16 * VF_THREADS);
+struct PieceRegs {
+  u32x4 v[VF_VEC];
+  float end;
+  int a0, a1, e;   // aligned range, position of `end` (or -1)
+};
+template <class T>
+__device__ __forceinline__ void load_piece(const T* row, int2 r, PieceRegs& x) {
+  constexpr int N = 16 / sizeof(T);
+  const int mis = (int)((reinterpret_cast<uintptr_t>(row + r.x) / sizeof(T)) % N);
+  x.a0 = min(r.y, r.x + (mis ? N - mis : 0));
+  x.a1 = x.a0 + (r.y - x.a0) / N * N;
+#pragma unroll
+  for (int i = 0; i < VF_VEC; ++i) {
+    const int e = x.a0 + (i * VF_THREADS + (int)threadIdx.x) * N;
+    if (e < x.a1) x.v[i] = *reinterpret_cast<const u32x4*>(row + e);
   }
-  const int nt = a.rows * a.pieces_t;
-  if (w < nt) {
-    const int r = w / a.pieces_t, p = w % a.pieces_t;
-    if (a.cu && r >= a.cu[a.B]) return;
-    const int2 e = piece_range(a.V, a.pieces_t, p);
-    const float4 s = row_stats<T, GREEDY>(static_cast<const T*>(a.target) + (size_t)r * a.V, e.x, e.y, GREEDY ? 1.f : a.inv_t);
-    if (threadIdx.x == 0) a.stat_t[w] = s;
-  } else if constexpr (!GREEDY) {
-    const int x = w - nt, r = x / a.pieces_d, p = x % a.pieces_d;
-    const int b = r / a.k, j = r % a.k;
-    if (a.cu && j >= chunk_rows(a.cu, b, a.rows, a.k + 1).n - 1) return;
-    const int2 e = piece_range(a.Vd, a.pieces_d, p);
-    const float4 s = row_stats<float, false>(a.draft + (size_t)r * a.Vd, e.x, e.y, a.inv_td);
-    if (threadIdx.x == 0) a.stat_d[x] = s;
-  }
+  const int head = x.a0 - r.x, t = threadIdx.x;
+  x.e = t < head ? r.x + t : t < head + (r.y - x.a1) ? x.a1 + t - head : -1;   // (fewer than 2 N of them)
+  if (x.e >= 0) x.end = to_f32(row[x.e]);
 }
 
-// log(sum) of a row's pieces; flag: a value was not finite, or no value is above -inf.
-__device__ __forceinline__ float join_pieces(const float4* s, int n, bool& flag) {
-  Lse t;
-  for (int i = 0; i < n; ++i) {
-    const float4 x = s[i];
-    t.join(x.x, x.y);
-    flag |= x.w != 0.f;
+// What a wave has of a piece: (maximum, sum) or the argmax key, and whether a value was not finite.
+struct PieceStat {
+  Lse l;
+  unsigned long long key = 0;
+  bool bad = false;
+};
+// f(value, element) for a thread's values, the ragged ends' last.
+template <class T, class F>
+__device__ __forceinline__ void each_value(const PieceRegs& x, F f) {
+  constexpr int N = 16 / sizeof(T);
+#pragma unroll
+  for (int i = 0; i < VF_VEC; ++i) {
+    const int e = x.a0 + (i * VF_THREADS + (int)threadIdx.x) * N;
+    if (e < x.a1) {
+#pragma unroll
+      for (int q = 0; q < N; ++q) {
+        if constexpr (N == 4) f(__uint_as_float(x.v[i][q]), e + q);
+        else f(__uint_as_float(q % 2 ? x.v[i][q / 2] & 0xffff0000u : x.v[i][q / 2] << 16), e + q);
+      }
+    }
   }
-  flag |= t.m == -INFINITY;
-  return t.m == -INFINITY ? -INFINITY : t.m + __builtin_amdgcn_logf(t.s) * LN2;
+  if (x.e >= 0) f(x.end, x.e);
+}
+// Two passes over the registers: the maximum (which a NaN comes through), then the sum against it or its first place.
+// Per value a multiply-add, an exponential and half a comparison; values that are not finite take the pieces they
+// are in through it again by the rules of scaled().
+template <class T, bool GREEDY>
+__device__ __forceinline__ PieceStat piece_stat(const PieceRegs& x, float c) {
+  PieceStat s;
+  float mx = -INFINITY;
+  each_value<T>(x, [&](float v, int) { mx = __builtin_elementwise_maximum(mx, v); });
+  bool odd = !(mx <= FLT_MAX) || mx * c > FLT_MAX;
+  if (__any(odd)) {
+    mx = -INFINITY;
+    each_value<T>(x, [&](float v, int) { mx = fmaxf(mx, scaled(v, c, s.bad)); });
+    const float ref = mx == -INFINITY ? 0.f : mx;
+    s.l.m = mx;
+    each_value<T>(x, [&](float v, int e) {
+      const float y = scaled(v, c, s.bad);
+      if constexpr (GREEDY) {
+        const unsigned long long k = ((unsigned long long)score_ord(y + 0.f) << 32) | ~(unsigned)e;
+        s.key = k > s.key ? k : s.key;
+      } else {
+        s.l.s += __builtin_amdgcn_exp2f(y - ref);
+      }
+    });
+  } else if constexpr (GREEDY) {
+    int at = INT_MAX;   // (-0 and 0 are equal)
+    each_value<T>(x, [&](float v, int e) { at = v == mx ? min(at, e) : at; });
+    if (at != INT_MAX) s.key = ((unsigned long long)score_ord(mx + 0.f) << 32) | ~(unsigned)at;
+  } else {
+    s.l.m = mx * c;
+    const float ref = s.l.m == -INFINITY ? 0.f : s.l.m;
+    each_value<T>(x, [&](float v, int) { s.l.s += __builtin_amdgcn_exp2f(__builtin_fmaf(v, c, -ref)); });
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    if constexpr (GREEDY) {
+      const unsigned long long k = ((unsigned long long)__shfl_xor((unsigned)(s.key >> 32), o) << 32) | __shfl_xor((unsigned)s.key, o);
+      s.key = k > s.key ? k : s.key;
+    } else {
+      const float m2 = __shfl_xor(s.l.m, o), s2 = __shfl_xor(s.l.s, o);
+      s.l.join(m2, s2);
+    }
+  }
+  s.bad = __any(s.bad);
+  return s;
+}
+
+// ------------------------------------------------------------------------ rows, decisions
+
+// Drafts of a request and its first row.
+__device__ __forceinline__ ChunkRows request_rows(const VerifyArgs& a, int b) {
+  if (a.cu) return chunk_rows(a.cu, b, a.rows, a.k + 1);
+  return ChunkRows{b * (a.k + 1), a.k + 1, true};
+}
+// Target id of a drafted token, or -1.
+__device__ __forceinline__ int target_id(const VerifyArgs& a, int d) {
+  const int t = d < 0 || d >= a.Vd ? -1 : a.d2t ? a.d2t[d] : d;
+  return t < a.V ? max(t, -1) : -1;
 }
 // x - lse, for rows of nothing but -inf too
 __device__ __forceinline__ float log_prob(float x, float lse) { return x == -INFINITY ? -INFINITY : x - lse; }
-__device__ __forceinline__ float exp_nat(float x) { return __builtin_amdgcn_exp2f(x * LOG2E); }
+
+__global__ void verify_init(VerifyArgs a) {
+  const int i = blockIdx.x * blockDim.x + threadIdx.x;
+  if (i == 0) a.status[0] = 0;
+  if (i < a.B * (a.k + 1)) a.count[(size_t)i * kVerifyLine] = 0;
+  if (i < a.B) {
+    const ChunkRows r = request_rows(a, i);
+    a.n[i * kVerifyLine] = r.n - 1;   // (-1: no rows)
+    a.req[i] = int2{r.row0, r.n - 1};
+    a.done[i * kVerifyLine] = 0;
+    a.keys[i * kVerifyLine / 2] = 0;
+  }
+}
+
+// What a piece leaves is stored past the caches (agent scope) and waited for before its row's counter is raised, so
+// that the last workgroup of a row, on any die, reads all of them.
+__device__ __forceinline__ void publish(unsigned long long* p, unsigned long long v) {
+  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  wait_vmcnt<0>();
+}
+__device__ __forceinline__ unsigned long long fetch(const unsigned long long* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+// A piece as 64 bits: (maximum, sum) with the sum's sign as the flag of a value that was not finite, or the argmax key
+// with the top bit of ~token (always 1: tokens are below 2^31) turned off by the flag.
+constexpr unsigned long long KEY_BIT = 0x80000000ull;
+__device__ __forceinline__ unsigned long long pack_lse(float m, float s, bool flag) {
+  return ((unsigned long long)__float_as_uint(m) << 32) | __float_as_uint(flag ? -s : s);
+}
+__device__ __forceinline__ Lse unpack_lse(unsigned long long v, bool& flag) {
+  const unsigned s = (unsigned)v;
+  flag |= (s >> 31) != 0;
+  return Lse{__uint_as_float((unsigned)(v >> 32)), __uint_as_float(s & 0x7fffffffu)};
+}
+__device__ __forceinline__ unsigned long long pack_key(unsigned long long key, bool flag) {
+  if (!key) key = ((unsigned long long)score_ord(-INFINITY) << 32) | 0xffffffffu;   // (of no values)
+  return flag ? key & ~KEY_BIT : key;
+}
+__device__ __forceinline__ unsigned long long unpack_key(unsigned long long v, bool& flag) {
+  flag |= !(v & KEY_BIT);
+  return v | KEY_BIT;
+}
+
+// Over the wave's lanes, of the pieces [0, n), n <= 64: log2 of the sum of 2^x, and the flag.
+__device__ __forceinline__ float join_pieces(const unsigned long long* p, int n, bool& flag) {
+  const int lane = threadIdx.x & 63;
+  Lse t;
+  if (lane < n) t = unpack_lse(fetch(p + lane), flag);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    const float m2 = __shfl_xor(t.m, o), s2 = __shfl_xor(t.s, o);
+    t.join(m2, s2);
+  }
+  flag = __any(flag) || t.m == -INFINITY;
+  return t.m == -INFINITY ? -INFINITY : t.m + __builtin_amdgcn_logf(t.s);
+}
+
+// Whether draft j of request b stands, and what the choice needs of its row (one wave).
+template <class T, bool GREEDY>
+__device__ __forceinline__ void decide(const VerifyArgs& a, int b, int j, const ChunkRows& cr) {
+  const int lane = threadIdx.x & 63, drafts = cr.n - 1;
+  const size_t row = (size_t)(cr.row0 + j);
+  const int d = j < drafts ? a.draft_tokens[(size_t)b * a.k + j] : -1;
+  const int t = target_id(a, d);
+  bool flag = false, stands = false;
+  VerifyRow r{0.f, 0.f, 0, 0};
+  if constexpr (GREEDY) {
+    unsigned long long top = 0;
+    if (lane < a.pieces_t) top = unpack_key(fetch(a.stat_t + row * a.pieces_t + lane), flag);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      const unsigned long long k = ((unsigned long long)__shfl_xor((unsigned)(top >> 32), o) << 32) | __shfl_xor((unsigned)top, o);
+      top = k > top ? k : top;
+    }
+    flag = __any(flag) || (unsigned)(top >> 32) == score_ord(-INFINITY);
+    r.top = key_token(top);
+    stands = r.top == t;
+  } else {
+    bool ignore = false;
+    // the drafted token's logits beside the pieces
+    const float x = t >= 0 ? to_f32(static_cast<const T*>(a.target)[row * a.V + t]) : 0.f;
+    const bool has_q = a.draft && j < drafts;
+    const size_t dr = (size_t)b * a.k + j;
+    const float y = has_q && t >= 0 ? a.draft[dr * a.Vd + d] : 0.f;
+    const float u = j < drafts ? a.u[dr] : 0.f;
+    r.lse_p = join_pieces(a.stat_t + row * a.pieces_t, a.pieces_t, flag);
+    float q = 1.f;
+    if (has_q) {
+      r.lse_q = join_pieces(a.stat_d + dr * a.pieces_d, a.pieces_d, flag);
+      q = __builtin_amdgcn_exp2f(log_prob(scaled(y, a.c_d, ignore), r.lse_q));
+    }
+    stands = t >= 0 && u * q < __builtin_amdgcn_exp2f(log_prob(scaled(x, a.c_t, ignore), r.lse_p));
+  }
+  r.flags = (flag ? ST_NONFINITE : 0) | (j < drafts && t < 0 ? ST_BAD_TOKEN : 0);
+  if (lane == 0) {
+    a.row[(size_t)b * (a.k + 1) + j] = r;
+    if (j < drafts && !stands) atomicMin(a.n + b * kVerifyLine, j);
+  }
+}
+
+// Pieces of rows j of every request, for j in turn.
+template <class T, bool GREEDY>
+__global__ void __launch_bounds__(VF_THREADS) verify_rows(VerifyArgs a) {
+  __shared__ unsigned long long s_stat[VF_THREADS / 64];   // as published
+  __shared__ int s_need;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const unsigned pieces = a.pieces_t + (a.draft ? a.pieces_d : 0), per_j = a.B * pieces;
+  const unsigned total = (a.k + 1) * per_j;   // (host: below 2^31)
+  for (unsigned w = blockIdx.x; w < total; w += gridDim.x) {
+    const int j = w / per_j, b = w % per_j / pieces, p = w % pieces;
+    const int2 rq = a.req[b];
+    // a request's decision so far (hearing of it later costs work, not the result): read once, so that all waves agree
+    if (tid == 0) s_need = j <= __hip_atomic_load(a.n + b * kVerifyLine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    const bool need = s_need && (p < a.pieces_t || j < rq.y);   // (the row after the last draft has no draft row)
+    if (need) {
+      PieceRegs x;
+      PieceStat st;
+      if (p < a.pieces_t) {
+        load_piece(static_cast<const T*>(a.target) + (size_t)(rq.x + j) * a.V, piece_range(a.V, a.pieces_t, p), x);
+        st = piece_stat<T, GREEDY>(x, a.c_t);
+      } else if constexpr (!GREEDY) {
+        load_piece(a.draft + ((size_t)b * a.k + j) * a.Vd, piece_range(a.Vd, a.pieces_d, p - a.pieces_t), x);
+        st = piece_stat<float, false>(x, a.c_d);
+      }
+      if (lane == 0) s_stat[wave] = GREEDY ? pack_key(st.key, st.bad) : pack_lse(st.l.m, st.l.s, st.bad);
+    }
+    __syncthreads();
+    if (need && wave == 0) {
+      unsigned long long v = 0;
+      bool bad = false;
+      Lse t;
+#pragma unroll
+      for (int i = 0; i < VF_THREADS / 64; ++i) {
+        if constexpr (GREEDY) {
+          const unsigned long long k = unpack_key(s_stat[i], bad);
+          v = k > v ? k : v;
+        } else {
+          const Lse l = unpack_lse(s_stat[i], bad);
+          t.join(l.m, l.s);
+        }
+      }
+      v = GREEDY ? pack_key(v, bad) : pack_lse(t.m, t.s, bad);
+      int last = 0;
+      if (lane == 0) {
+        publish(p < a.pieces_t ? a.stat_t + (size_t)(rq.x + j) * a.pieces_t + p
+                               : a.stat_d + ((size_t)b * a.k + j) * a.pieces_d + (p - a.pieces_t), v);
+        const int all = a.pieces_t + (a.draft && j < rq.y ? a.pieces_d : 0);
+        last = atomicAdd(a.count + ((size_t)b * (a.k + 1) + j) * kVerifyLine, 1) == all - 1;
+      }
+      if (__builtin_amdgcn_readfirstlane(last)) decide<T, GREEDY>(a, b, j, ChunkRows{rq.x, rq.y + 1, true});
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------ choice
+
+// N values from any 4-byte boundary.
+template <int N, class V>
+__device__ __forceinline__ void load_n(const V* p, V (&v)[N]) {
+  typedef V V4 __attribute__((ext_vector_type(4), aligned(4)));
+  if constexpr (N == 1) {
+    v[0] = p[0];
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      const V4 x = *reinterpret_cast<const V4*>(p + i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[i + e] = x[e];
+    }
+  }
+}
 
 // One workgroup per (request, piece of the vocabulary); greedy takes one piece and needs no row.
 template <class T, bool GREEDY>
 __global__ void __launch_bounds__(VF_THREADS) verify_pick(VerifyArgs a) {
-  __shared__ int s_n, s_flags, s_last;
-  __shared__ float s_lse_p, s_lse_q;
-  __shared__ unsigned long long s_key[VF_THREADS / 64][kVerifyKeys];
+  __shared__ int s_flags, s_last;
+  __shared__ unsigned long long s_key[VF_THREADS / 64];
   const int b = blockIdx.x / a.pieces_r, piece = blockIdx.x % a.pieces_r;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  ChunkRows cr;
-  if (a.cu) {
-    cr = chunk_rows(a.cu, b, a.rows, a.k + 1);
-  } else {
-    cr.row0 = b * (a.k + 1);
-    cr.n = a.k + 1;
-    cr.ok = true;
-  }
-  if (!cr.ok && tid == 0) set_status(a.status, ST_BAD_ROWS);
+  const ChunkRows cr = request_rows(a, b);
+  const int n = max(a.n[b * kVerifyLine], 0);
   int32_t* out = a.tokens + (size_t)b * (a.k + 1);
   if (cr.n == 0) {   // a request without rows
     if (piece == 0) {
       for (int i = tid; i <= a.k; i += VF_THREADS) out[i] = -1;
-      if (tid == 0) a.accepted[b] = 0;
+      if (tid == 0) {
+        a.accepted[b] = 0;
+        if (!cr.ok) set_status(a.status, ST_BAD_ROWS);
+      }
     }
     return;
   }
   const int drafts = cr.n - 1;
-  if (tid == 0) {
-    s_n = drafts;
-    s_flags = 0;
-  }
-  __syncthreads();
-  // the first draft that does not stand
-  for (int j0 = 0; j0 < drafts; j0 += VF_THREADS) {
-    const int j = j0 + tid;
-    bool stands = true;
-    if (j < drafts) {
-      const int d = a.draft_tokens[(size_t)b * a.k + j];
-      const int t = d < 0 || d >= a.Vd ? -1 : a.d2t ? a.d2t[d] : d;
-      stands = false;
-      if (t >= 0 && t < a.V) {
-        const float4* st = a.stat_t + (size_t)(cr.row0 + j) * a.pieces_t;
-        if constexpr (GREEDY) {
-          unsigned long long top = 0;
-          for (int i = 0; i < a.pieces_t; ++i) {
-            const unsigned long long k = ((unsigned long long)__float_as_uint(st[i].x) << 32) | __float_as_uint(st[i].y);
-            top = k > top ? k : top;
-          }
-          stands = key_token(top) == t;
-        } else {
-          bool flag = false, ignore = false;
-          const float lse = join_pieces(st, a.pieces_t, flag);
-          const float x = scaled(to_f32(static_cast<const T*>(a.target)[(size_t)(cr.row0 + j) * a.V + t]), a.inv_t, ignore);
-          const float p = exp_nat(log_prob(x, lse));
-          float q = 1.f;
-          if (a.draft) {
-            const size_t r = (size_t)b * a.k + j;
-            const float lq = join_pieces(a.stat_d + r * a.pieces_d, a.pieces_d, flag);
-            q = exp_nat(log_prob(scaled(a.draft[r * a.Vd + d], a.inv_td, ignore), lq));
-          }
-          stands = a.u[(size_t)b * a.k + j] * q < p;
-        }
-      }
-    }
-    if (!stands) atomicMin(&s_n, j);
+  const VerifyRow* rows = a.row + (size_t)b * (a.k + 1);
+  const VerifyRow rn = rows[n];
+  if (piece == 0) {   // flags of the rows that decided
+    if (tid == 0) s_flags = cr.ok ? 0 : ST_BAD_ROWS;
     __syncthreads();
-    if (s_n < drafts) break;
-  }
-  __syncthreads();
-  const int n = s_n;
-  // flags of the rows that decided: their values, and the drafts' tokens
-  for (int j = tid; j <= n; j += VF_THREADS) {
     int f = 0;
-    const float4* st = a.stat_t + (size_t)(cr.row0 + j) * a.pieces_t;
-    bool flag = false;
-    if constexpr (GREEDY) {
-      unsigned top = 0;
-      for (int i = 0; i < a.pieces_t; ++i) {
-        flag |= st[i].w != 0.f;
-        top = max(top, __float_as_uint(st[i].x));
-      }
-      flag |= top == score_ord(-INFINITY);
-    } else {
-      const float lse = join_pieces(st, a.pieces_t, flag);
-      if (j == n) s_lse_p = lse;
-      if (a.draft && j < drafts) {
-        const float lq = join_pieces(a.stat_d + ((size_t)b * a.k + j) * a.pieces_d, a.pieces_d, flag);
-        if (j == n) s_lse_q = lq;
-      }
-    }
-    if (flag) f |= ST_NONFINITE;
-    if (j < drafts) {
-      const int d = a.draft_tokens[(size_t)b * a.k + j];
-      const int t = d < 0 || d >= a.Vd ? -1 : a.d2t ? a.d2t[d] : d;
-      if (t < 0 || t >= a.V) f |= ST_BAD_TOKEN;
-    }
-    if (f && piece == 0) atomicOr(&s_flags, f);
+    for (int j = tid; j <= n; j += VF_THREADS) f |= rows[j].flags;
+    if (f) atomicOr(&s_flags, f);
+    __syncthreads();
+    if (tid == 0 && s_flags) set_status(a.status, s_flags);
   }
-  __syncthreads();
   int next = -1;
   if constexpr (GREEDY) {
-    unsigned long long top = 0;
-    const float4* st = a.stat_t + (size_t)(cr.row0 + n) * a.pieces_t;
-    for (int i = 0; i < a.pieces_t; ++i) {
-      const unsigned long long k = ((unsigned long long)__float_as_uint(st[i].x) << 32) | __float_as_uint(st[i].y);
-      top = k > top ? k : top;
-    }
-    next = key_token(top);
-    if (tid == 0 && s_flags) set_status(a.status, s_flags);
+    next = rn.top;
   } else {
     const T* row = static_cast<const T*>(a.target) + (size_t)(cr.row0 + n) * a.V;
     const float* noise = a.gumbel + (size_t)b * a.V;
     const bool rejected = n < drafts;
     const float* drow = rejected && a.draft ? a.draft + ((size_t)b * a.k + n) * a.Vd : nullptr;
-    int hot = -1;   // the draft that all of q is on
-    if (rejected && !a.draft) {
-      const int d = a.draft_tokens[(size_t)b * a.k + n];
-      hot = d < 0 || d >= a.Vd ? -1 : a.d2t ? a.d2t[d] : d;
-    }
-    const float lse_p = s_lse_p, lse_q = drow ? s_lse_q : 0.f;
-    unsigned long long best[kVerifyKeys] = {0, 0};
-    bool bad_noise = false, bad_map = false, ignore = false;
-    const int2 e = piece_range(a.V, a.pieces_r, piece);
-    each_piece(row, e.x, e.y, [&](int v0, const float* x, auto cnt) {
-      constexpr int N = decltype(cnt)::value;
+    // the draft that all of q is on
+    const int hot = rejected && !a.draft ? target_id(a, a.draft_tokens[(size_t)b * a.k + n]) : -1;
+    bool bad_noise = false, bad_map = false;
+    const bool careful = (rn.flags & ST_NONFINITE) != 0;
+    // The best (score, token) of elements [e0, e1) for a thread: of the residual, or of the target's own probabilities.
+    auto choose = [&](int e0, int e1, auto own_) -> unsigned long long {
+      constexpr bool OWN = decltype(own_)::value;
+      const bool sub = !OWN && drow;
+      float best = -INFINITY;
+      int at = -1;
+      each_piece(row, e0, e1, [&](int v0, const float* x, auto cnt) {
+        constexpr int N = decltype(cnt)::value;
+        float gn[N], y[N];
+        int d[N];
+        load_n<N>(noise + v0, gn);
+        if (sub) {
+          if (a.t2d) load_n<N>(a.t2d + v0, d);
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const int v = v0 + i;
-        const float lp = log_prob(scaled(x[i], a.inv_t, ignore), lse_p);
-        const float gn = noise[v];
-        float own = lp + gn, rest = own;
-        bool some = lp > -INFINITY && v != hot;
-        if (drow) {
-          int d = a.t2d ? a.t2d[v] : v < a.Vd ? v : -1;
-          if (d < -1 || d >= a.Vd) {
-            bad_map = true;
-            d = -1;
-          }
-          if (d >= 0) {
-            const float lq = log_prob(scaled(drow[d], a.inv_td, ignore), lse_q);
-            if (lq > -INFINITY) {
-              const float r = exp_nat(lp) - exp_nat(lq);
-              some = r > 0.f;
-              rest = __builtin_amdgcn_logf(r) * LN2 + gn;
+          for (int i = 0; i < N; ++i) {
+            if (!a.t2d) d[i] = v0 + i < a.Vd ? v0 + i : -1;
+            if ((unsigned)(d[i] + 1) > (unsigned)a.Vd) {
+              bad_map = true;
+              d[i] = -1;
             }
+            y[i] = d[i] >= 0 ? drow[d[i]] : -INFINITY;
           }
         }
-        if (!(own == own)) {
-          bad_noise = bad_noise || !(gn == gn);
-          own = -INFINITY;
-        }
-        if (!(rest == rest)) rest = -INFINITY;
-        const unsigned long long k0 = some ? ((unsigned long long)score_ord(rest) << 32) | ~(unsigned)v : 0ull;
-        const unsigned long long k1 = ((unsigned long long)score_ord(own) << 32) | ~(unsigned)v;
-        best[0] = k0 > best[0] ? k0 : best[0];
-        best[1] = k1 > best[1] ? k1 : best[1];
-      }
-    });
-    const int f = (__any(bad_noise) ? ST_NONFINITE : 0) | (__any(bad_map) ? ST_BAD_TOKEN : 0);
-    if (f && lane == 0) set_status(a.status, f);
 #pragma unroll
-    for (int i = 0; i < kVerifyKeys; ++i) {
+        for (int i = 0; i < N; ++i) {
+          bool ignore = false;
+          float lp = __builtin_fmaf(x[i], a.c_t, -rn.lse_p);
+          if (careful) lp = log_prob(scaled(x[i], a.c_t, ignore), rn.lse_p);
+          float lg = lp;
+          if (sub) {
+            float lq = __builtin_fmaf(y[i], a.c_d, -rn.lse_q);
+            if (careful) lq = log_prob(scaled(y[i], a.c_d, ignore), rn.lse_q);
+            const float q = __builtin_amdgcn_exp2f(lq);
+            // (of a difference below 0 the logarithm is NaN, which no comparison lets through)
+            if (q > 0.f) lg = __builtin_amdgcn_logf(__builtin_amdgcn_exp2f(lp) - q);
+          }
+          const float sc = __builtin_fmaf(lg, LN2, gn[i]);
+          bad_noise |= !(gn[i] == gn[i]);
+          const bool better = sc > best && (OWN || v0 + i != hot);
+          best = better ? sc : best;
+          at = better ? v0 + i : at;
+        }
+      });
+      return at < 0 ? 0ull : ((unsigned long long)score_ord(best + 0.f) << 32) | ~(unsigned)at;
+    };
+    auto wave_best = [&](unsigned long long k) {
 #pragma unroll
       for (int o = 32; o > 0; o >>= 1) {
-        const unsigned long long k = ((unsigned long long)__shfl_xor((unsigned)(best[i] >> 32), o) << 32) |
-                                     __shfl_xor((unsigned)best[i], o);
-        best[i] = k > best[i] ? k : best[i];
+        const unsigned long long v = ((unsigned long long)__shfl_xor((unsigned)(k >> 32), o) << 32) | __shfl_xor((unsigned)k, o);
+        k = v > k ? v : k;
       }
-      if (lane == 0) s_key[wave][i] = best[i];
-    }
-    __syncthreads();
-    if (tid < kVerifyKeys) {
-      unsigned long long k = s_key[0][tid];
-      for (int w = 1; w < VF_THREADS / 64; ++w) k = s_key[w][tid] > k ? s_key[w][tid] : k;
-      if (k) atomicMax(a.keys + b * kVerifyKeys + tid, k);
-      __threadfence();
-    }
-    __syncthreads();
+      return k;
+    };
+    auto all_best = [&](unsigned long long k) {   // of the workgroup, in every thread
+      k = wave_best(k);
+      __syncthreads();
+      if (lane == 0) s_key[wave] = k;
+      __syncthreads();
+      k = s_key[0];
+#pragma unroll
+      for (int w = 1; w < VF_THREADS / 64; ++w) k = s_key[w] > k ? s_key[w] : k;
+      return k;
+    };
+    const int2 e = piece_range(a.V, a.pieces_r, piece);
+    const unsigned long long mine = all_best(choose(e.x, e.y, std::false_type{}));
+    const int f = (__any(bad_noise) ? ST_NONFINITE : 0) | (__any(bad_map) ? ST_BAD_TOKEN : 0);
+    if (f && lane == 0) set_status(a.status, f);
     if (tid == 0) {
-      if (s_flags) set_status(a.status, s_flags);
-      s_last = atomicAdd(a.count + b, 1) == a.pieces_r - 1;
+      if (mine) __hip_atomic_fetch_max(a.keys + b * kVerifyLine / 2, mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      wait_vmcnt<0>();   // done before the counter is raised
+      s_last = atomicAdd(a.done + b * kVerifyLine, 1) == a.pieces_r - 1;
     }
     __syncthreads();
     if (!s_last) return;
-    const unsigned long long k0 = __hip_atomic_load(a.keys + b * kVerifyKeys, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const unsigned long long k1 = __hip_atomic_load(a.keys + b * kVerifyKeys + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    next = key_token(k0 ? k0 : k1);
+    unsigned long long top = fetch(a.keys + b * kVerifyLine / 2);
+    if (!top) top = all_best(choose(0, a.V, std::true_type{}));   // (rare: no positive difference anywhere)
+    next = top ? key_token(top) : 0;                              // (nothing above -inf: the lowest token)
   }
-  for (int i = tid; i <= a.k; i += VF_THREADS) {
-    int t = i == n ? next : -1;
-    if (i < n) {
-      const int d = a.draft_tokens[(size_t)b * a.k + i];
-      t = a.d2t ? a.d2t[d] : d;
-    }
-    out[i] = t;
-  }
+  for (int i = tid; i <= a.k; i += VF_THREADS)
+    out[i] = i < n ? target_id(a, a.draft_tokens[(size_t)b * a.k + i]) : i == n ? next : -1;
   if (tid == 0) a.accepted[b] = n;
 }
 
 template <class T>
 hipError_t launch_typed(const VerifyArgs& a, hipStream_t s) {
   const bool greedy = a.u == nullptr;
-  const long long wgs = (long long)a.rows * a.pieces_t + (!greedy && a.draft ? (long long)a.B * a.k * a.pieces_d : 0);
-  auto stats = greedy ? verify_stats<T, true> : verify_stats<T, false>;
-  hipLaunchKernelGGL(stats, dim3((unsigned)wgs), dim3(VF_THREADS), 0, s, a);
+  hipLaunchKernelGGL(verify_init, dim3((a.B * (a.k + 1) + 255) / 256), dim3(256), 0, s, a);
+  if (hipError_t e = hipGetLastError()) return e;
+  const long long items = (long long)(a.k + 1) * a.B * (a.pieces_t + (a.draft ? a.pieces_d : 0));
+  auto rows = greedy ? verify_rows<T, true> : verify_rows<T, false>;
+  hipLaunchKernelGGL(rows, dim3((unsigned)std::min(items, (long long)VF_GRID)), dim3(VF_THREADS), 0, s, a);
   if (hipError_t e = hipGetLastError()) return e;
   auto pick = greedy ? verify_pick<T, true> : verify_pick<T, false>;
   hipLaunchKernelGGL(pick, dim3((unsigned)(a.B * (long long)a.pieces_r)), dim3(VF_THREADS), 0, s, a);
@@ -401,18 +510,17 @@ hipError_t launch_typed(const VerifyArgs& a, hipStream_t s) {
 }  // namespace
 
 void verify_bounds(VerifyArgs& a) {
-  // workgroups aimed for, and elements a piece has at least
-  auto pieces = [](long long rows, int V) {
-    const long long want = std::max(1LL, 4096 / std::max(rows, 1LL)), most = std::max(1, V / 4096);
-    return (int)std::min(want, std::min(most, 64LL));
-  };
-  a.pieces_t = pieces(a.rows, a.V);
-  a.pieces_d = pieces((long long)a.B * a.k, a.Vd);
-  a.pieces_r = a.u ? pieces(a.B, a.V) : 1;
+  auto pieces = [](long long bytes) { return (int)((bytes + VF_PIECE - 1) / VF_PIECE); };   // at most 64 (host check)
+  a.pieces_t = pieces((long long)a.V * (a.f32 ? 4 : 2));
+  a.pieces_d = pieces((long long)a.Vd * 4);
+  // the choice reads one row a request: enough workgroups for the chip, of at least 4096 logits
+  a.pieces_r = (int)std::max(1LL, std::min({1024LL / a.B, a.V / 4096LL, 64LL}));
 }
 
 hipError_t launch_verify(const VerifyArgs& a, hipStream_t s) {
-  return a.f32 ? launch_typed<float>(a, s) : launch_typed<bf16>(a, s);
+  VerifyArgs x = a;
+  if (!a.u) x.pieces_r = 1;
+  return a.f32 ? launch_typed<float>(x, s) : launch_typed<bf16>(x, s);
 }
 
 }  // namespace hspec

@@ -423,23 +423,26 @@ def kv_inject(cfg, IW: dict, h_new, caches: list, page_table, ctx_lens, ws):
 
 # ----------------------------------------------------------------- the target's side of a step
 
-def _args(want: dict, **tensors):
-    """Pointers of device tensors on the current device, of the type and shape each has to have
-    (want: name -> (dtype, shape); None passes through where the C call allows it)."""
+def _dev() -> int:
+    return _torch().cuda.current_device()
+
+
+def _arg(name, t, dtype, shape, dev):
+    """Address of a contiguous tensor of this type and shape on device `dev` (None -> NULL)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor {tuple(shape)} on the current device, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _run(fn, dev, ws, *args):
+    """One call on the current stream of `dev`, with workspace `ws` (uint8, on the same device)."""
     torch = _torch()
-    dev = torch.cuda.current_device()
-    out = []
-    for name, t in tensors.items():
-        if t is None:
-            out.append(None)
-            continue
-        dt, shape = want[name]
-        if not (t.is_cuda and t.device.index == dev and t.is_contiguous()):
-            raise ValueError(f"{name}: expected a contiguous tensor on the current device")
-        if t.dtype != dt or tuple(t.shape) != tuple(shape):
-            raise ValueError(f"{name}: expected {dt} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
-        out.append(C.c_void_p(t.data_ptr()))
-    return out
+    if ws.dtype is not torch.uint8 or ws.get_device() != dev or not ws.is_contiguous():
+        raise ValueError("ws: expected a contiguous uint8 tensor on the current device")
+    _check(fn(*args, ws.data_ptr(), ws.numel(), torch.cuda.current_stream(dev).cuda_stream))
 
 
 def _storage(dtype: int):
@@ -453,15 +456,6 @@ def chunk_cfg(B, T, max_new, Hq, Hkv, D, page_size, max_pages, num_pages, dtype=
     return ChunkCfg(B, T, max_new, Hq, Hkv, D, page_size, max_pages, num_pages, window, dtype, eps, scale, rope_theta)
 
 
-def _chunk_want(cc: ChunkCfg) -> dict:
-    torch = _torch()
-    st, i32 = _storage(cc.dtype), torch.int32
-    pool = (cc.num_pages, cc.page_size, cc.Hkv, cc.D)
-    return dict(q=(st, (cc.T, cc.Hq, cc.D)), o=(st, (cc.T, cc.Hq, cc.D)), k_cache=(st, pool), v_cache=(st, pool),
-                cu_new=(i32, (cc.B + 1,)), ctx_lens=(i32, (cc.B,)), page_table=(i32, (cc.B, cc.max_pages)),
-                q_norm_w=(torch.float32, (cc.D,)), k_norm_w=(torch.float32, (cc.D,)))
-
-
 def chunk_append_workspace(cc: ChunkCfg) -> int:
     return lib().hspec_chunk_append_workspace(C.byref(cc))
 
@@ -469,12 +463,16 @@ def chunk_append_workspace(cc: ChunkCfg) -> int:
 def chunk_append(cc: ChunkCfg, qkv, cu_new, ctx_lens, q, k_cache, v_cache, page_table, ws, q_norm_w=None, k_norm_w=None):
     """Norm and RoPE of the new tokens' q and k; q out, K and V into the pages (hspec_chunk_append)."""
     torch = _torch()
-    want = _chunk_want(cc)
-    code = F32 if qkv.dtype == torch.float32 else BF16
-    want["qkv"] = (_storage(code), (cc.T, (cc.Hq + 2 * cc.Hkv) * cc.D))
-    a = _args(want, qkv=qkv, q_norm_w=q_norm_w, k_norm_w=k_norm_w, cu_new=cu_new, ctx_lens=ctx_lens, q=q,
-              k_cache=k_cache, v_cache=v_cache, page_table=page_table)
-    _check(lib().hspec_chunk_append(C.byref(cc), code, *a, ptr(ws), ws.numel(), stream_ptr()))
+    dev, i32, f32, st = _dev(), torch.int32, torch.float32, _storage(cc.dtype)
+    B, T, Hq, Hkv, D = cc.B, cc.T, cc.Hq, cc.Hkv, cc.D
+    pool = (cc.num_pages, cc.page_size, Hkv, D)
+    code = F32 if qkv.dtype is f32 else BF16
+    _run(lib().hspec_chunk_append, dev, ws, C.byref(cc), code,
+         _arg("qkv", qkv, _storage(code), (T, (Hq + 2 * Hkv) * D), dev), _arg("q_norm_w", q_norm_w, f32, (D,), dev),
+         _arg("k_norm_w", k_norm_w, f32, (D,), dev), _arg("cu_new", cu_new, i32, (B + 1,), dev),
+         _arg("ctx_lens", ctx_lens, i32, (B,), dev), _arg("q", q, st, (T, Hq, D), dev),
+         _arg("k_cache", k_cache, st, pool, dev), _arg("v_cache", v_cache, st, pool, dev),
+         _arg("page_table", page_table, i32, (B, cc.max_pages), dev))
 
 
 def chunk_attn_workspace(cc: ChunkCfg, max_len: int) -> int:
@@ -483,9 +481,13 @@ def chunk_attn_workspace(cc: ChunkCfg, max_len: int) -> int:
 
 def chunk_attn(cc: ChunkCfg, q, cu_new, k_cache, v_cache, page_table, ctx_lens, max_len: int, o, ws):
     """o [T, Hq, D] = causal attention of the new tokens over the paged cache (hspec_chunk_attn)."""
-    a = _args(_chunk_want(cc), q=q, cu_new=cu_new, k_cache=k_cache, v_cache=v_cache, page_table=page_table,
-              ctx_lens=ctx_lens, o=o)
-    _check(lib().hspec_chunk_attn(C.byref(cc), *a[:6], int(max_len), a[6], ptr(ws), ws.numel(), stream_ptr()))
+    torch = _torch()
+    dev, i32, st = _dev(), torch.int32, _storage(cc.dtype)
+    B, rows, pool = cc.B, (cc.T, cc.Hq, cc.D), (cc.num_pages, cc.page_size, cc.Hkv, cc.D)
+    _run(lib().hspec_chunk_attn, dev, ws, C.byref(cc), _arg("q", q, st, rows, dev),
+         _arg("cu_new", cu_new, i32, (B + 1,), dev), _arg("k_cache", k_cache, st, pool, dev),
+         _arg("v_cache", v_cache, st, pool, dev), _arg("page_table", page_table, i32, (B, cc.max_pages), dev),
+         _arg("ctx_lens", ctx_lens, i32, (B,), dev), int(max_len), _arg("o", o, st, rows, dev))
 
 
 def verify_cfg(B, k, rows, vocab, draft_vocab, dtype=BF16, temperature=1.0, draft_temperature=1.0) -> VerifyCfg:
@@ -500,11 +502,11 @@ def verify(vc: VerifyCfg, target_logits, draft_tokens, tokens, n_accepted, ws, d
            t2d=None, u=None, gumbel=None):
     """tokens [B, k+1], n_accepted [B] = which drafts stand against the target (hspec_verify)."""
     torch = _torch()
-    f32, i32 = torch.float32, torch.int32
-    want = dict(target_logits=(_storage(vc.dtype), (vc.rows, vc.vocab)), draft_logits=(f32, (vc.B, vc.k, vc.draft_vocab)),
-                draft_tokens=(i32, (vc.B, vc.k)), cu_rows=(i32, (vc.B + 1,)), d2t=(i32, (vc.draft_vocab,)),
-                t2d=(i32, (vc.vocab,)), u=(f32, (vc.B, vc.k)), gumbel=(f32, (vc.B, vc.vocab)),
-                tokens=(i32, (vc.B, vc.k + 1)), n_accepted=(i32, (vc.B,)))
-    a = _args(want, target_logits=target_logits, draft_logits=draft_logits, draft_tokens=draft_tokens, cu_rows=cu_rows,
-              d2t=d2t, t2d=t2d, u=u, gumbel=gumbel, tokens=tokens, n_accepted=n_accepted)
-    _check(lib().hspec_verify(C.byref(vc), *a, ptr(ws), ws.numel(), stream_ptr()))
+    dev, i32, f32 = _dev(), torch.int32, torch.float32
+    B, k, V, Vd = vc.B, vc.k, vc.vocab, vc.draft_vocab
+    _run(lib().hspec_verify, dev, ws, C.byref(vc),
+         _arg("target_logits", target_logits, _storage(vc.dtype), (vc.rows, V), dev),
+         _arg("draft_logits", draft_logits, f32, (B, k, Vd), dev), _arg("draft_tokens", draft_tokens, i32, (B, k), dev),
+         _arg("cu_rows", cu_rows, i32, (B + 1,), dev), _arg("d2t", d2t, i32, (Vd,), dev), _arg("t2d", t2d, i32, (V,), dev),
+         _arg("u", u, f32, (B, k), dev), _arg("gumbel", gumbel, f32, (B, V), dev),
+         _arg("tokens", tokens, i32, (B, k + 1), dev), _arg("n_accepted", n_accepted, i32, (B,), dev))

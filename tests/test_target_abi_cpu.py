@@ -117,8 +117,13 @@ def test_workspace_of_a_bad_verification_is_zero():
 
 def test_binding_checks_tensors():
     torch = pytest.importorskip("torch")
-    if torch.cuda.is_available():
-        pytest.skip("host tensors are refused for their device on any host; run without a GPU")
-    want = dict(x=(torch.float32, (2, 3)))
-    with pytest.raises((ValueError, RuntimeError, AssertionError)):
-        hspec._args(want, x=torch.zeros(2, 3))
+    x = torch.zeros(2, 3)                                    # (a host tensor: device -1)
+    assert hspec._arg("x", x, torch.float32, (2, 3), -1) == x.data_ptr()
+    assert hspec._arg("x", None, torch.float32, (2, 3), -1) is None
+    for bad in (x.int(), x[:1], x.t(), torch.zeros(2, 6)[:, ::2]):
+        with pytest.raises(ValueError, match="x: expected"):
+            hspec._arg("x", bad, torch.float32, (2, 3), -1)
+    with pytest.raises(ValueError, match="on the current device"):
+        hspec._arg("x", x, torch.float32, (2, 3), 0)
+    with pytest.raises(ValueError, match="ws"):
+        hspec._run(None, 0, torch.zeros(8, dtype=torch.uint8))
