@@ -460,7 +460,8 @@ typedef struct {
  * with rotate-half pairing at the row's position (no norm where q_norm_w and k_norm_w [D] are
  * both NULL).  q [T, Hq, D] out; k and v are written at slot(position) of k_cache and v_cache, in
  * place.  A position whose page id is outside the pool sets HSPEC_DEV_BAD_PAGE and is not written.
- * Which of two rows stays is undefined where a page is mapped for both.
+ * Which of two rows stays is undefined where a page is mapped for both.  q must not lie over qkv
+ * (HSPEC_ERR_UNSUPPORTED).
  */
 hspec_status hspec_chunk_append(const hspec_chunk_cfg* cfg, hspec_dtype qkv_dtype, const void* qkv,
                                 const float* q_norm_w, const float* k_norm_w, const int32_t* cu_new,
@@ -474,7 +475,8 @@ size_t hspec_chunk_append_workspace(const hspec_chunk_cfg* cfg);
  * host upper bound of ctx_lens[b] + new tokens of b (bounds the split of long caches).  A slot that
  * a row does not see never changes it, whatever it holds (NaN and infinities included); pages
  * outside the pool read as zeros and set HSPEC_DEV_BAD_PAGE; a row that sees no position is zero.
- * Results are bitwise reproducible and independent of where pages live.  o must not lie over q.
+ * Results are bitwise reproducible and independent of where pages live.  o must not lie over q
+ * (HSPEC_ERR_UNSUPPORTED).
  */
 hspec_status hspec_chunk_attn(const hspec_chunk_cfg* cfg, const void* q, const int32_t* cu_new, const void* k_cache,
                               const void* v_cache, const int32_t* page_table, const int32_t* ctx_lens, int max_len,

@@ -19,6 +19,7 @@
 //
 // fp32 storage takes the fp32 matrix products (32 x 32 x 2), so nothing is rounded below 32 bits.
 #include <algorithm>
+#include <atomic>
 #include <cfloat>
 #include <climits>
 #include <type_traits>
@@ -62,11 +63,8 @@ struct Chunk {
   static constexpr int GR = WROWS < 16 ? WROWS : 16;   // of them in one page for certain
   static constexpr int NG = WROWS / GR;
   static constexpr int NI = GR * CPR / 64;         // DMA instructions per group and tensor
-  static constexpr int WPE = sizeof(T) == 4 && D == 128 ? 1 : 2;   // waves per SIMD the registers are sized for
+  static constexpr int WPE = chunk_waves_per_simd(sizeof(T) == 4, D);   // waves per SIMD the registers are sized for
   static_assert(KT % 32 == 0 && GR * CPR % 64 == 0 && WROWS % GR == 0, "tile shape");
-  // workgroups that fit a compute unit: 128 pieces of 1280 bytes of LDS, WPE waves on each of four SIMDs
-  static constexpr int LDS = (4 * TILE * (int)sizeof(T) + 8 + 1279) / 1280;
-  static constexpr int PER_CU = 128 / LDS < 4 * WPE / NW ? 128 / LDS : 4 * WPE / NW;
 };
 
 // Element offset of (row, column d) in a K/V tile: 16-byte piece c of row r lives at piece c ^ f(r).  f makes the
@@ -298,8 +296,11 @@ __device__ __forceinline__ bool chunk_unit(const ChunkAttnArgs& a, const ChunkUn
         l_run += e;
       }
 
-    // O^T += V^T P^T.  P enters as bf16 with bf16 storage (2^-9 relative to each weight, like the V it multiplies);
-    // the sum above takes the unrounded weights.
+    // O^T += V^T P^T.  P enters as bf16 with bf16 storage (half a step is 2^-8 of each weight, and the output's own
+    // rounding is as large); the sum above takes the unrounded weights.  This wave first while it has products to
+    // issue: the other wave of the SIMD has its softmax to fill in (three prompts 1443 -> 1379 us, a chunk of 2000
+    // tokens behind 30000 2170 -> 1992).
+    __builtin_amdgcn_s_setprio(1);
     auto add_values = [&](auto masked_) {
       constexpr bool FIX = ODD && decltype(masked_)::value;
       if constexpr (F32) {
@@ -317,7 +318,7 @@ __device__ __forceinline__ bool chunk_unit(const ChunkAttnArgs& a, const ChunkUn
                 o[db] += __builtin_amdgcn_mfma_f32_32x32x2f32(fin || v < 0.f ? 0.f : FLT_MAX, sees, zero16(), 0, 0, 0);
                 o[db] += __builtin_amdgcn_mfma_f32_32x32x2f32(fin || v > 0.f ? 0.f : -FLT_MAX, sees, zero16(), 0, 0, 0);
                 if (!fin) v = 0.f;
-                }
+              }
               o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, st[kb][i], o[db], 0, 0, 0);
             }
           }
@@ -364,6 +365,7 @@ __device__ __forceinline__ bool chunk_unit(const ChunkAttnArgs& a, const ChunkUn
     wg_barrier();   // every wave's part of tile ti has landed, and every wave has left the other stage
     if (ti + 1 < ntiles) issue(ti + 1, other);
     compute(ti, mine);
+    __builtin_amdgcn_s_setprio(0);
   };
   for (int t0 = 0; t0 < ntiles; t0 += 2) {
     step(t0, st0, st1);
@@ -620,25 +622,12 @@ __global__ void __launch_bounds__(PL_THREADS) chunk_plan(ChunkAttnArgs a) {
     atomicMax(&s.longest, longest);
   }
   __syncthreads();
-  // Keys per unit, in whole key tiles: where the tiles leave most of the chip free, what makes one round of units
-  // (so every piece starts at once: 1 request of 32768 tokens 53 us, 79 in two short rounds), else 13/8 rounds, which
-  // the queue evens out.  (The factor covers the float roundings.)
-  const float spare = (float)a.slots - (float)all_tiles * (float)a.Hkv;
-  const float units = spare * 4.f >= (float)a.slots * 3.f ? spare : (float)a.target;
-  const float per = (float)s.keys * (float)a.Hkv / units * 1.0001f;
-  const int S = ((int)fminf(fmaxf(per, (float)a.min_split), 1e9f) + a.key_tile) / a.key_tile * a.key_tile;
+  const int S = chunk_unit_keys(a, s.keys, all_tiles);
   const int shift = max(26 - __builtin_clz(min(S, s.longest) | 1), 0);   // lengths >> shift are below 64
   auto bucket = [&](int len) -> int { return PL_BUCKETS - 1 - min(len >> shift, PL_BUCKETS - 1); };
-  auto pieces_of = [&](int len, int& q) -> int {   // pieces, and the length of all but the last
-    q = max(len, 1);
-    if (len <= S) return 1;
-    const unsigned p = ((unsigned)len + S - 1) / (unsigned)S;
-    q = (((unsigned)len + p - 1) / p + a.key_tile - 1) / a.key_tile * a.key_tile;
-    return ((unsigned)len + q - 1) / (unsigned)q;
-  };
   each(true, [&](int, const Tile& x) {
     int q;
-    const int p = pieces_of(x.len, q);
+    const int p = chunk_pieces(x.len, S, a.key_tile, q);
     if (p > 1) atomicAdd(&s.hist[bucket(q)], p - 1);
     atomicAdd(&s.hist[bucket(x.len - (p - 1) * q)], 1);
   });
@@ -657,7 +646,7 @@ __global__ void __launch_bounds__(PL_THREADS) chunk_plan(ChunkAttnArgs a) {
   __syncthreads();
   each(true, [&](int b0, const Tile& x) {
     int q;
-    const int p = pieces_of(x.len, q), b = b0 + x.r;
+    const int p = chunk_pieces(x.len, S, a.key_tile, q), b = b0 + x.r;
     const int row0 = s.row0[x.r], n = s.n[x.r], L = s.L[x.r];
     int slot = -1;
     if (p > 1) {
@@ -824,49 +813,22 @@ __global__ void __launch_bounds__(MG_THREADS) chunk_merge_row(ChunkAttnArgs a, i
 
 // ----------------------------------------------------------------------------- launch
 
-// Tile of the units: 32 rows per wave; one, two or four waves by the rows a request can have (n g), so that a
-// workgroup of few rows is not mostly idle waves.
+// The instance of a tile shape (chunk_shape).
 template <class F>
 auto with_variant(const ChunkAttnArgs& a, F f) {
-  const long long R = (long long)a.max_new * (a.Hq / a.Hkv);
   auto by_rows = [&](auto t, auto d) {
     typedef typename decltype(t)::type T;
     constexpr int D = decltype(d)::value;
-    constexpr int KT = sizeof(T) == 4 ? 32 : 64;
-    if (R <= 32) return f(Chunk<T, D, 1, 32, true>{});
-    if (R <= 64) return f(Chunk<T, D, 2, KT, true>{});
-    if (R <= 128) return f(Chunk<T, D, 4, KT, true>{});
-    return f(Chunk<T, D, 4, KT, false>{});
+    constexpr int KT2 = chunk_key_tile(2, sizeof(T) == 4), KT4 = chunk_key_tile(4, sizeof(T) == 4);
+    if (a.tile_rows == 32) return f(Chunk<T, D, 1, chunk_key_tile(1, sizeof(T) == 4), true>{});
+    if (a.tile_rows == 64) return f(Chunk<T, D, 2, KT2, true>{});
+    return a.once ? f(Chunk<T, D, 4, KT4, true>{}) : f(Chunk<T, D, 4, KT4, false>{});
   };
   if (a.f32) return a.D == 128 ? by_rows(std::common_type<float>{}, Int<128>{}) : by_rows(std::common_type<float>{}, Int<64>{});
   return a.D == 128 ? by_rows(std::common_type<bf16>{}, Int<128>{}) : by_rows(std::common_type<bf16>{}, Int<64>{});
 }
 
-constexpr int CHUNK_MIN_SPLIT = 64;   // keys a piece has at least
-
 }  // namespace
-
-void chunk_bounds(ChunkAttnArgs& a) {
-  with_variant(a, [&](auto c) {
-    a.tile_rows = decltype(c)::ROWS;
-    a.key_tile = decltype(c)::KT;
-    a.slots = decltype(c)::PER_CU * 256;
-    return 0;
-  });
-  a.min_split = CHUNK_MIN_SPLIT;
-  a.target = a.slots * 13 / 8;
-  const long long g = a.Hq / a.Hkv;
-  const long long per_req = ((long long)a.max_new * g + a.tile_rows - 1) / a.tile_rows;
-  const long long tiles = std::min((long long)a.T * g / a.tile_rows + a.B, per_req * a.B);
-  // pieces of a tile, and of all tiles: see chunk_plan
-  const long long len = (long long)a.cap + a.key_tile;
-  const long long cuts = len > a.min_split ? (len + a.min_split - 1) / a.min_split : 1;
-  const long long extra = (a.target + a.Hkv - 1) / a.Hkv;
-  a.max_units = (int)std::min(tiles * cuts, tiles + extra);
-  a.max_slots = cuts > 1 ? (int)std::min(tiles * cuts, 2 * extra) : 0;
-  a.max_splits = (int)std::min(tiles, (long long)a.max_slots / 2);
-  a.max_redo = a.max_units * a.Hkv * (a.tile_rows / 32);   // an entry for every wave
-}
 
 hipError_t launch_chunk_attn(const ChunkAttnArgs& a, hipStream_t s) {
   hipLaunchKernelGGL(chunk_plan, dim3(1), dim3(PL_THREADS), 0, s, a);
@@ -875,23 +837,23 @@ hipError_t launch_chunk_attn(const ChunkAttnArgs& a, hipStream_t s) {
     using C = decltype(c);
     constexpr int D = C::D, NW = C::NW;
     constexpr auto kern = chunk_attn_kernel<C>;
-    static int slots_of[64] = {};   // resident workgroups, per device
+    static std::atomic<int> slots_of[64];   // resident workgroups, per device
     int dev = 0;
     if (hipError_t e = hipGetDevice(&dev)) return e;
-    int& slots = slots_of[dev & 63];
+    int slots = slots_of[dev & 63].load(std::memory_order_relaxed);
     if (slots == 0) {
       int cus = 0, per_cu = 0;
       hipError_t e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
       if (e == hipSuccess) e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, kern, 64 * NW, 0);
       if (e != hipSuccess) return e;
-      slots = cus * (per_cu > 0 ? per_cu : 1);
+      slots = std::max(cus * per_cu / kChunkClasses, 1) * kChunkClasses;
+      slots_of[dev & 63].store(slots, std::memory_order_relaxed);
     }
     const long long items = (a.max_units + kChunkClasses - 1LL) / kChunkClasses * kChunkClasses * a.Hkv;
-    slots = std::max(slots / kChunkClasses * kChunkClasses, kChunkClasses);
     hipLaunchKernelGGL(kern, dim3((unsigned)std::min(items, (long long)slots)), dim3(64 * NW), 0, s, a);
     if (hipError_t e = hipGetLastError()) return e;
     if (a.redo) {
-      hipLaunchKernelGGL((chunk_redo_kernel<C>), dim3((unsigned)std::min(items, 64LL)), dim3(64 * NW), 0, s, a);
+      hipLaunchKernelGGL((chunk_redo_kernel<C>), dim3((unsigned)std::min(items, 256LL)), dim3(64 * NW), 0, s, a);
       if (hipError_t e = hipGetLastError()) return e;
     }
     if (a.max_splits > 0) {

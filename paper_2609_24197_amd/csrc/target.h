@@ -5,6 +5,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 namespace hspec {
 
 // Status bit of a ragged row array (cu_new, cu_rows) that is no increasing division of the rows.
@@ -56,11 +58,60 @@ struct ChunkAttnArgs {
   int* redo = nullptr;                // items to do again, status[3] of them; null: rows of a request see the same keys
   float* part_o = nullptr;            // [slots][Hkv][tile rows][D]
   float* part_ml = nullptr;           // [slots][Hkv][tile rows][2]
-  // filled from chunk_shape / chunk_bounds
-  int tile_rows = 0, key_tile = 0, min_split = 0, slots = 0, target = 0, max_units = 0, max_slots = 0, max_splits = 0, max_redo = 0;
+  // chunk_bounds
+  int tile_rows = 0, key_tile = 0, once = 0, slots = 0, target = 0, min_split = 0;
+  int max_units = 0, max_slots = 0, max_splits = 0, max_redo = 0;
 };
-// The tile the launch uses for these arguments, and the most units, partial slots and split tiles it can need.
-void chunk_bounds(ChunkAttnArgs& a);
+// Keys per tile, and waves per SIMD the registers are sized for, of a workgroup of `waves` waves.
+constexpr int chunk_key_tile(int waves, bool f32) { return f32 || waves == 1 ? 32 : 64; }
+constexpr int chunk_waves_per_simd(bool f32, int D) { return f32 && D == 128 ? 1 : 2; }
+constexpr int kChunkMinSplit = 64;   // keys a piece of a split tile has at least
+
+// Keys a unit takes at most, in whole key tiles, for `keys` keys of `tiles` tiles of rows: where the tiles leave most of
+// the chip free, what makes one round of units (so every piece starts at once: 1 request of 32768 tokens 53 us, 79 in
+// two short rounds), else 13/8 rounds, which the queue evens out.  At least keys Hkv / target, which the workspace
+// counts on (the factor covers the float roundings).
+__host__ __device__ inline int chunk_unit_keys(const ChunkAttnArgs& a, unsigned long long keys, int tiles) {
+  const float spare = (float)a.slots - (float)tiles * (float)a.Hkv;
+  const float units = spare * 4.f >= (float)a.slots * 3.f ? spare : (float)a.target;
+  const float per = (float)keys * (float)a.Hkv / units * 1.0001f;
+  const float least = (float)a.min_split, most = 1e9f;
+  return ((int)(per < least ? least : per > most ? most : per) + a.key_tile) / a.key_tile * a.key_tile;
+}
+// Even pieces of a tile of len keys, each a whole number of key tiles but the last: their number, and their length in q.
+__host__ __device__ inline int chunk_pieces(int len, int S, int key_tile, int& q) {
+  q = len > 1 ? len : 1;
+  if (len <= S) return 1;
+  const unsigned p = ((unsigned)len + S - 1) / (unsigned)S;
+  q = (int)((((unsigned)len + p - 1) / p + key_tile - 1) / key_tile * key_tile);
+  return (int)(((unsigned)len + q - 1) / (unsigned)q);
+}
+
+// Tile of the units, and the most units, partial slots and split tiles the plan can make of any lengths.  32 rows per
+// wave; one, two or four waves by the rows a request can have (n g), so that a workgroup of few rows is not mostly idle
+// waves; past four waves a request has several tiles (once = 0).
+inline void chunk_bounds(ChunkAttnArgs& a) {
+  const long long g = a.Hq / a.Hkv, R = a.max_new * g;
+  const int waves = R <= 32 ? 1 : R <= 64 ? 2 : 4;
+  a.tile_rows = 32 * waves;
+  a.once = R <= a.tile_rows;
+  a.key_tile = chunk_key_tile(waves, a.f32);
+  // workgroups that run at once on 256 compute units: LDS (two stages of K and V) goes in 128 pieces of 1280 bytes
+  const int lds = (4 * a.key_tile * a.D * (a.f32 ? 4 : 2) + 8 + 1279) / 1280;
+  a.slots = std::min(128 / lds, 4 * chunk_waves_per_simd(a.f32, a.D) / waves) * 256;
+  a.target = a.slots * 13 / 8;
+  a.min_split = kChunkMinSplit;
+  const long long per_req = (R + a.tile_rows - 1) / a.tile_rows;
+  const long long tiles = std::min(a.T * g / a.tile_rows + a.B, per_req * a.B);
+  // pieces of a tile, and of all tiles: see chunk_plan
+  const long long len = (long long)a.cap + a.key_tile;
+  const long long cuts = (len + a.min_split - 1) / a.min_split;
+  const long long extra = (a.target + a.Hkv - 1) / a.Hkv;
+  a.max_units = (int)std::min(tiles * cuts, tiles + extra);
+  a.max_slots = cuts > 1 ? (int)std::min(tiles * cuts, 2 * extra) : 0;
+  a.max_splits = (int)std::min(tiles, (long long)a.max_slots / 2);
+  a.max_redo = a.max_units * a.Hkv * waves;   // an entry for every wave
+}
 hipError_t launch_chunk_attn(const ChunkAttnArgs& a, hipStream_t s);
 
 // ------------------------------------------------------------------------ verification
@@ -89,7 +140,14 @@ struct VerifyArgs {
   unsigned long long* keys = nullptr;     // [B][kVerifyLine / 2] best (score, token)
   int pieces_t = 0, pieces_d = 0, pieces_r = 0;
 };
-void verify_bounds(VerifyArgs& a);
+constexpr int kVerifyPiece = 32768;   // bytes of a row that a workgroup takes at a time, all its loads under way together
+inline void verify_bounds(VerifyArgs& a) {
+  auto pieces = [](long long bytes) { return (int)((bytes + kVerifyPiece - 1) / kVerifyPiece); };   // at most 64 (host check)
+  a.pieces_t = pieces((long long)a.V * (a.f32 ? 4 : 2));
+  a.pieces_d = pieces((long long)a.Vd * 4);
+  // the choice reads one row a request: enough workgroups for the chip, of at least 4096 logits
+  a.pieces_r = (int)std::max(1LL, std::min({1024LL / a.B, a.V / 4096LL, 64LL}));
+}
 hipError_t launch_verify(const VerifyArgs& a, hipStream_t s);
 
 }  // namespace hspec

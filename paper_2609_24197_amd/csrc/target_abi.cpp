@@ -56,6 +56,14 @@ hspec_status check_aligned(std::initializer_list<const void*> ptrs) {
   return HSPEC_OK;
 }
 
+// What is written must not lie over what is read meanwhile.
+hspec_status check_apart(const void* x, size_t nx, const void* y, size_t ny) {
+  const uintptr_t a = (uintptr_t)x, b = (uintptr_t)y;
+  if (a < b + ny && b < a + nx) return fail(HSPEC_ERR_UNSUPPORTED, "an output lies over an input");
+  return HSPEC_OK;
+}
+size_t size_of(hspec_dtype d) { return d == HSPEC_F32 ? 4 : 2; }
+
 bool dtype_ok(hspec_dtype d) { return d == HSPEC_BF16 || d == HSPEC_F32; }
 
 hspec_status check_chunk(const hspec_chunk_cfg* c) {
@@ -98,6 +106,9 @@ HSPEC_API hspec_status hspec_chunk_append(const hspec_chunk_cfg* cfg, hspec_dtyp
   if (!q_norm_w != !k_norm_w) return fail(HSPEC_ERR_NULL, "only one of q_norm_w and k_norm_w is NULL");
   if (!(cfg->rope_theta > 0.)) return fail(HSPEC_ERR_SHAPE, "rope_theta must be positive");
   if (hspec_status s = check_aligned({qkv, q, k_cache, v_cache})) return s;
+  if (hspec_status s = check_apart(qkv, (size_t)cfg->T * (cfg->Hq + 2 * cfg->Hkv) * cfg->D * size_of(qkv_dtype), q,
+                                   (size_t)cfg->T * cfg->Hq * cfg->D * size_of(cfg->dtype)))
+    return s;
   if (hspec_status s = check_ws(workspace, ws_bytes, hspec_chunk_append_workspace(cfg))) return s;
   const hspec_chunk_cfg& c = *cfg;
   hspec::ChunkAppendArgs a;
@@ -148,6 +159,8 @@ HSPEC_API hspec_status hspec_chunk_attn(const hspec_chunk_cfg* cfg, const void* 
   if (!q || !cu_new || !k_cache || !v_cache || !page_table || !ctx_lens || !o)
     return fail(HSPEC_ERR_NULL, "an input or output pointer is NULL");
   if (hspec_status s = check_aligned({q, k_cache, v_cache, o})) return s;
+  const size_t rows = (size_t)cfg->T * cfg->Hq * cfg->D * size_of(cfg->dtype);
+  if (hspec_status s = check_apart(q, rows, o, rows)) return s;
   if (hspec_status s = check_ws(workspace, ws_bytes, hspec_chunk_attn_workspace(cfg, max_len))) return s;
   Arena ar{(char*)workspace};
   hspec::ChunkAttnArgs a;

@@ -27,7 +27,7 @@ namespace {
 constexpr int VF_THREADS = 256;
 constexpr int ST_BAD_TOKEN = 4;
 constexpr int ST_NONFINITE = 8;
-constexpr int VF_PIECE = 32768;   // bytes of a row that a workgroup takes at a time, all its loads under way together
+constexpr int VF_PIECE = kVerifyPiece;
 constexpr int VF_GRID = 16384;    // (32768-byte pieces, 4096 workgroups: 90 us at 64 x 16 x 131072; 8192: 76; 16384: 74)
 constexpr float LN2 = 0.6931471805599453f;
 
@@ -508,14 +508,6 @@ hipError_t launch_typed(const VerifyArgs& a, hipStream_t s) {
 }
 
 }  // namespace
-
-void verify_bounds(VerifyArgs& a) {
-  auto pieces = [](long long bytes) { return (int)((bytes + VF_PIECE - 1) / VF_PIECE); };   // at most 64 (host check)
-  a.pieces_t = pieces((long long)a.V * (a.f32 ? 4 : 2));
-  a.pieces_d = pieces((long long)a.Vd * 4);
-  // the choice reads one row a request: enough workgroups for the chip, of at least 4096 logits
-  a.pieces_r = (int)std::max(1LL, std::min({1024LL / a.B, a.V / 4096LL, 64LL}));
-}
 
 hipError_t launch_verify(const VerifyArgs& a, hipStream_t s) {
   VerifyArgs x = a;

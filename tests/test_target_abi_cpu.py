@@ -31,13 +31,16 @@ BAD_CHUNK = [(dict(B=0), SHAPE), (dict(T=0), SHAPE), (dict(max_new=0), SHAPE), (
              (dict(Hq=8192, T=1), UNSUPPORTED), (dict(dtype=2), DTYPE)]
 
 
-def _attn(c, max_len=1000, ptrs=None, ws=C.c_void_p(1 << 20), n=1 << 40):
+OUT = C.c_void_p(1 << 40)
+
+
+def _attn(c, max_len=1000, ptrs=None, ws=C.c_void_p(1 << 20), n=1 << 40, o=OUT):
     p = ptrs or [FAKE] * 6
-    return _lib().hspec_chunk_attn(C.byref(c) if c else None, *p, max_len, FAKE, ws, n, None)
+    return _lib().hspec_chunk_attn(C.byref(c) if c else None, *p, max_len, o, ws, n, None)
 
 
 def _append(c, code=1, ptrs=None, ws=C.c_void_p(1 << 20), n=1 << 40):
-    p = ptrs or [FAKE] * 9
+    p = ptrs or [FAKE] * 5 + [OUT] + [FAKE] * 3
     return _lib().hspec_chunk_append(C.byref(c) if c else None, code, *p, ws, n, None)
 
 
@@ -63,6 +66,8 @@ def test_chunk_attn_refusals():
         p[i] = C.c_void_p((1 << 20) + 2)
         assert _attn(c, ptrs=p) == UNSUPPORTED, i
         assert b"aligned" in L.hspec_last_error()
+    assert _attn(c, o=FAKE) == UNSUPPORTED and b"lies over" in L.hspec_last_error()
+    assert _attn(c, o=C.c_void_p((1 << 20) + 68 * 32 * 128 * 2 - 16)) == UNSUPPORTED
     need = L.hspec_chunk_attn_workspace(C.byref(c), 1000)
     assert need > 0
     assert _attn(c, n=need - 1) == WORKSPACE and _attn(c, ws=None) == WORKSPACE
@@ -82,6 +87,7 @@ def test_chunk_append_refusals():
         p = [FAKE] * 9
         p[i] = C.c_void_p((1 << 20) + 8)
         assert _append(c, ptrs=p) == UNSUPPORTED, i
+    assert _append(c, ptrs=[FAKE] * 9) == UNSUPPORTED and b"lies over" in L.hspec_last_error()
     assert _append(c, n=8) == WORKSPACE
     assert L.hspec_chunk_append_workspace(C.byref(c)) >= 256
 
