@@ -681,7 +681,7 @@ constexpr int MG_THREADS = 256;
 // o = sum_i O_i 2^(m_i - m*) / sum_i l_i 2^(m_i - m*) over a row's pieces, in an order of their own (not of time).
 // Bound by the round trips of a row's loads: a workgroup takes one row, with its pieces spread over groups of D / 4
 // threads, where that makes few workgroups (few rows, so perhaps many pieces each: 1 request of 32768 tokens, 128
-// pieces, 77 us for the whole call with a thread for all of a row's pieces, now 48), else 1024 / D rows.
+// pieces, 77 us for the whole call with a thread for all of a row's pieces, now 53), else 1024 / D rows.
 constexpr int MG_FEW = 4096;   // workgroups up to which each takes one row
 
 template <class T, int D>

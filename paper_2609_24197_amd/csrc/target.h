@@ -115,9 +115,13 @@ inline void chunk_bounds(ChunkAttnArgs& a) {
 hipError_t launch_chunk_attn(const ChunkAttnArgs& a, hipStream_t s);
 
 // ------------------------------------------------------------------------ verification
-// What a finished row leaves for the choice: log2 of its sums of 2^x, status bits, greedy's argmax.
+// A row's largest logit, and log2 of the sum of 2^((l - m) c).
+struct RowSum {
+  float m, log_s;
+};
+// What a finished row leaves for the choice: the sums of the target's and the draft's row, status bits, greedy's argmax.
 struct VerifyRow {
-  float lse_p, lse_q;
+  RowSum p, q;
   int flags, top;
 };
 constexpr int kVerifyLine = 32;   // ints between counters: a 128-byte line each, so that they are not one line's traffic
@@ -129,6 +133,7 @@ struct VerifyArgs {
   int32_t *tokens = nullptr, *accepted = nullptr;
   int B = 0, k = 0, rows = 0, V = 0, Vd = 0, f32 = 0;
   float c_t = 1.f, c_d = 1.f;             // log2(e) / temperature, of the target and of the drafts
+  double c64_t = 1., c64_d = 1.;
   int* status = nullptr;
   unsigned long long* stat_t = nullptr;   // [rows][pieces_t]
   unsigned long long* stat_d = nullptr;   // [B*k][pieces_d]
@@ -137,7 +142,7 @@ struct VerifyArgs {
   int* n = nullptr;                       // [B][kVerifyLine] first draft found not to stand
   int2* req = nullptr;                    // [B] first row, drafts
   int* done = nullptr;                    // [B][kVerifyLine] workgroups of the choice that are done
-  unsigned long long* keys = nullptr;     // [B][kVerifyLine / 2] best (score, token)
+  unsigned long long* keys = nullptr;     // [B][kVerifyLine / 2] best (score, token), and the best in doubt
   int pieces_t = 0, pieces_d = 0, pieces_r = 0;
 };
 constexpr int kVerifyPiece = 32768;   // bytes of a row that a workgroup takes at a time, all its loads under way together

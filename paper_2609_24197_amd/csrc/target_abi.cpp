@@ -234,7 +234,9 @@ HSPEC_API hspec_status hspec_verify(const hspec_verify_cfg* cfg, const void* tar
   a.target = target_logits; a.draft = draft_logits; a.draft_tokens = draft_tokens; a.cu = cu_rows; a.d2t = d2t;
   a.t2d = t2d; a.gumbel = gumbel; a.tokens = tokens; a.accepted = n_accepted;
   const double log2e = 1.4426950408889634074;
-  a.c_t = u ? (float)(log2e / cfg->temperature) : 1.f;
-  a.c_d = draft_logits ? (float)(log2e / cfg->draft_temperature) : 1.f;
+  a.c64_t = u ? log2e / cfg->temperature : 1.;
+  a.c64_d = draft_logits ? log2e / cfg->draft_temperature : 1.;
+  a.c_t = (float)a.c64_t;
+  a.c_d = (float)a.c64_d;
   return launched(hspec::launch_verify(a, (hipStream_t)stream));
 }

@@ -11,7 +11,7 @@
 // is comes out of the rows before it: the pieces of all rows are taken in the order of j by a grid that holds little
 // more than one j of every request at a time; the workgroup that finishes a row decides its draft, and pieces of rows
 // past a request's decision are left out.  Then row n is read once more for the choice.  64 requests x 16 drafts,
-// 131072 bf16 logits: 162 us when every row was read first, now 74.
+// 131072 bf16 logits: 162 us when every row was read first, now 66.
 #include <algorithm>
 #include <cfloat>
 #include <climits>
@@ -28,26 +28,24 @@ constexpr int VF_THREADS = 256;
 constexpr int ST_BAD_TOKEN = 4;
 constexpr int ST_NONFINITE = 8;
 constexpr int VF_PIECE = kVerifyPiece;
-constexpr int VF_GRID = 16384;    // (32768-byte pieces, 4096 workgroups: 90 us at 64 x 16 x 131072; 8192: 76; 16384: 74)
+constexpr int VF_GRID = 16384;    // (90 us at 64 x 16 x 131072 with 4096, 76 with 8192, then 74)
 constexpr float LN2 = 0.6931471805599453f;
 
-// Logits are taken in units of log 2: x = l c with c = log2(e) / T.
-
-// One as the definition wants it: NaN counts as -inf and +inf (or what overflows) as the largest float; both flag.
-__device__ __forceinline__ float scaled(float l, float c, bool& bad) {
-  const float x = l * c;
-  if (x <= FLT_MAX) return x;
+// A logit as the definition wants it: NaN counts as -inf and +inf as the largest float; both flag.
+__device__ __forceinline__ float clean(float l, bool& bad) {
+  if (l <= FLT_MAX) return l;
   bad = true;
-  return x == x ? FLT_MAX : -INFINITY;
+  return l == l ? FLT_MAX : -INFINITY;
 }
 
-// (maximum, sum of 2^(x - maximum)).
+// (maximum, sum of 2^((l - maximum) c)), c = log2(e) / T.  The difference is taken before the scale: of x = l c and a
+// logarithm of their sum as large, it would carry the rounding of both (2^-24 of 40 / T).
 struct Lse {
   float m = -INFINITY, s = 0.f;
-  __device__ __forceinline__ void join(float m2, float s2) {
+  __device__ __forceinline__ void join(float m2, float s2, float c) {
     const float mn = fmaxf(m, m2);
     const float ref = mn == -INFINITY ? 0.f : mn;
-    s = s * __builtin_amdgcn_exp2f(m - ref) + s2 * __builtin_amdgcn_exp2f(m2 - ref);
+    s = s * __builtin_amdgcn_exp2f((m - ref) * c) + s2 * __builtin_amdgcn_exp2f((m2 - ref) * c);
     m = mn;
   }
 };
@@ -133,36 +131,27 @@ __device__ __forceinline__ void each_value(const PieceRegs& x, F f) {
   if (x.e >= 0) f(x.end, x.e);
 }
 // Two passes over the registers: the maximum (which a NaN comes through), then the sum against it or its first place.
-// Per value a multiply-add, an exponential and half a comparison; values that are not finite take the pieces they
-// are in through it again by the rules of scaled().
+// A wave with values that are not finite goes through its piece again by the rules of clean().
 template <class T, bool GREEDY>
 __device__ __forceinline__ PieceStat piece_stat(const PieceRegs& x, float c) {
   PieceStat s;
   float mx = -INFINITY;
   each_value<T>(x, [&](float v, int) { mx = __builtin_elementwise_maximum(mx, v); });
-  bool odd = !(mx <= FLT_MAX) || mx * c > FLT_MAX;
-  if (__any(odd)) {
+  const bool odd = __any(!(mx <= FLT_MAX));
+  if (odd) {
     mx = -INFINITY;
-    each_value<T>(x, [&](float v, int) { mx = fmaxf(mx, scaled(v, c, s.bad)); });
-    const float ref = mx == -INFINITY ? 0.f : mx;
-    s.l.m = mx;
-    each_value<T>(x, [&](float v, int e) {
-      const float y = scaled(v, c, s.bad);
-      if constexpr (GREEDY) {
-        const unsigned long long k = ((unsigned long long)score_ord(y + 0.f) << 32) | ~(unsigned)e;
-        s.key = k > s.key ? k : s.key;
-      } else {
-        s.l.s += __builtin_amdgcn_exp2f(y - ref);
-      }
-    });
-  } else if constexpr (GREEDY) {
+    each_value<T>(x, [&](float v, int) { mx = fmaxf(mx, clean(v, s.bad)); });
+  }
+  const float ref = mx == -INFINITY ? 0.f : mx;
+  s.l.m = mx;
+  if constexpr (GREEDY) {
     int at = INT_MAX;   // (-0 and 0 are equal)
-    each_value<T>(x, [&](float v, int e) { at = v == mx ? min(at, e) : at; });
+    each_value<T>(x, [&](float v, int e) { at = (odd ? clean(v, s.bad) : v) == mx ? min(at, e) : at; });
     if (at != INT_MAX) s.key = ((unsigned long long)score_ord(mx + 0.f) << 32) | ~(unsigned)at;
+  } else if (odd) {
+    each_value<T>(x, [&](float v, int) { s.l.s += __builtin_amdgcn_exp2f((clean(v, s.bad) - ref) * c); });
   } else {
-    s.l.m = mx * c;
-    const float ref = s.l.m == -INFINITY ? 0.f : s.l.m;
-    each_value<T>(x, [&](float v, int) { s.l.s += __builtin_amdgcn_exp2f(__builtin_fmaf(v, c, -ref)); });
+    each_value<T>(x, [&](float v, int) { s.l.s += __builtin_amdgcn_exp2f((v - ref) * c); });
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
@@ -171,7 +160,7 @@ __device__ __forceinline__ PieceStat piece_stat(const PieceRegs& x, float c) {
       s.key = k > s.key ? k : s.key;
     } else {
       const float m2 = __shfl_xor(s.l.m, o), s2 = __shfl_xor(s.l.s, o);
-      s.l.join(m2, s2);
+      s.l.join(m2, s2, c);
     }
   }
   s.bad = __any(s.bad);
@@ -190,8 +179,10 @@ __device__ __forceinline__ int target_id(const VerifyArgs& a, int d) {
   const int t = d < 0 || d >= a.Vd ? -1 : a.d2t ? a.d2t[d] : d;
   return t < a.V ? max(t, -1) : -1;
 }
-// x - lse, for rows of nothing but -inf too
-__device__ __forceinline__ float log_prob(float x, float lse) { return x == -INFINITY ? -INFINITY : x - lse; }
+// log2 of a probability; of -inf, also in a row of nothing else, it is -inf.
+__device__ __forceinline__ float log_prob(float l, const RowSum& r, float c) {
+  return l == -INFINITY ? -INFINITY : __builtin_fmaf(l - r.m, c, -r.log_s);
+}
 
 __global__ void verify_init(VerifyArgs a) {
   const int i = blockIdx.x * blockDim.x + threadIdx.x;
@@ -202,7 +193,7 @@ __global__ void verify_init(VerifyArgs a) {
     a.n[i * kVerifyLine] = r.n - 1;   // (-1: no rows)
     a.req[i] = int2{r.row0, r.n - 1};
     a.done[i * kVerifyLine] = 0;
-    a.keys[i * kVerifyLine / 2] = 0;
+    a.keys[i * kVerifyLine / 2] = a.keys[i * kVerifyLine / 2 + 1] = 0;
   }
 }
 
@@ -235,18 +226,18 @@ __device__ __forceinline__ unsigned long long unpack_key(unsigned long long v, b
   return v | KEY_BIT;
 }
 
-// Over the wave's lanes, of the pieces [0, n), n <= 64: log2 of the sum of 2^x, and the flag.
-__device__ __forceinline__ float join_pieces(const unsigned long long* p, int n, bool& flag) {
+// Over the wave's lanes, of the pieces [0, n), n <= 64: a row's maximum and the log2 of its sum, and the flag.
+__device__ __forceinline__ RowSum join_pieces(const unsigned long long* p, int n, float c, bool& flag) {
   const int lane = threadIdx.x & 63;
   Lse t;
   if (lane < n) t = unpack_lse(fetch(p + lane), flag);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
     const float m2 = __shfl_xor(t.m, o), s2 = __shfl_xor(t.s, o);
-    t.join(m2, s2);
+    t.join(m2, s2, c);
   }
   flag = __any(flag) || t.m == -INFINITY;
-  return t.m == -INFINITY ? -INFINITY : t.m + __builtin_amdgcn_logf(t.s);
+  return RowSum{t.m, __builtin_amdgcn_logf(t.s)};
 }
 
 // Whether draft j of request b stands, and what the choice needs of its row (one wave).
@@ -257,7 +248,7 @@ __device__ __forceinline__ void decide(const VerifyArgs& a, int b, int j, const 
   const int d = j < drafts ? a.draft_tokens[(size_t)b * a.k + j] : -1;
   const int t = target_id(a, d);
   bool flag = false, stands = false;
-  VerifyRow r{0.f, 0.f, 0, 0};
+  VerifyRow r{};
   if constexpr (GREEDY) {
     unsigned long long top = 0;
     if (lane < a.pieces_t) top = unpack_key(fetch(a.stat_t + row * a.pieces_t + lane), flag);
@@ -277,13 +268,13 @@ __device__ __forceinline__ void decide(const VerifyArgs& a, int b, int j, const 
     const size_t dr = (size_t)b * a.k + j;
     const float y = has_q && t >= 0 ? a.draft[dr * a.Vd + d] : 0.f;
     const float u = j < drafts ? a.u[dr] : 0.f;
-    r.lse_p = join_pieces(a.stat_t + row * a.pieces_t, a.pieces_t, flag);
+    r.p = join_pieces(a.stat_t + row * a.pieces_t, a.pieces_t, a.c_t, flag);
     float q = 1.f;
     if (has_q) {
-      r.lse_q = join_pieces(a.stat_d + dr * a.pieces_d, a.pieces_d, flag);
-      q = __builtin_amdgcn_exp2f(log_prob(scaled(y, a.c_d, ignore), r.lse_q));
+      r.q = join_pieces(a.stat_d + dr * a.pieces_d, a.pieces_d, a.c_d, flag);
+      q = __builtin_amdgcn_exp2f(log_prob(clean(y, ignore), r.q, a.c_d));
     }
-    stands = t >= 0 && u * q < __builtin_amdgcn_exp2f(log_prob(scaled(x, a.c_t, ignore), r.lse_p));
+    stands = t >= 0 && u * q < __builtin_amdgcn_exp2f(log_prob(clean(x, ignore), r.p, a.c_t));
   }
   r.flags = (flag ? ST_NONFINITE : 0) | (j < drafts && t < 0 ? ST_BAD_TOKEN : 0);
   if (lane == 0) {
@@ -332,7 +323,7 @@ __global__ void __launch_bounds__(VF_THREADS) verify_rows(VerifyArgs a) {
           v = k > v ? k : v;
         } else {
           const Lse l = unpack_lse(s_stat[i], bad);
-          t.join(l.m, l.s);
+          t.join(l.m, l.s, p < a.pieces_t ? a.c_t : a.c_d);
         }
       }
       v = GREEDY ? pack_key(v, bad) : pack_lse(t.m, t.s, bad);
@@ -371,6 +362,7 @@ template <class T, bool GREEDY>
 __global__ void __launch_bounds__(VF_THREADS) verify_pick(VerifyArgs a) {
   __shared__ int s_flags, s_last;
   __shared__ unsigned long long s_key[VF_THREADS / 64];
+  __shared__ int s_who[VF_THREADS / 64];
   const int b = blockIdx.x / a.pieces_r, piece = blockIdx.x % a.pieces_r;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const ChunkRows cr = request_rows(a, b);
@@ -410,61 +402,61 @@ __global__ void __launch_bounds__(VF_THREADS) verify_pick(VerifyArgs a) {
     const int hot = rejected && !a.draft ? target_id(a, a.draft_tokens[(size_t)b * a.k + n]) : -1;
     bool bad_noise = false, bad_map = false;
     const bool careful = (rn.flags & ST_NONFINITE) != 0;
-    // The best (score, token) of elements [e0, e1) for a thread: of the residual, or of the target's own probabilities.
-    auto choose = [&](int e0, int e1, auto own_) -> unsigned long long {
-      constexpr bool OWN = decltype(own_)::value;
-      const bool sub = !OWN && drow;
-      float best = -INFINITY;
-      int at = -1;
-      each_piece(row, e0, e1, [&](int v0, const float* x, auto cnt) {
-        constexpr int N = decltype(cnt)::value;
-        float gn[N], y[N];
-        int d[N];
-        load_n<N>(noise + v0, gn);
-        if (sub) {
-          if (a.t2d) load_n<N>(a.t2d + v0, d);
-#pragma unroll
-          for (int i = 0; i < N; ++i) {
-            if (!a.t2d) d[i] = v0 + i < a.Vd ? v0 + i : -1;
-            if ((unsigned)(d[i] + 1) > (unsigned)a.Vd) {
-              bad_map = true;
-              d[i] = -1;
-            }
-            y[i] = d[i] >= 0 ? drow[d[i]] : -INFINITY;
-          }
-        }
+    auto draft_of = [&](int v) {   // draft id of a target token, or -1
+      const int d = a.t2d ? a.t2d[v] : v < a.Vd ? v : -1;
+      return d < a.Vd ? max(d, -1) : -1;
+    };
+    // The thread's best (score, token), and the most that a token could score whose p and q agree in their first ten
+    // bits, so that little of their difference is left in 32.
+    float best = -INFINITY, doubt = -INFINITY;
+    int at = -1;
+    const int2 e = piece_range(a.V, a.pieces_r, piece);
+    each_piece(row, e.x, e.y, [&](int v0, const float* x, auto cnt) {
+      constexpr int N = decltype(cnt)::value;
+      float gn[N], y[N];
+      int d[N];
+      load_n<N>(noise + v0, gn);
+      if (drow) {
+        if (a.t2d) load_n<N>(a.t2d + v0, d);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          bool ignore = false;
-          float lp = __builtin_fmaf(x[i], a.c_t, -rn.lse_p);
-          if (careful) lp = log_prob(scaled(x[i], a.c_t, ignore), rn.lse_p);
-          float lg = lp;
-          if (sub) {
-            float lq = __builtin_fmaf(y[i], a.c_d, -rn.lse_q);
-            if (careful) lq = log_prob(scaled(y[i], a.c_d, ignore), rn.lse_q);
-            const float q = __builtin_amdgcn_exp2f(lq);
-            // (of a difference below 0 the logarithm is NaN, which no comparison lets through)
-            if (q > 0.f) lg = __builtin_amdgcn_logf(__builtin_amdgcn_exp2f(lp) - q);
+          if (!a.t2d) d[i] = v0 + i < a.Vd ? v0 + i : -1;
+          if ((unsigned)(d[i] + 1) > (unsigned)a.Vd) {
+            bad_map = true;
+            d[i] = -1;
           }
-          const float sc = __builtin_fmaf(lg, LN2, gn[i]);
-          bad_noise |= !(gn[i] == gn[i]);
-          const bool better = sc > best && (OWN || v0 + i != hot);
-          best = better ? sc : best;
-          at = better ? v0 + i : at;
+          y[i] = d[i] >= 0 ? drow[d[i]] : -INFINITY;
         }
-      });
-      return at < 0 ? 0ull : ((unsigned long long)score_ord(best + 0.f) << 32) | ~(unsigned)at;
-    };
-    auto wave_best = [&](unsigned long long k) {
+      }
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        bool ignore = false;
+        float lp = __builtin_fmaf(x[i] - rn.p.m, a.c_t, -rn.p.log_s);
+        if (careful) lp = log_prob(clean(x[i], ignore), rn.p, a.c_t);
+        float lg = lp;
+        if (drow) {
+          float lq = __builtin_fmaf(y[i] - rn.q.m, a.c_d, -rn.q.log_s);
+          if (careful) lq = log_prob(clean(y[i], ignore), rn.q, a.c_d);
+          const float p = __builtin_amdgcn_exp2f(lp), q = __builtin_amdgcn_exp2f(lq);
+          // (of a difference below 0 the logarithm is NaN, which no comparison lets through)
+          if (q > 0.f) {
+            lg = __builtin_amdgcn_logf(p - q);
+            if (fabsf(p - q) < 0x1p-10f * p) doubt = fmaxf(doubt, __builtin_fmaf(lp - 10.f, LN2, gn[i]));
+          }
+        }
+        const float sc = __builtin_fmaf(lg, LN2, gn[i]);
+        bad_noise |= !(gn[i] == gn[i]);
+        const bool better = sc > best && v0 + i != hot;
+        best = better ? sc : best;
+        at = better ? v0 + i : at;
+      }
+    });
+    auto all_best = [&](unsigned long long k) {   // the largest of the workgroup, in every thread
 #pragma unroll
       for (int o = 32; o > 0; o >>= 1) {
         const unsigned long long v = ((unsigned long long)__shfl_xor((unsigned)(k >> 32), o) << 32) | __shfl_xor((unsigned)k, o);
         k = v > k ? v : k;
       }
-      return k;
-    };
-    auto all_best = [&](unsigned long long k) {   // of the workgroup, in every thread
-      k = wave_best(k);
       __syncthreads();
       if (lane == 0) s_key[wave] = k;
       __syncthreads();
@@ -473,20 +465,84 @@ __global__ void __launch_bounds__(VF_THREADS) verify_pick(VerifyArgs a) {
       for (int w = 1; w < VF_THREADS / 64; ++w) k = s_key[w] > k ? s_key[w] : k;
       return k;
     };
-    const int2 e = piece_range(a.V, a.pieces_r, piece);
-    const unsigned long long mine = all_best(choose(e.x, e.y, std::false_type{}));
+    const unsigned long long mine =
+        all_best(at < 0 ? 0ull : ((unsigned long long)score_ord(best + 0.f) << 32) | ~(unsigned)at);
+    const unsigned long long most = all_best((unsigned long long)score_ord(doubt) << 32);
     const int f = (__any(bad_noise) ? ST_NONFINITE : 0) | (__any(bad_map) ? ST_BAD_TOKEN : 0);
     if (f && lane == 0) set_status(a.status, f);
+    unsigned long long* keys = a.keys + b * kVerifyLine / 2;
     if (tid == 0) {
-      if (mine) __hip_atomic_fetch_max(a.keys + b * kVerifyLine / 2, mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (mine) __hip_atomic_fetch_max(keys, mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_fetch_max(keys + 1, most, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       wait_vmcnt<0>();   // done before the counter is raised
       s_last = atomicAdd(a.done + b * kVerifyLine, 1) == a.pieces_r - 1;
     }
     __syncthreads();
     if (!s_last) return;
-    unsigned long long top = fetch(a.keys + b * kVerifyLine / 2);
-    if (!top) top = all_best(choose(0, a.V, std::true_type{}));   // (rare: no positive difference anywhere)
-    next = top ? key_token(top) : 0;                              // (nothing above -inf: the lowest token)
+    const unsigned long long top = fetch(keys);
+    if (drow && (!top || fetch(keys + 1) >> 32 >= top >> 32)) {
+      // Rare: the difference that decides is below what 32 bits hold of p and q.  The row once more in 64.
+      auto sum_of = [&](auto value, int count, double m, double c) {
+        double t = 0.;
+        for (int v = tid; v < count; v += VF_THREADS) t += exp2((value(v) - m) * c);
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) t += __shfl_xor(t, o);
+        __syncthreads();
+        if (lane == 0) s_key[wave] = (unsigned long long)__double_as_longlong(t);
+        __syncthreads();
+        t = 0.;
+#pragma unroll
+        for (int w = 0; w < VF_THREADS / 64; ++w) t += __longlong_as_double((long long)s_key[w]);
+        return t;
+      };
+      bool ignore = false;
+      auto target = [&](int v) { return (double)clean(to_f32(row[v]), ignore); };
+      auto draft = [&](int d) { return (double)clean(drow[d], ignore); };
+      const double sp = sum_of(target, a.V, rn.p.m, a.c64_t), sq = sum_of(draft, a.Vd, rn.q.m, a.c64_d);
+      for (int own = 0; own < 2; ++own) {   // (own: no difference is positive)
+        double hi = -INFINITY;
+        int who = INT_MAX;
+        for (int v = tid; v < a.V; v += VF_THREADS) {
+          double p = exp2((target(v) - rn.p.m) * a.c64_t) / sp;
+          const int d = draft_of(v);
+          if (!own && d >= 0) p -= exp2((draft(d) - rn.q.m) * a.c64_d) / sq;
+          const double sc = log(p) + noise[v];   // (NaN below 0)
+          if (sc > hi) {
+            hi = sc;
+            who = v;
+          }
+        }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+          const double h2 = __shfl_xor(hi, o);
+          const int w2 = __shfl_xor(who, o);
+          if (h2 > hi || (h2 == hi && w2 < who)) {
+            hi = h2;
+            who = w2;
+          }
+        }
+        __syncthreads();
+        if (lane == 0) {
+          s_key[wave] = (unsigned long long)__double_as_longlong(hi);
+          s_who[wave] = who;
+        }
+        __syncthreads();
+        for (int w = 0; w < VF_THREADS / 64; ++w) {
+          const double h2 = __longlong_as_double((long long)s_key[w]);
+          if (h2 > hi || (h2 == hi && s_who[w] < who)) {
+            hi = h2;
+            who = s_who[w];
+          }
+        }
+        next = who == INT_MAX ? 0 : who;
+        if (who != INT_MAX) break;
+      }
+    } else if (top) {
+      next = key_token(top);
+    } else {   // (p is all on the draft too, or nothing is above -inf: the lowest token)
+      bool ignore = false;
+      next = hot >= 0 && clean(to_f32(row[hot]), ignore) > -INFINITY && noise[hot] > -INFINITY ? hot : 0;
+    }
   }
   for (int i = tid; i <= a.k; i += VF_THREADS)
     out[i] = i < n ? target_id(a, a.draft_tokens[(size_t)b * a.k + i]) : i == n ? next : -1;

@@ -145,6 +145,39 @@ def test_a_request_longer_than_the_positions_there_are():
     assert torch.count_nonzero(o[20:40]) == 0
 
 
+def test_pages_past_32_bit_offsets():
+    """A pool of more than 2^32 elements, used at its end."""
+    import torch
+    u = _u()
+    x = u.batch([200, 40], [17, 3], 8, 4, 128, ps=64, seed=7, poison=0.0)
+    want, _ = u.attend(x)
+    per = 64 * 4 * 128
+    pages = (1 << 32) // per + 100
+    assert torch.cuda.mem_get_info()[0] > 2 * 2 * pages * per + (1 << 30)
+    y = dict(x, pages=pages)
+    for name in ("k_cache", "v_cache"):
+        big = torch.empty((pages, 64, 4, 128), dtype=torch.bfloat16, device="cuda")
+        big[pages - x["pages"]:] = x[name]
+        y[name] = big
+    y["table"] = torch.where(x["table"] >= 0, x["table"] + (pages - x["pages"]), x["table"])
+    y["cfg"] = hspec.chunk_cfg(2, x["T"], x["max_new"], 8, 4, 128, 64, x["table"].shape[1], pages)
+    o, ws = u.attend(y)
+    assert hspec.read_status(ws) == 0 and torch.equal(o, want)
+    # and the append that fills them
+    qkv = torch.randn(x["T"], 16 * 128, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    res = []
+    for z in (x, y):
+        wa = hspec.workspace(hspec.chunk_append_workspace(z["cfg"]))
+        q = torch.zeros_like(z["q"])
+        hspec.chunk_append(z["cfg"], qkv, z["cu"], z["lens"], q, z["k_cache"], z["v_cache"], z["table"], wa)
+        assert hspec.read_status(wa) == 0
+        res.append((q, z["k_cache"][-x["pages"]:], z["v_cache"][-x["pages"]:]))
+    for a, b in zip(*res):
+        assert torch.equal(a, b)
+    del big, y, res
+    torch.cuda.empty_cache()
+
+
 def test_same_bits_every_time_and_wherever_pages_live():
     import torch
     u = _u()

@@ -262,6 +262,67 @@ def test_tokens_follow_the_target():
     assert ((counts / n - p).abs() <= 5 * torch.sqrt(p * (1 - p) / n) + 1e-9).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("mode", ["greedy", "sample", "onehot"])
+@pytest.mark.parametrize("shift", [1, 3])
+def test_rows_at_any_element(shift, mode, dtype):
+    """Logits that begin anywhere: no 16-byte boundary is expected of a row."""
+    s = _make(3, 4, 5003, 2001, dtype, mode, seed=shift)
+    for name in ("target", "draft", "gumbel"):
+        if s[name] is not None:
+            t = s[name]
+            big = t.new_empty(t.numel() + 8)
+            big[shift:shift + t.numel()] = t.flatten()
+            s[name] = big[shift:shift + t.numel()].view(t.shape)
+    _check(s)
+
+
+@pytest.mark.parametrize("T", [0.02, 1.0, 5.0])
+@pytest.mark.parametrize("mode", ["sample", "onehot"])
+def test_temperatures(mode, T):
+    """At low temperatures too the probabilities are those of differences of logits, not of their scaled values."""
+    for seed in range(3):
+        s = _make(8, 4, 900, None, "f32", mode, seed=seed)
+        s["target"] += 500.0                                  # (probabilities do not change; 500 / 0.02 is far from small)
+        s["T"], s["Td"] = T, T
+        if s["draft"] is not None:
+            s["draft"] += 500.0
+        _check(s)
+
+
+def test_differences_below_32_bits():
+    """p and q that agree in their leading bits: the residual is what 64 bits leave of them, or p itself where nothing
+    is positive."""
+    import torch
+    for seed in range(4):
+        s = _make(6, 2, 700, 500 if seed % 2 else None, "f32", "sample", seed=seed, close=1e-4)
+        s["T"] = s["Td"]
+        s["u"].fill_(1 - 2.0 ** -24)                          # (every draft with p < q is rejected)
+        tok, acc, ws = _run(s)
+        rt, ra = _ref(s)
+        for b in range(6):                                    # the decisions are at a border, the choices are not
+            if acc[b] == ra[b]:
+                assert torch.equal(tok[b], rt[b]), (seed, b)
+        assert (acc == ra).sum() >= 4
+    # q = p: a token that p does not give at all is rejected, and the choice falls back to p
+    s = _make(3, 1, 400, None, "f32", "sample", close=0.0)
+    s["target"] = s["target"].clone()
+    s["T"] = s["Td"] = 1.0
+    t = s["tok"][:, 0].long()
+    for b in range(3):
+        s["target"][2 * b, t[b]] = -float("inf")
+        s["draft"][b, 0, t[b]] = -float("inf")                # q(t) = 0 and p(t) = 0: 0 < 0 does not hold
+    _check(s)
+    # all of p on a draft that all of q is on, and a draw that no draft stands against
+    s = _make(2, 1, 300, None, "f32", "onehot")
+    t = s["tok"][:, 0].long()
+    s["target"] = torch.full_like(s["target"], -float("inf"))
+    for b in range(2):
+        s["target"][2 * b, t[b]] = 1.0
+    s["u"].fill_(1.0)
+    _check(s)
+
+
 @pytest.mark.parametrize("mode", ["greedy", "sample"])
 def test_graph_replays(mode):
     import torch
