@@ -501,6 +501,7 @@ size_t hspec_chunk_attn_workspace(const hspec_chunk_cfg* cfg, int max_len);
  * Greedy (u and gumbel NULL, draft_logits NULL): draft j stands while it is the argmax of row j;
  *   next = argmax of row a.  A tie goes to the lowest id.
  * tokens [B, k+1] int32: the a drafts that stand (target ids), next, then -1; n_accepted [B] = a.
+ * tokens must not lie over draft_tokens (HSPEC_ERR_UNSUPPORTED).
  * NaN logits count as -inf and +inf as the largest float; they, a NaN of gumbel and a row of nothing but
  * -inf set HSPEC_DEV_NONFINITE (rows up to a are looked at); a draft id outside [0, draft_vocab)
  * or a mapped id out of range does not stand (or counts as -1) and sets HSPEC_DEV_BAD_TOKEN;

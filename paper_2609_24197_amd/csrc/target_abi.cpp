@@ -227,6 +227,8 @@ HSPEC_API hspec_status hspec_verify(const hspec_verify_cfg* cfg, const void* tar
   if (!cu_rows && cfg->rows != (long long)cfg->B * (cfg->k + 1))
     return fail(HSPEC_ERR_SHAPE, "without cu_rows, rows must be B * (k + 1)");
   if (hspec_status s = check_ws(workspace, ws_bytes, hspec_verify_workspace(cfg))) return s;
+  const size_t drafts = (size_t)cfg->B * cfg->k * 4;
+  if (hspec_status s = check_apart(draft_tokens, drafts, tokens, drafts + (size_t)cfg->B * 4)) return s;
   Arena ar{(char*)workspace};
   hspec::VerifyArgs a;
   plan_verify(ar, *cfg, a);

@@ -116,6 +116,13 @@ def test_verify_refusals(kw, want):
     assert _lib().hspec_last_error()
 
 
+def test_tokens_over_drafts_are_refused():
+    far = C.c_void_p(FAKE.value + (1 << 24))
+    for tok, tokens in ((FAKE, FAKE), (FAKE, C.c_void_p(FAKE.value + 4 * 7 * 4 - 4)), (C.c_void_p(FAKE.value + 4 * 8 * 4 - 4), FAKE)):
+        assert _verify(ptrs=dict(tok=tok, tokens=tokens, acc=far)) == UNSUPPORTED
+        assert b"lies over" in _lib().hspec_last_error()
+
+
 def test_workspace_of_a_bad_verification_is_zero():
     c = hspec.verify_cfg(4, 7, 32, 1000, 2000)
     assert _lib().hspec_verify_workspace(C.byref(c)) == 0
