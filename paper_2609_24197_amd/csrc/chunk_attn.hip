@@ -47,10 +47,10 @@ static __device__ __align__(16) const unsigned char zero_row[512] = {};
 // many powers of two; probabilities then stay below 2^8.
 constexpr float CHUNK_SLACK = 8.f;
 
-// NW waves, KT keys per tile.  ONCE: a request's rows
-// fit one tile, so its K and V are read once: non-temporal loads, and a die takes all heads of its units, so that it
-// reads whole rows of the cache; otherwise a die keeps to its KV heads, whose K and V the tiles of a request share
-// in its L2.
+// NW waves, KT keys per tile.  ONCE: a request's rows fit one tile, so its K and V are read once: non-temporal loads,
+// and a die takes all heads of its units, so that it reads whole rows of the cache (64 requests of 1 row 212 us, 237
+// the other way); otherwise a die keeps to its KV heads, whose K and V the tiles of a request share in its L2 (three
+// prompts 1284 us, 1766 the other way).
 template <class T_, int D_, int NW_, int KT_, bool ONCE_>
 struct Chunk {
   typedef T_ T;
@@ -548,7 +548,7 @@ __global__ void __launch_bounds__(PL_THREADS) chunk_plan(ChunkAttnArgs a) {
   }
   for (int i = tid; i < kChunkClasses * kChunkQueueStride; i += PL_THREADS) a.queue[i] = 0;
 
-  // Requests [c0, c0 + 1024): rows, lengths and tile counts into LDS.  Returns the chunk's tiles.
+  // Requests [c0, c0 + PL_THREADS): rows, lengths and tile counts into LDS.  Returns the chunk's tiles.
   auto load = [&](int c0) -> int {
     __syncthreads();
     const int b = c0 + tid;
@@ -684,8 +684,9 @@ constexpr int MG_THREADS = 256;
 
 // o = sum_i O_i 2^(m_i - m*) / sum_i l_i 2^(m_i - m*) over a row's pieces, in an order of their own (not of time).
 // Bound by the round trips of a row's loads: a workgroup takes one row, with its pieces spread over groups of D / 4
-// threads, where that makes few workgroups (few rows, so perhaps many pieces each: 1 request of 32768 tokens, 128
-// pieces, 77 us for the whole call with a thread for all of a row's pieces, now 53), else 1024 / D rows.
+// threads, where that makes few workgroups (few rows, so perhaps many pieces each: 1 request of 32768 tokens, 64 pieces,
+// 47 us for the whole call, 60 with a thread for all of a row's pieces), else 1024 / D rows (64 requests of
+// 68 rows 255 us for the whole call, 288 with a row each).
 constexpr int MG_FEW = 4096;   // workgroups up to which each takes one row
 
 template <class T, int D>
@@ -817,15 +818,17 @@ __global__ void __launch_bounds__(MG_THREADS) chunk_merge_row(ChunkAttnArgs a, i
 
 // ----------------------------------------------------------------------------- launch
 
-// The instance of a tile shape (chunk_shape).
+// The instance of a tile (chunk_bounds).
 template <class F>
 auto with_variant(const ChunkAttnArgs& a, F f) {
   auto by_rows = [&](auto t, auto d) {
     typedef typename decltype(t)::type T;
     constexpr int D = decltype(d)::value;
-    constexpr int KT2 = chunk_key_tile(2, sizeof(T) == 4), KT4 = chunk_key_tile(4, sizeof(T) == 4);
-    if (a.tile_rows == 32) return f(Chunk<T, D, 1, chunk_key_tile(1, sizeof(T) == 4), true>{});
-    if (a.tile_rows == 64) return f(Chunk<T, D, 2, KT2, true>{});
+    constexpr bool F32 = sizeof(T) == 4;
+    constexpr int KT4 = chunk_key_tile(4, F32);
+    if (a.tile_rows == 32) return f(Chunk<T, D, 1, chunk_key_tile(1, F32), true>{});
+    if constexpr (F32)
+      if (a.tile_rows == 64) return f(Chunk<T, D, 2, chunk_key_tile(2, F32), true>{});
     return a.once ? f(Chunk<T, D, 4, KT4, true>{}) : f(Chunk<T, D, 4, KT4, false>{});
   };
   if (a.f32) return a.D == 128 ? by_rows(std::common_type<float>{}, Int<128>{}) : by_rows(std::common_type<float>{}, Int<64>{});

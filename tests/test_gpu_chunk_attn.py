@@ -54,6 +54,26 @@ def test_long_caches_are_split(n, dtype):
     u.check_attend(u.batch([20011, 3, 9000], [n, n, n], 8, 2, 128, dtype=dtype, seed=n))
 
 
+@pytest.mark.parametrize("window", [0, 100])
+@pytest.mark.parametrize("Hq,Hkv,D", [(32, 8, 128), (8, 8, 64), (24, 8, 128)])
+@pytest.mark.parametrize("new", [[1, 1, 1, 1], [8, 0, 3, 1]])
+def test_few_rows_over_many_long_caches(Hq, Hkv, D, new, window):
+    """One wave a unit: 4 requests of 8 KV heads, more than 4096 positions."""
+    import torch
+    u = _u()
+    x = u.batch([4200, 0, 31, 999], new, Hq, Hkv, D, window=window, seed=D + window)
+    o, ws = u.check_attend(x)
+    assert hspec.read_status(ws) == 0
+    # the first request's last token, infinite or NaN: its other rows as they were
+    last, pos = new[0] - 1, 4200 + new[0] - 1
+    for what in (float("inf"), float("nan")):
+        y = {**x, "v_cache": x["v_cache"].clone()}
+        y["v_cache"][int(x["table"][0, pos // x["ps"]]), pos % x["ps"]] = what
+        p, _ = u.attend(y)
+        assert torch.equal(p[:last], o[:last]) and torch.equal(p[new[0]:], o[new[0]:])
+        assert not torch.isfinite(p[last].float()).any()
+
+
 def test_many_requests():
     import torch
     u = _u()
