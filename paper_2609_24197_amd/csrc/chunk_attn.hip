@@ -20,8 +20,8 @@
 // fp32 storage takes the fp32 matrix products (32 x 32 x 2), so nothing is rounded below 32 bits.
 //
 // Bound by reading K and V where requests have few rows (64 requests x 1 token, 512..8192 cached, 32 and 8 heads of
-// 128: 212 us for 1.2 GB; x 17 tokens 254), by the matrix and vector units, busy in 52 % and 46 % of the cycles, in
-// prompts (three of about 6000 tokens 1290 us, 1054 TFLOP/s; 2000 tokens behind 30000, 64 heads, 1856 us, 1094).
+// 128: 212 us for 1.2 GB; x 17 tokens 256), by the matrix and vector units, busy in 52 % and 46 % of the cycles, in
+// prompts (three of about 6000 tokens 1277 us, 1065 TFLOP/s; 2000 tokens behind 30000, 64 heads, 1840 us, 1104).
 #include <algorithm>
 #include <atomic>
 #include <cfloat>

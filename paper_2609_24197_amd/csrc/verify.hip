@@ -494,7 +494,8 @@ __global__ void __launch_bounds__(VF_THREADS) verify_pick(VerifyArgs a) {
     if (!s_last) return;
     const unsigned long long top = fetch(keys);
     if (drow && (!top || fetch(keys + 1) >> 32 >= top >> 32)) {
-      // Rare: the difference that decides is below what 32 bits hold of p and q.  The row once more in 64.
+      // Rare: the difference that decides is below what 32 bits hold of p and q.  The row once more in 64 (0.85 ms at
+      // 131072 tokens).
       auto sum_of = [&](auto value, int count, double m, double c) {
         double t = 0.;
         for (int v = tid; v < count; v += VF_THREADS) t += exp2((value(v) - m) * c);
