@@ -40,8 +40,7 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 #define LDS_AS __attribute__((address_space(3)))
 #define GLB_AS __attribute__((address_space(1)))
 
-// Source of K/V rows whose page id is outside the pool, and of tile rows no unit sees.
-static __device__ __align__(16) const unsigned char zero_row[512] = {};
+constexpr int BUFFER_FLAGS = 0x00027000;   // 32-bit data, no swizzle
 
 // Softmax reference maximum: raised, and O and the sum rescaled, only when a tile exceeds it by more than this
 // many powers of two; probabilities then stay below 2^8.
@@ -130,6 +129,7 @@ __device__ __forceinline__ bool chunk_unit(const ChunkAttnArgs& a, const ChunkUn
   const T* Kc = static_cast<const T*>(a.k_cache);
   const T* Vc = static_cast<const T*>(a.v_cache);
   const int row_elems = a.Hkv * D;
+  const unsigned row_bytes = (unsigned)row_elems * (unsigned)sizeof(T);
   const int R = u.n * g;                        // rows of the request
   const int c0 = u.tile * C::ROWS + wave * 32;  // first row of this wave
   const bool live = c0 < R;
@@ -183,15 +183,15 @@ __device__ __forceinline__ bool chunk_unit(const ChunkAttnArgs& a, const ChunkUn
     const int v2 = __builtin_amdgcn_readlane(id2, e & 63), v3 = __builtin_amdgcn_readlane(id3, e & 63);
     return e < 128 ? (e < 64 ? v0 : v1) : (e < 192 ? v2 : v3);
   };
-  // this lane's row and 16-byte piece of each DMA instruction of a group (the same in every group), and its offset
+  // this lane's row of DMA instruction i of a group, and the byte offset of its 16-byte piece from the group's first
+  // row (the same in every group)
+  auto dma_row = [&](int i) { return (i * 64 + lane) / C::CPR; };
   unsigned at[C::NI];
-  int rr[C::NI], piece[C::NI];
 #pragma unroll
   for (int i = 0; i < C::NI; ++i) {
-    rr[i] = (i * 64 + lane) / C::CPR;
-    const int r = wave * C::WROWS + rr[i];
-    piece[i] = kv_off<T, C::CPR>(r, (i * 64 + lane) % C::CPR * C::EPC) - r * D;   // stored at this lane's place
-    at[i] = (unsigned)(rr[i] * row_elems + piece[i]) * (unsigned)sizeof(T);
+    const int r = wave * C::WROWS + dma_row(i);
+    const int piece = kv_off<T, C::CPR>(r, (i * 64 + lane) % C::CPR * C::EPC) - r * D;   // stored at this lane's place
+    at[i] = (unsigned)(dma_row(i) * row_elems + piece) * (unsigned)sizeof(T);
   }
   // DMA of tile ti into a stage: K rows, then V rows
   auto issue = [&](int ti, T* sb) {
@@ -203,29 +203,21 @@ __device__ __forceinline__ bool chunk_unit(const ChunkAttnArgs& a, const ChunkUn
       if (any && (key0 >> lps) >= pg0 + 256) load_ids(key0 >> lps);
       const int pid = any ? page_id(key0 >> lps) : -1;
       const bool good = (unsigned)pid < (unsigned)a.num_pages;
-      const size_t base = (((size_t)(good ? pid : 0) << lps) + (key0 & (a.ps - 1))) * row_elems + h * D;
-      const char* kp = reinterpret_cast<const char*>(Kc + base);
-      const char* vp = reinterpret_cast<const char*>(Vc + base);
-      unsigned off[C::NI];
-#pragma unroll
-      for (int i = 0; i < C::NI; ++i) off[i] = at[i];
-      if (!good || key0 < k_min || key0 + C::GR > u.k1) {
-        // Rows outside the visible range repeat one inside it (they are masked, and a stale slot may hold NaN);
-        // rows of a page outside the pool, and groups with nothing visible, are zeros.
-        if (any && !good && lane == 0) set_status(a.status, ST_BAD_PAGE);
-        const int first = max(k_min - key0, 0), last = max(min(u.k1 - key0, C::GR) - 1, 0);
-        if (!good) kp = vp = reinterpret_cast<const char*>(zero_row);
-#pragma unroll
-        for (int i = 0; i < C::NI; ++i)
-          off[i] = (unsigned)((good ? min(max(rr[i], first), last) * row_elems : 0) + piece[i]) * (unsigned)sizeof(T);
-      }
+      // Buffers over the group's visible rows [first, last): what lies outside, a row before them by wrap-around, reads
+      // as zeros without an access.  (No repeats of a row in its place: its infinity times weight 0 is NaN.)
+      const int first = max(k_min - key0, 0), last = good ? min(u.k1 - key0, C::GR) : first;
+      if (any && !good && lane == 0) set_status(a.status, ST_BAD_PAGE);
+      const size_t base = (((size_t)(good ? pid : 0) << lps) + ((key0 + first) & (a.ps - 1))) * row_elems + h * D;
+      const unsigned bytes = (unsigned)max(last - first, 0) * row_bytes, skip = (unsigned)first * row_bytes;
+      const auto kr = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(Kc + base), 0, bytes, BUFFER_FLAGS);
+      const auto vr = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(Vc + base), 0, bytes, BUFFER_FLAGS);
       int to = r0 * D;
       asm volatile("" : "+s"(to));   // (else the LDS address of every instruction and stage takes a register of its own)
 #pragma unroll
       for (int i = 0; i < C::NI; ++i) {
         T* dst = sb + to + i * 64 * C::EPC;
-        __builtin_amdgcn_global_load_lds((const GLB_AS void*)(kp + off[i]), (LDS_AS void*)dst, 16, 0, C::AUX);
-        __builtin_amdgcn_global_load_lds((const GLB_AS void*)(vp + off[i]), (LDS_AS void*)(dst + C::TILE), 16, 0, C::AUX);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (LDS_AS void*)dst, 16, at[i] - skip, 0, 0, C::AUX);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (LDS_AS void*)(dst + C::TILE), 16, at[i] - skip, 0, 0, C::AUX);
       }
     }
   };

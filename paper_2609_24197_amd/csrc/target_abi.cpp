@@ -133,7 +133,7 @@ static void plan_chunk_attn(Arena& ar, const hspec_chunk_cfg& c, int max_len, hs
   a.queue = ar.take<int>(hspec::kChunkClasses * hspec::kChunkQueueStride);
   a.units = ar.take<hspec::ChunkUnit>(a.max_units);
   a.splits = ar.take<hspec::ChunkSplit>(a.max_splits);
-  // one new token a request: its rows see the same keys, and keys it does not see are not in its tiles
+  // one new token a request: its rows see the same keys, and the others' places in its tiles are zeros
   if (a.max_new > 1) a.redo = ar.take<int>(a.max_redo);
   const size_t rows = (size_t)a.max_slots * c.Hkv * a.tile_rows;
   a.part_o = ar.take<float>(rows * c.D);

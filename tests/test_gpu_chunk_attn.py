@@ -121,6 +121,54 @@ def test_later_tokens_never_change_a_row(dtype, what):
     assert torch.equal(o[:i], clean[:i]) and torch.isnan(o[i:new[0], :g].float()).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("what", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("new,window", [([1, 1], 0), ([1, 1], 50), ([3, 1], 50)])
+def test_what_a_row_sees_reaches_it(new, window, what, dtype):
+    """Infinities and NaN at the first and the last position of a row come out as they are."""
+    import torch
+    u = _u()
+    x = u.batch([100, 20], new, 8, 2, 128, window=window, dtype=dtype, seed=6)
+    clean, _ = u.attend(x)
+    row, last = new[0] - 1, 100 + new[0] - 1
+    for pos in (last, last - window + 1 if window else 0):
+        y = {**x, "v_cache": x["v_cache"].clone()}
+        y["v_cache"][int(x["table"][0, pos // 16]), pos % 16, 1, 5] = what
+        o, _ = u.attend(y)
+        seen = o[row, 4:, 5]
+        assert (torch.isnan(seen) if what != what else seen == what).all(), pos
+        same = torch.ones_like(o, dtype=torch.bool)
+        same[:new[0], 4:, 5] = False
+        assert torch.equal(o[same], clean[same])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Hq,Hkv,D", [(4, 1, 64), (7, 1, 128), (8, 8, 128)])
+@pytest.mark.parametrize("window", [1, 7, 16, 90])
+def test_what_a_single_row_does_not_see(window, Hq, Hkv, D, dtype):
+    """NaN in every cached K and V before the window and in every slot behind the row."""
+    import torch
+    u = _u()
+    x = u.batch([100, 37], [1, 1], Hq, Hkv, D, window=window, dtype=dtype, seed=window)
+    clean, _ = u.attend(x)
+    for b, L in enumerate((100, 37)):
+        for pos in range(0, max(0, L + 1 - window)):
+            for c in ("k_cache", "v_cache"):
+                x[c][int(x["table"][b, pos // 16]), pos % 16] = float("nan")
+    o, _ = u.attend(x)
+    assert torch.equal(o, clean)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_no_tokens_at_all(dtype):
+    """Requests without new tokens only: every row belongs to no request."""
+    import torch
+    u = _u()
+    x = u.batch([100, 0], [0, 0], 8, 2, 64, dtype=dtype, seed=6)
+    o, ws = u.attend(x)
+    assert hspec.read_status(ws) == 0 and torch.equal(o, torch.full_like(o, 7.0))
+
+
 def test_bad_pages_read_as_zeros():
     import torch
     u = _u()
