@@ -6,6 +6,8 @@
 
 #include <type_traits>
 
+#include "status.h"
+
 namespace hspec {
 
 typedef __bf16 bf16;
@@ -18,12 +20,6 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int WAVE = 64;
-
-// Device status word bits (first int32 of every workspace).
-enum : int {
-  ST_BAD_PAGE = 1,      // a page id outside [0, num_pages)
-  ST_BAD_CTX_LEN = 2,   // ctx_len < 0 or beyond the table / max_ctx_len
-};
 
 __device__ __forceinline__ float bf2f(bf16 v) { return (float)v; }
 __device__ __forceinline__ bf16 f2bf(float v) { return (bf16)v; }   // v_cvt_pk_bf16_f32, RNE

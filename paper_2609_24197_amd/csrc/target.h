@@ -9,9 +9,6 @@
 
 namespace hspec {
 
-// Status bit of a ragged row array (cu_new, cu_rows) that is no increasing division of the rows.
-enum : int { ST_BAD_ROWS = 16 };
-
 // ------------------------------------------------------------------------------ append
 struct ChunkAppendArgs {
   const void* qkv = nullptr;          // [T, (Hq + 2 Hkv) D], fp32 or bf16

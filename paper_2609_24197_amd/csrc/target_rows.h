@@ -1,7 +1,7 @@
 // Which rows of a ragged batch belong to which request, checked: shared by the kernels that take one.
 #pragma once
-#include "common.h"
-#include "target.h"
+#include <hip/hip_runtime.h>
+#include <stdint.h>
 
 namespace hspec {
 
