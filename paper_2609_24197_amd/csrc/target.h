@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <climits>
 
 namespace hspec {
 
@@ -63,6 +64,7 @@ struct ChunkAttnArgs {
 constexpr int chunk_key_tile(int waves, bool f32) { return f32 || waves == 1 ? 32 : 64; }
 constexpr int chunk_waves_per_simd(bool f32, int D) { return f32 && D == 128 ? 1 : 2; }
 constexpr int kChunkMinSplit = 64;   // keys a piece of a split tile has at least
+constexpr int kMaxPositions = INT_MAX - 65536;   // of a request: places past the end of a tile stay inside 31 bits
 
 // Keys a unit takes at most, in whole key tiles, for `keys` keys of `tiles` tiles of rows: where the tiles leave most of
 // the chip free, what makes one round of units (so every piece starts at once: 1 request of 32768 tokens 47 us, 60 in
@@ -72,7 +74,8 @@ __host__ __device__ inline int chunk_unit_keys(const ChunkAttnArgs& a, unsigned 
   const float spare = (float)a.slots - (float)tiles * (float)a.Hkv;
   const float units = spare * 4.f >= (float)a.slots * 3.f ? spare : (float)a.target;
   const float per = (float)keys * (float)a.Hkv / units * 1.0001f;
-  const float least = (float)a.min_split, most = 1e9f;
+  // (at the most no tile is split, so that the bound on the pieces holds for any number of keys)
+  const float least = (float)a.min_split, most = (float)kMaxPositions;
   return ((int)(per < least ? least : per > most ? most : per) + a.key_tile) / a.key_tile * a.key_tile;
 }
 // Even pieces of a tile of len keys, each a whole number of key tiles but the last: their number, and their length in q.

@@ -3,7 +3,6 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <climits>
 #include <cmath>
 #include <cstdio>
 #include <initializer_list>
@@ -85,7 +84,7 @@ hspec_status check_chunk(const hspec_chunk_cfg* c) {
 }
 
 int positions(const hspec_chunk_cfg& c) {
-  return (int)std::min((long long)c.max_pages * c.page_size, (long long)INT_MAX - 65536);
+  return (int)std::min((long long)c.max_pages * c.page_size, (long long)hspec::kMaxPositions);
 }
 
 }  // namespace
