@@ -433,7 +433,8 @@ size_t hspec_linear_workspace(hspec_dtype dtype, int M, int N, int K);
  *   attend:  every row attends to its request's positions up to its own
  *   verify:  the drafts that the target's logits let stand, and the next token
  * The arrays describing the batch are checked on the device: a row range outside [0, T], falling,
- * or longer than max_new is clamped and sets HSPEC_DEV_BAD_ROWS; a length below 0, or with the new
+ * or longer than max_new is clamped and sets HSPEC_DEV_BAD_ROWS (attention: a row of several ranges
+ * is the first request's); a length below 0, or with the new
  * tokens above the positions there are (max_pages * page_size, and max_len where it is given), is
  * clamped and sets HSPEC_DEV_BAD_CTX_LEN.  Data tensors are 16-byte aligned, else
  * HSPEC_ERR_UNSUPPORTED.  Outputs of append and attention are in the storage dtype (what the next

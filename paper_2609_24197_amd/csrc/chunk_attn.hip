@@ -426,7 +426,7 @@ chunk_attn_kernel(ChunkAttnArgs a) {
   };
   // the first item's unit, read beside the number of units (what it holds past them is not used)
   ChunkUnit u = a.units[min(place(cls, blockIdx.x / kChunkClasses) / a.Hkv, a.max_units - 1)];
-  const int n_units = min(a.status[1], a.max_units);
+  const int n_units = a.status[1];
   auto tickets = [&](int c) {   // of a class
     return C::ONCE ? (n_units - c + kChunkClasses - 1) / kChunkClasses * a.Hkv
                    : (n_units * a.Hkv - c + kChunkClasses - 1) / kChunkClasses;

@@ -3,8 +3,6 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
-#include <climits>
-
 #include "status.h"
 #include "target.h"
 #include "target_rows.h"
@@ -18,7 +16,8 @@ constexpr int PL_BUCKETS = 64;
 struct PlanLds {
   int first[PL_THREADS + 1];          // tiles before each request of the chunk
   int row0[PL_THREADS], n[PL_THREADS], L[PL_THREADS];
-  int wave_sum[PL_THREADS / 64];
+  int wave_sum[PL_THREADS / 64], wave_end[PL_THREADS / 64];
+  int end;                            // of the rows of the requests before the chunk
   unsigned long long keys;            // keys of all tiles
   int longest, slots, n_splits, bits;
   int hist[PL_BUCKETS];
@@ -54,14 +53,27 @@ __global__ void __launch_bounds__(PL_THREADS) chunk_plan(ChunkAttnArgs a) {
   }
   for (int i = tid; i < kChunkClasses * kChunkQueueStride; i += PL_THREADS) a.queue[i] = 0;
 
-  // Requests [c0, c0 + PL_THREADS): rows, lengths and tile counts into LDS.  Returns the chunk's tiles.
+  // Requests [c0, c0 + PL_THREADS): rows, lengths and tile counts into LDS.  Returns the chunk's tiles.  A request's rows
+  // begin behind those of every request before it, also where cu falls: no row is in two requests, so there are never
+  // more tiles than the workspace holds.
   auto load = [&](int c0) -> int {
     __syncthreads();
+    if (tid == 0 && c0 == 0) s.end = 0;
     const int b = c0 + tid;
+    const int from = b < a.B ? a.cu[b] : 0, to = b < a.B ? a.cu[b + 1] : 0, len = b < a.B ? a.ctx_lens[b] : 0;
+    int end = min(max(to, from), a.T);   // of the rows up to this request's
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) end = max(end, __shfl_up(end, o));   // (a lane without one gets its own)
+    if (lane == 63) s.wave_end[wave] = end;
+    const int before_me = __shfl_up(end, 1);
+    __syncthreads();
+    int start = max(s.end, lane ? before_me : 0);
+    for (int w = 0; w < wave; ++w) start = max(start, s.wave_end[w]);
     int nt = 0;
     if (b < a.B) {
-      const ChunkRows r = chunk_rows(a.cu, b, a.T, a.max_new);
-      const ChunkPos p = chunk_pos(a.ctx_lens[b], r.n, a.cap);
+      ChunkRows r = clamp_rows(max(from, start), max(to, start), a.T, a.max_new);
+      r.ok = r.ok && from >= start && to >= from && (b > 0 || from == 0);
+      const ChunkPos p = chunk_pos(len, r.n, a.cap);
       if (!r.ok || !p.ok) atomicOr(&s.bits, (r.ok ? 0 : ST_BAD_ROWS) | (p.ok ? 0 : ST_BAD_CTX_LEN));
       s.row0[tid] = r.row0;
       s.n[tid] = r.n;
@@ -79,7 +91,10 @@ __global__ void __launch_bounds__(PL_THREADS) chunk_plan(ChunkAttnArgs a) {
     int before = 0;
     for (int w = 0; w < wave; ++w) before += s.wave_sum[w];
     s.first[tid + 1] = before + v;
-    if (tid == 0) s.first[0] = 0;
+    if (tid == 0) {
+      s.first[0] = 0;
+      for (int w = 0; w < PL_THREADS / 64; ++w) s.end = max(s.end, s.wave_end[w]);
+    }
     __syncthreads();
     return s.first[PL_THREADS];
   };
@@ -161,25 +176,18 @@ __global__ void __launch_bounds__(PL_THREADS) chunk_plan(ChunkAttnArgs a) {
     int slot = -1;
     if (p > 1) {
       slot = atomicAdd(&s.slots, p);
-      const int e = atomicAdd(&s.n_splits, 1);
-      if (slot + p <= a.max_slots && e < a.max_splits)
-        a.splits[e] = ChunkSplit{b, x.tile, slot, p, row0, n, L, 0};
-      else   // (cu that divides the rows cannot need more than the workspace holds)
-        slot = INT_MIN;
+      a.splits[atomicAdd(&s.n_splits, 1)] = ChunkSplit{b, x.tile, slot, p, row0, n, L, 0};
     }
     for (int i = 0; i < p; ++i) {
-      const bool whole = slot == INT_MIN && i == 0;   // (then the other pieces are empty)
-      const int at0 = i * q, at1 = whole || i == p - 1 ? x.len : at0 + q;
-      const int at = atomicAdd(&s.hist[bucket(i == p - 1 ? x.len - at0 : q)], 1);
-      if (at >= a.max_units) continue;
-      if (slot == INT_MIN && !whole) a.units[at] = ChunkUnit{b, 0, 0, 0, -1, 0, 0, 0};
-      else a.units[at] = ChunkUnit{b, x.tile, x.k0 + at0, x.k0 + at1, slot < 0 ? -1 : slot + i, row0, n, L};
+      const int at0 = i * q, at1 = i == p - 1 ? x.len : at0 + q;
+      const int at = atomicAdd(&s.hist[bucket(at1 - at0)], 1);
+      a.units[at] = ChunkUnit{b, x.tile, x.k0 + at0, x.k0 + at1, slot < 0 ? -1 : slot + i, row0, n, L};
     }
   });
   __syncthreads();
   if (tid == 0) {
     a.status[0] = s.bits;
-    a.status[2] = min(s.n_splits, a.max_splits);
+    a.status[2] = s.n_splits;
     a.status[3] = 0;
   }
 }

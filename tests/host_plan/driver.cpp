@@ -1,7 +1,7 @@
-// Runs the chunk attention's plan kernel on the host over random batches, and checks what it
+// Runs the chunk attention's plan kernel on the host over random batches, divided well and badly, and checks what it
 // leaves: units and split tiles inside the workspace that the host reserves, every entry written, rows of no two
 // requests the same, every key of every tile of rows in exactly one unit.
-//   driver valid | longest
+//   driver valid | malformed | longest
 #include <hip/hip_runtime.h>
 
 #include <map>
@@ -135,6 +135,23 @@ int main(int argc, char** argv) {
       a.T = max(x.cu.back() + pick(r, 0, 3), 1);
       a.window = pick(r, 0, 2) ? 0 : pick(r, 1, longest);
       check(a, x, true, n);
+    }
+  } else if (mode == "malformed") {
+    for (; n < 150; ++n) {
+      ChunkAttnArgs a = heads(r);
+      if (n % 2) a.Hkv = 1, a.Hq = 8;   // few heads: the most slots a tile
+      a.B = pick(r, 2, n % 10 ? 60 : 300);
+      a.T = pick(r, 100, 600);
+      a.max_new = pick(r, 0, 1) ? a.T : pick(r, 1, a.T);
+      a.cap = pick(r, 100, 700);
+      Batch x;
+      const int kind = n % 3;   // up and down, any numbers, good but for one entry
+      for (int b = 0; b <= a.B; ++b)
+        x.cu.push_back(kind == 0 ? (b % 2 ? a.T : 0) : kind == 1 ? pick(r, -50, a.T + 50) : (int)((long long)a.T * b / a.B));
+      if (kind == 1 && pick(r, 0, 1)) x.cu[a.B / 2] = pick(r, 0, 1) ? INT_MAX : INT_MIN;
+      if (kind == 2) x.cu[pick(r, 0, a.B)] = a.T + 1;
+      for (int b = 0; b < a.B; ++b) x.lens.push_back(pick(r, 0, 9) ? pick(r, 0, a.cap) : (int)r());
+      check(a, x, false, n);
     }
   } else if (mode == "longest") {   // more keys in all than S can count in 32 bits
     for (int hkv : {1, 4}) {

@@ -22,7 +22,7 @@ def driver(tmp_path_factory):
     return out
 
 
-@pytest.mark.parametrize("mode", ["valid", "longest"])
+@pytest.mark.parametrize("mode", ["valid", "malformed", "longest"])
 def test_plans(driver, mode):
     r = subprocess.run([driver, mode], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, (r.returncode, r.stderr[-2000:])
