@@ -276,7 +276,8 @@ __device__ __forceinline__ bool chunk_unit(const ChunkAttnArgs& a, const ChunkUn
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, st[kb][i]);
     mx = half_max(mx) * a.scale_log2;
     if (__any(mx > m_run + CHUNK_SLACK)) {
-      const float m_new = fmaxf(m_run, mx);
+      // a row's own scores alone decide: rows that share the wave may see keys that it does not
+      const float m_new = mx > m_run + CHUNK_SLACK ? mx : m_run;
       const float alpha = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
       l_run *= alpha;
 #pragma unroll

@@ -28,3 +28,50 @@ def test_rows_claimed_by_many_requests_are_the_firsts(Hq, Hkv, dtype):
         o, ws = u.attend(y, ws=buf[:need])
         assert hspec.read_status(ws) & hspec.DEV_BAD_ROWS
         assert torch.equal(o, want) and (buf[need:] == 0xa5).all()
+
+
+def _at(x, b, pos):
+    return int(x["table"][b, pos // x["ps"]]), pos % x["ps"]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("ctx,new", [(300, 8), (60, 8), (0, 200), (20011, 5), (5000, 70)])
+def test_bits_of_a_row_do_not_depend_on_later_keys(ctx, new, dtype):
+    """A key with the largest score of all, or with an infinity, at the last token: the rows before it as they were."""
+    import torch
+    u = _u()
+    x = u.batch([ctx], [new], 16, 4, 128, dtype=dtype, seed=ctx + new)
+    want, _ = u.attend(x)
+    for what in (4.0, 100.0, 1e30, float("inf"), -float("inf")):
+        y = {**x, "k_cache": x["k_cache"].clone(), "v_cache": x["v_cache"].clone()}
+        slot = _at(x, 0, ctx + new - 1)
+        key = x["q"][new - 1, ::4]                                   # along the last token's first query of each group
+        y["k_cache"][slot] = key * what if abs(what) < 1e31 else what
+        o, _ = u.attend(y)
+        assert torch.equal(o[:new - 1], want[:new - 1]), what
+        y["v_cache"][slot] = float("nan")
+        o, _ = u.attend(y)
+        assert torch.equal(o[:new - 1], want[:new - 1]), what
+        assert torch.isnan(o[new - 1].float()).any(-1).all()
+
+
+@pytest.mark.parametrize("window", [0, 100])
+def test_bits_of_a_row_do_not_depend_on_its_neighbours(window):
+    """Each token of a chunk alone in turn has the largest key; every row that does not see it keeps its bits."""
+    import torch
+    u = _u()
+    ctx, new = 150, 33
+    x = u.batch([ctx], [new], 8, 2, 64, window=window, seed=3)
+    want, _ = u.attend(x)
+    for i in range(0, new, 4):
+        y = {**x, "k_cache": x["k_cache"].clone()}
+        y["k_cache"][_at(x, 0, ctx + i)] = 20 * x["q"][i, ::4]
+        o, _ = u.attend(y)
+        assert torch.equal(o[:i], want[:i]), i
+        if window:
+            for pos in (ctx + i - window, ctx + i - window - 20):    # out of the window of row i and those behind it
+                if pos >= 0:
+                    z = {**x, "k_cache": x["k_cache"].clone()}
+                    z["k_cache"][_at(x, 0, pos)] = 20 * x["q"][max(i - 5, 0), ::4]
+                    o, _ = u.attend(z)
+                    assert torch.equal(o[i:new], want[i:new]), (i, pos)
