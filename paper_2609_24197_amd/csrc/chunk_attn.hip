@@ -519,10 +519,9 @@ __device__ __forceinline__ void merge_store(const ChunkAttnArgs& a, const ChunkS
   if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(dst) = acc;
   else *reinterpret_cast<bf16x4*>(dst) = bf16x4{f2bf(acc[0]), f2bf(acc[1]), f2bf(acc[2]), f2bf(acc[3])};
 }
-// Weight of a piece: 0 where the row sees nothing of it.
-__device__ __forceinline__ float piece_weight(float2 ml, float m_use) {
-  return ml.x == -INFINITY && ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - m_use);
-}
+// (A piece that a row sees nothing of has m = -inf, l = 0 and O = 0; no piece is left out for its weight, so that a NaN
+// among the scores or values of one shows as it does where a cache is not split.)
+__device__ __forceinline__ float piece_weight(float m, float m_use) { return __builtin_amdgcn_exp2f(m - m_use); }
 
 template <class T, int D>
 __global__ void __launch_bounds__(MG_THREADS) chunk_merge_rows(ChunkAttnArgs a, int blocks) {
@@ -560,8 +559,8 @@ __global__ void __launch_bounds__(MG_THREADS) chunk_merge_rows(ChunkAttnArgs a, 
       }
 #pragma unroll
       for (int x = 0; x < U; ++x) {
-        const float f = i + x < s.pieces ? piece_weight(ml[x], m_use) : 0.f;
-        if (f == 0.f) continue;   // (an O of 0 x infinity stays out)
+        if (i + x >= s.pieces) continue;
+        const float f = piece_weight(ml[x].x, m_use);
         l += ml[x].y * f;
         acc += o[x] * f;
       }
@@ -604,8 +603,8 @@ __global__ void __launch_bounds__(MG_THREADS) chunk_merge_row(ChunkAttnArgs a, i
       float f = 0.f;
       if (c0 + tid < s.pieces) {
         const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (p0 + (c0 + tid) * step) * 2);
-        f = piece_weight(ml, m_use);
-        if (f != 0.f) l += ml.y * f;
+        f = piece_weight(ml.x, m_use);
+        l += ml.y * f;
       }
       s_w[tid] = f;
       __syncthreads();
@@ -617,8 +616,7 @@ __global__ void __launch_bounds__(MG_THREADS) chunk_merge_row(ChunkAttnArgs a, i
         }
 #pragma unroll
         for (int x = 0; x < U; ++x) {
-          const float v = i + x * G < top ? s_w[i + x * G] : 0.f;
-          if (v != 0.f) acc += o[x] * v;   // (an O of 0 x infinity stays out)
+          if (i + x * G < top) acc += o[x] * s_w[i + x * G];
         }
       }
     }

@@ -75,3 +75,51 @@ def test_bits_of_a_row_do_not_depend_on_its_neighbours(window):
                     z["k_cache"][_at(x, 0, pos)] = 20 * x["q"][max(i - 5, 0), ::4]
                     o, _ = u.attend(z)
                     assert torch.equal(o[i:new], want[i:new]), (i, pos)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,Hq,Hkv,ctx,new", [(1, 8, 2, 20011, 5), (24, 16, 4, 4000, 17), (1, 4, 4, 3000, 1)])
+def test_nan_in_whole_pieces_shows(B, Hq, Hkv, ctx, new, dtype):
+    """K of the first cached tokens is NaN, up to every length that a piece of a split cache can have."""
+    import torch
+    u = _u()
+    x = u.batch([ctx] * B, [new] * B, Hq, Hkv, 128, dtype=dtype, seed=B)
+    clean, _ = u.attend(x)
+    assert torch.isfinite(clean[:B * new]).all()
+    bad = B - 1
+    for end in range(32, 2048 + 1, 32):
+        ids = x["table"][bad, (end - 32) // 16:end // 16].long()
+        x["k_cache"][ids] = float("nan")
+        o, _ = u.attend(x)
+        assert torch.isnan(o[bad * new:B * new].float()).all(), end
+        assert torch.equal(o[:bad * new], clean[:bad * new])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Hq,Hkv,D", [(4, 4, 128), (8, 2, 64)])
+@pytest.mark.parametrize("ctx", [1280, 1281, 2048, 128 * 40])
+def test_nan_in_the_last_key_shows(ctx, Hq, Hkv, D, dtype):
+    """A last piece of one or two keys."""
+    import torch
+    u = _u()
+    x = u.batch([ctx], [1], Hq, Hkv, D, dtype=dtype, seed=ctx)
+    x["k_cache"][_at(x, 0, ctx)] = float("nan")
+    o, _ = u.attend(x)
+    assert torch.isnan(o[0].float()).all()
+
+
+@pytest.mark.parametrize("what", [float("nan"), float("inf")])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("ctx", [100, 5000])
+def test_values_of_no_weight_show(ctx, dtype, what):
+    """A key whose weight is below what 32 bits hold, with a V that is not finite: the row is not finite, whether its cache
+    is split or not."""
+    import torch
+    u = _u()
+    x = u.batch([ctx], [1], 4, 4, 64, dtype=dtype, seed=ctx)
+    ids = x["table"][0, :4].long()
+    q = x["q"][0].float()
+    x["k_cache"][ids] = (-100 * 8 * q / (q * q).sum(-1, keepdim=True)).to(x["q"].dtype)   # scores of -100, 64 keys
+    x["v_cache"][_at(x, 0, 5)] = what
+    o, _ = u.attend(x)
+    assert not torch.isfinite(o[0].float()).any()
