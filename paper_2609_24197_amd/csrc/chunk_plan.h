@@ -16,8 +16,8 @@ constexpr int PL_BUCKETS = 64;
 struct PlanLds {
   int first[PL_THREADS + 1];          // tiles before each request of the chunk
   int row0[PL_THREADS], n[PL_THREADS], L[PL_THREADS];
-  int wave_sum[PL_THREADS / 64], wave_end[PL_THREADS / 64];
-  int end;                            // of the rows of the requests before the chunk
+  int wave_sum[PL_THREADS / 64];
+  int end;                            // the largest of cu before the chunk, where its rows are bad
   unsigned long long keys;            // keys of all tiles
   int longest, slots, n_splits, bits;
   int hist[PL_BUCKETS];
@@ -53,48 +53,50 @@ __global__ void __launch_bounds__(PL_THREADS) chunk_plan(ChunkAttnArgs a) {
   }
   for (int i = tid; i < kChunkClasses * kChunkQueueStride; i += PL_THREADS) a.queue[i] = 0;
 
-  // Requests [c0, c0 + PL_THREADS): rows, lengths and tile counts into LDS.  Returns the chunk's tiles.  A request's rows
-  // begin behind those of every request before it, also where cu falls: no row is in two requests, so there are never
-  // more tiles than the workspace holds.
+  // Requests [c0, c0 + PL_THREADS): rows, lengths and tile counts into LDS.  Returns the chunk's tiles.  Once a request's
+  // rows are found bad, those of each begin behind all before it: no row is in two requests, so there are
+  // never more tiles than the workspace holds.
   auto load = [&](int c0) -> int {
     __syncthreads();
-    if (tid == 0 && c0 == 0) s.end = 0;
     const int b = c0 + tid;
     const int from = b < a.B ? a.cu[b] : 0, to = b < a.B ? a.cu[b + 1] : 0, len = b < a.B ? a.ctx_lens[b] : 0;
-    int end = min(max(to, from), a.T);   // of the rows up to this request's
+    int start = from, before = 0, v = 0;
+    for (bool again = false;; again = true) {
+      int nt = 0;
+      if (b < a.B) {
+        ChunkRows r = clamp_rows(start, max(to, start), a.T, a.max_new);
+        r.ok = r.ok && start == from && to >= from && (b > 0 || from == 0);
+        const ChunkPos p = chunk_pos(len, r.n, a.cap);
+        if (!r.ok || !p.ok) atomicOr(&s.bits, (r.ok ? 0 : ST_BAD_ROWS) | (p.ok ? 0 : ST_BAD_CTX_LEN));
+        s.row0[tid] = r.row0;
+        s.n[tid] = r.n;
+        s.L[tid] = p.L;
+        nt = (int)(((long long)r.n * g + a.tile_rows - 1) / a.tile_rows);
+      }
+      v = nt;
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) end = max(end, __shfl_up(end, o));   // (a lane without one gets its own)
-    if (lane == 63) s.wave_end[wave] = end;
-    const int before_me = __shfl_up(end, 1);
-    __syncthreads();
-    int start = max(s.end, lane ? before_me : 0);
-    for (int w = 0; w < wave; ++w) start = max(start, s.wave_end[w]);
-    int nt = 0;
-    if (b < a.B) {
-      ChunkRows r = clamp_rows(max(from, start), max(to, start), a.T, a.max_new);
-      r.ok = r.ok && from >= start && to >= from && (b > 0 || from == 0);
-      const ChunkPos p = chunk_pos(len, r.n, a.cap);
-      if (!r.ok || !p.ok) atomicOr(&s.bits, (r.ok ? 0 : ST_BAD_ROWS) | (p.ok ? 0 : ST_BAD_CTX_LEN));
-      s.row0[tid] = r.row0;
-      s.n[tid] = r.n;
-      s.L[tid] = p.L;
-      nt = (int)(((long long)r.n * g + a.tile_rows - 1) / a.tile_rows);
+      for (int o = 1; o < 64; o <<= 1) {
+        const int w = __shfl_up(v, o);
+        if (lane >= o) v += w;
+      }
+      if (lane == 63) s.wave_sum[wave] = v;
+      if (tid == 0) s.end = 0;
+      __syncthreads();
+      before = 0;
+      for (int w = 0; w < wave; ++w) before += s.wave_sum[w];
+      if (again || !(s.bits & ST_BAD_ROWS)) break;   // (uniform)
+      // the largest of cu up to this request
+      int top = 0;
+      for (int i = tid; i <= c0; i += PL_THREADS) top = max(top, a.cu[i]);
+      atomicMax(&s.end, top);
+      s.first[tid] = from;
+      __syncthreads();
+      start = s.end;
+      for (int i = 0; i <= tid; ++i) start = max(start, s.first[i]);
+      __syncthreads();
     }
-    int v = nt;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int w = __shfl_up(v, o);
-      if (lane >= o) v += w;
-    }
-    if (lane == 63) s.wave_sum[wave] = v;
-    __syncthreads();
-    int before = 0;
-    for (int w = 0; w < wave; ++w) before += s.wave_sum[w];
     s.first[tid + 1] = before + v;
-    if (tid == 0) {
-      s.first[0] = 0;
-      for (int w = 0; w < PL_THREADS / 64; ++w) s.end = max(s.end, s.wave_end[w]);
-    }
+    if (tid == 0) s.first[0] = 0;
     __syncthreads();
     return s.first[PL_THREADS];
   };
