@@ -507,7 +507,7 @@ size_t hspec_chunk_attn_workspace(const hspec_chunk_cfg* cfg, int max_len);
  * -inf set HSPEC_DEV_NONFINITE (rows up to a are looked at); a draft id outside [0, draft_vocab)
  * or a mapped id out of range does not stand (or counts as -1) and sets HSPEC_DEV_BAD_TOKEN;
  * HSPEC_DEV_BAD_ROWS as above, with max_new = k + 1.  B <= 32767, k <= 4096, B (k+1) and rows <= 2^22,
- * draft_vocab <= vocab <= 2^19.
+ * draft_vocab <= vocab <= 2^19; temperatures that the call uses are finite and above 0 (and 1.5 / T is finite).
  */
 typedef struct {
   int B, k, rows, vocab, draft_vocab;

@@ -185,6 +185,9 @@ static hspec_status check_verify(const hspec_verify_cfg* c) {
   return HSPEC_OK;
 }
 
+// log2(e) / T is positive and finite.
+static bool temperature_ok(float t) { return t > 0.f && std::isfinite(t) && std::isfinite((float)(1.5 / t)); }
+
 static void plan_verify(Arena& ar, const hspec_verify_cfg& c, hspec::VerifyArgs& a) {
   a.B = c.B; a.k = c.k; a.rows = c.rows; a.V = c.vocab; a.Vd = c.draft_vocab; a.f32 = c.dtype == HSPEC_F32;
   hspec::verify_bounds(a);
@@ -219,10 +222,10 @@ HSPEC_API hspec_status hspec_verify(const hspec_verify_cfg* cfg, const void* tar
   if (!u != !gumbel) return fail(HSPEC_ERR_NULL, "sampling needs both u and gumbel, greedy verification neither");
   if (!u && draft_logits) return fail(HSPEC_ERR_UNSUPPORTED, "greedy verification takes no draft logits");
   if (draft_logits && !d2t != !t2d) return fail(HSPEC_ERR_NULL, "draft logits need both vocabulary maps or neither");
-  if (u && !(cfg->temperature > 0.f && std::isfinite((float)(1.5 / cfg->temperature))))
-    return fail(HSPEC_ERR_SHAPE, "sampling needs temperature > 0");
-  if (draft_logits && !(cfg->draft_temperature > 0.f && std::isfinite((float)(1.5 / cfg->draft_temperature))))
-    return fail(HSPEC_ERR_SHAPE, "draft logits need draft_temperature > 0");
+  if (u && !temperature_ok(cfg->temperature))
+    return fail(HSPEC_ERR_SHAPE, "sampling needs a finite temperature > 0");
+  if (draft_logits && !temperature_ok(cfg->draft_temperature))
+    return fail(HSPEC_ERR_SHAPE, "draft logits need a finite draft_temperature > 0");
   if (!cu_rows && cfg->rows != (long long)cfg->B * (cfg->k + 1))
     return fail(HSPEC_ERR_SHAPE, "without cu_rows, rows must be B * (k + 1)");
   if (hspec_status s = check_ws(workspace, ws_bytes, hspec_verify_workspace(cfg))) return s;
