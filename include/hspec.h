@@ -434,11 +434,11 @@ size_t hspec_linear_workspace(hspec_dtype dtype, int M, int N, int K);
  *   verify:  the drafts that the target's logits let stand, and the next token
  * The arrays describing the batch are checked on the device: a row range outside [0, T], falling,
  * or longer than max_new is clamped and sets HSPEC_DEV_BAD_ROWS (attention: a row of several ranges
- * is the first request's); a length below 0, or with the new
- * tokens above the positions there are (max_pages * page_size, and max_len where it is given), is
- * clamped and sets HSPEC_DEV_BAD_CTX_LEN.  Data tensors are 16-byte aligned, else
- * HSPEC_ERR_UNSUPPORTED.  Outputs of append and attention are in the storage dtype (what the next
- * projection and the cache take), unlike those of the drafting calls.
+ * is the first request's); a length below 0, or with the new tokens above the positions there are
+ * (max_pages * page_size, and max_len where it is given), is clamped and sets HSPEC_DEV_BAD_CTX_LEN.
+ * Data tensors are 16-byte aligned, and outputs and the workspace lie over nothing else that the
+ * call is given, else HSPEC_ERR_UNSUPPORTED.  Outputs of append and attention are in the storage
+ * dtype (what the next projection and the cache take), unlike those of the drafting calls.
  *
  *   B requests (at most 32767), T rows, max_new: host upper bound of one request's new tokens, Hq
  *   query and Hkv KV heads (query head q reads KV head q / (Hq/Hkv)), D head dim (64 or 128),
@@ -461,8 +461,7 @@ typedef struct {
  * with rotate-half pairing at the row's position (no norm where q_norm_w and k_norm_w [D] are
  * both NULL).  q [T, Hq, D] out; k and v are written at slot(position) of k_cache and v_cache, in
  * place.  A position whose page id is outside the pool sets HSPEC_DEV_BAD_PAGE and is not written.
- * Which of two rows stays is undefined where a page is mapped for both.  q must not lie over qkv
- * (HSPEC_ERR_UNSUPPORTED).
+ * Which of two rows stays is undefined where a page is mapped for both.
  */
 hspec_status hspec_chunk_append(const hspec_chunk_cfg* cfg, hspec_dtype qkv_dtype, const void* qkv,
                                 const float* q_norm_w, const float* k_norm_w, const int32_t* cu_new,
@@ -476,8 +475,7 @@ size_t hspec_chunk_append_workspace(const hspec_chunk_cfg* cfg);
  * host upper bound of ctx_lens[b] + new tokens of b (bounds the split of long caches).  A slot that
  * a row does not see never changes it, whatever it holds (NaN and infinities included); pages
  * outside the pool read as zeros and set HSPEC_DEV_BAD_PAGE; a row that sees no position is zero.
- * Results are bitwise reproducible and independent of where pages live.  o must not lie over q
- * (HSPEC_ERR_UNSUPPORTED).
+ * Results are bitwise reproducible and independent of where pages live.
  */
 hspec_status hspec_chunk_attn(const hspec_chunk_cfg* cfg, const void* q, const int32_t* cu_new, const void* k_cache,
                               const void* v_cache, const int32_t* page_table, const int32_t* ctx_lens, int max_len,
@@ -502,7 +500,6 @@ size_t hspec_chunk_attn_workspace(const hspec_chunk_cfg* cfg, int max_len);
  * Greedy (u and gumbel NULL, draft_logits NULL): draft j stands while it is the argmax of row j;
  *   next = argmax of row a.  A tie goes to the lowest id.
  * tokens [B, k+1] int32: the a drafts that stand (target ids), next, then -1; n_accepted [B] = a.
- * tokens must not lie over draft_tokens (HSPEC_ERR_UNSUPPORTED).
  * NaN logits count as -inf and +inf as the largest float; they, a NaN of gumbel and a row of nothing but
  * -inf set HSPEC_DEV_NONFINITE (rows up to a are looked at); a draft id outside [0, draft_vocab)
  * or a mapped id out of range does not stand (or counts as -1) and sets HSPEC_DEV_BAD_TOKEN;

@@ -55,10 +55,28 @@ hspec_status check_aligned(std::initializer_list<const void*> ptrs) {
   return HSPEC_OK;
 }
 
-// What is written must not lie over what is read meanwhile.
-hspec_status check_apart(const void* x, size_t nx, const void* y, size_t ny) {
-  const uintptr_t a = (uintptr_t)x, b = (uintptr_t)y;
-  if (a < b + ny && b < a + nx) return fail(HSPEC_ERR_UNSUPPORTED, "an output lies over an input");
+// Memory of an argument; an extent past what can be addressed counts as 2^62 bytes.
+struct Span {
+  const void* p;
+  size_t n;
+};
+Span span(const void* p, std::initializer_list<size_t> dims) {
+  unsigned __int128 n = 1;
+  for (size_t d : dims) n = std::min(n * d, (unsigned __int128)1 << 62);
+  return Span{p, (size_t)n};
+}
+// What a call writes must lie over nothing else that it is given.
+hspec_status check_apart(std::initializer_list<Span> outs, std::initializer_list<Span> ins) {
+  auto over = [](const Span& x, const Span& y) {
+    const uintptr_t a = (uintptr_t)x.p, b = (uintptr_t)y.p;
+    return a && b && (a < b ? b - a < x.n : a - b < y.n);
+  };
+  for (const Span* x = outs.begin(); x != outs.end(); ++x) {
+    bool bad = false;
+    for (const Span& y : ins) bad |= over(*x, y);
+    for (const Span* y = x + 1; y != outs.end(); ++y) bad |= over(*x, *y);
+    if (bad) return fail(HSPEC_ERR_UNSUPPORTED, "an output or the workspace lies over another argument");
+  }
   return HSPEC_OK;
 }
 size_t size_of(hspec_dtype d) { return d == HSPEC_F32 ? 4 : 2; }
@@ -83,6 +101,14 @@ hspec_status check_chunk(const hspec_chunk_cfg* c) {
   return HSPEC_OK;
 }
 
+Span cache_span(const hspec_chunk_cfg& c, const void* p) {
+  return span(p, {(size_t)c.num_pages, (size_t)c.page_size, (size_t)c.Hkv, (size_t)c.D, size_of(c.dtype)});
+}
+Span rows_span(const hspec_chunk_cfg& c, const void* p) {
+  return span(p, {(size_t)c.T, (size_t)c.Hq, (size_t)c.D, size_of(c.dtype)});
+}
+Span ints_span(const void* p, size_t n, size_t m = 1) { return span(p, {n, m, 4}); }
+
 int positions(const hspec_chunk_cfg& c) {
   return (int)std::min((long long)c.max_pages * c.page_size, (long long)hspec::kMaxPositions);
 }
@@ -105,11 +131,14 @@ HSPEC_API hspec_status hspec_chunk_append(const hspec_chunk_cfg* cfg, hspec_dtyp
   if (!q_norm_w != !k_norm_w) return fail(HSPEC_ERR_NULL, "only one of q_norm_w and k_norm_w is NULL");
   if (!(cfg->rope_theta > 0.)) return fail(HSPEC_ERR_SHAPE, "rope_theta must be positive");
   if (hspec_status s = check_aligned({qkv, q, k_cache, v_cache})) return s;
-  if (hspec_status s = check_apart(qkv, (size_t)cfg->T * (cfg->Hq + 2 * cfg->Hkv) * cfg->D * size_of(qkv_dtype), q,
-                                   (size_t)cfg->T * cfg->Hq * cfg->D * size_of(cfg->dtype)))
-    return s;
-  if (hspec_status s = check_ws(workspace, ws_bytes, hspec_chunk_append_workspace(cfg))) return s;
+  const size_t need = hspec_chunk_append_workspace(cfg);
+  if (hspec_status s = check_ws(workspace, ws_bytes, need)) return s;
   const hspec_chunk_cfg& c = *cfg;
+  if (hspec_status s = check_apart({rows_span(c, q), cache_span(c, k_cache), cache_span(c, v_cache), Span{workspace, need}},
+                                   {span(qkv, {(size_t)c.T, (size_t)(c.Hq + 2 * c.Hkv), (size_t)c.D, size_of(qkv_dtype)}),
+                                    ints_span(q_norm_w, c.D), ints_span(k_norm_w, c.D), ints_span(cu_new, c.B + 1),
+                                    ints_span(ctx_lens, c.B), ints_span(page_table, c.B, c.max_pages)}))
+    return s;
   hspec::ChunkAppendArgs a;
   a.qkv = qkv; a.q = q; a.k_cache = k_cache; a.v_cache = v_cache; a.qw = q_norm_w; a.kw = k_norm_w;
   a.cu = cu_new; a.ctx_lens = ctx_lens; a.page_table = page_table;
@@ -158,9 +187,13 @@ HSPEC_API hspec_status hspec_chunk_attn(const hspec_chunk_cfg* cfg, const void* 
   if (!q || !cu_new || !k_cache || !v_cache || !page_table || !ctx_lens || !o)
     return fail(HSPEC_ERR_NULL, "an input or output pointer is NULL");
   if (hspec_status s = check_aligned({q, k_cache, v_cache, o})) return s;
-  const size_t rows = (size_t)cfg->T * cfg->Hq * cfg->D * size_of(cfg->dtype);
-  if (hspec_status s = check_apart(q, rows, o, rows)) return s;
-  if (hspec_status s = check_ws(workspace, ws_bytes, hspec_chunk_attn_workspace(cfg, max_len))) return s;
+  const size_t need = hspec_chunk_attn_workspace(cfg, max_len);
+  if (hspec_status s = check_ws(workspace, ws_bytes, need)) return s;
+  if (hspec_status s = check_apart({rows_span(*cfg, o), Span{workspace, need}},
+                                   {rows_span(*cfg, q), cache_span(*cfg, k_cache), cache_span(*cfg, v_cache),
+                                    ints_span(cu_new, cfg->B + 1), ints_span(ctx_lens, cfg->B),
+                                    ints_span(page_table, cfg->B, cfg->max_pages)}))
+    return s;
   Arena ar{(char*)workspace};
   hspec::ChunkAttnArgs a;
   plan_chunk_attn(ar, *cfg, max_len, a);
@@ -228,9 +261,13 @@ HSPEC_API hspec_status hspec_verify(const hspec_verify_cfg* cfg, const void* tar
     return fail(HSPEC_ERR_SHAPE, "draft logits need a finite draft_temperature > 0");
   if (!cu_rows && cfg->rows != (long long)cfg->B * (cfg->k + 1))
     return fail(HSPEC_ERR_SHAPE, "without cu_rows, rows must be B * (k + 1)");
-  if (hspec_status s = check_ws(workspace, ws_bytes, hspec_verify_workspace(cfg))) return s;
-  const size_t drafts = (size_t)cfg->B * cfg->k * 4;
-  if (hspec_status s = check_apart(draft_tokens, drafts, tokens, drafts + (size_t)cfg->B * 4)) return s;
+  const size_t need = hspec_verify_workspace(cfg), B = cfg->B, k = cfg->k, V = cfg->vocab, Vd = cfg->draft_vocab;
+  if (hspec_status s = check_ws(workspace, ws_bytes, need)) return s;
+  if (hspec_status s = check_apart({ints_span(tokens, B, k + 1), ints_span(n_accepted, B), Span{workspace, need}},
+                                   {span(target_logits, {(size_t)cfg->rows, V, size_of(cfg->dtype)}),
+                                    span(draft_logits, {B, k, Vd, 4}), ints_span(draft_tokens, B, k), ints_span(cu_rows, B + 1),
+                                    ints_span(d2t, Vd), ints_span(t2d, V), ints_span(u, B, k), ints_span(gumbel, B, V)}))
+    return s;
   Arena ar{(char*)workspace};
   hspec::VerifyArgs a;
   plan_verify(ar, *cfg, a);
