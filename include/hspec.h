@@ -494,7 +494,8 @@ size_t hspec_chunk_attn_workspace(const hspec_chunk_cfg* cfg, int max_len);
  *   p_j = softmax(target row j / temperature); q_j = softmax(draft_logits[b, j] /
  *   draft_temperature) (draft_logits [B, k, draft_vocab] fp32 as hspec_draft_head writes them), or
  *   all on the drafted token with draft_logits NULL (a greedy drafter);
- *   draft j stands if u[b, j] q_j(t_j) < p_j(t_j); a = the first that does not, or n;
+ *   draft j stands if u[b, j] q_j(t_j) < p_j(t_j) (a probability below 2^-1074 is 0); a = the first
+ *   that does not, or n;
  *   next = argmax_v log max(p_a(v) - q_a(v), 0) + gumbel[b, v], q = 0 for a = n (p_a alone where no
  *   difference is positive).
  * Greedy (u and gumbel NULL, draft_logits NULL): draft j stands while it is the argmax of row j;

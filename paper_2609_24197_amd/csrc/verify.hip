@@ -30,6 +30,7 @@ constexpr int ST_BAD_TOKEN = 4;
 constexpr int ST_NONFINITE = 8;
 constexpr int VF_PIECE = kVerifyPiece;
 constexpr int VF_GRID = 16384;    // (90 us at 64 x 16 x 131072 with 4096, 76 with 8192, then 74)
+constexpr float VF_LOWEST = -1074.f;   // log2 of the least probability that is not 0, as 64 bits have it
 constexpr float LN2 = 0.6931471805599453f;
 
 // A logit as the definition wants it: NaN counts as -inf and +inf as the largest float; both flag.
@@ -282,12 +283,15 @@ __device__ __forceinline__ void decide(const VerifyArgs& a, int b, int j, const 
     const float y = has_q && t >= 0 ? a.draft[dr * a.Vd + d] : 0.f;
     const float u = j < drafts ? a.u[dr] : 0.f;
     r.p = join_pieces(a.stat_t + row * a.pieces_t, a.pieces_t, a.c_t, flag);
-    float q = 1.f;
+    float lq = 0.f;
     if (has_q) {
       r.q = join_pieces(a.stat_d + dr * a.pieces_d, a.pieces_d, a.c_d, flag);
-      q = __builtin_amdgcn_exp2f(log_prob(clean(y, ignore), r.q, a.c_d));
+      lq = log_prob(clean(y, ignore), r.q, a.c_d);
     }
-    stands = t >= 0 && u * q < __builtin_amdgcn_exp2f(log_prob(clean(x, ignore), r.p, a.c_t));
+    // u q < p by their logarithms, since 32 bits hold neither below 2^-126; below VF_LOWEST they count as 0
+    const float lp = log_prob(clean(x, ignore), r.p, a.c_t);
+    const float e = __builtin_amdgcn_exp2f((lq - lp) * 0.5f);   // (two factors, so that a small u meets no infinity first)
+    stands = t >= 0 && lp >= VF_LOWEST && (u == 0.f || lq < VF_LOWEST || u * e * e < 1.f);
   }
   r.flags = (flag ? ST_NONFINITE : 0) | (j < drafts && t < 0 ? ST_BAD_TOKEN : 0);
   if (lane == 0) {
