@@ -130,6 +130,10 @@ struct VerifyRow {
   int flags, top;
 };
 constexpr int kVerifyLine = 32;   // ints between counters: a 128-byte line each, so that they are not one line's traffic
+// 64-bit words of a request's pieces of the choice, two each, in whole lines.
+__host__ __device__ constexpr int verify_key_stride(int pieces_r) {
+  return (2 * pieces_r + kVerifyLine / 2 - 1) / (kVerifyLine / 2) * (kVerifyLine / 2);
+}
 struct VerifyArgs {
   const void* target = nullptr;       // [rows, V]
   const float* draft = nullptr;       // [B, k, Vd] or null
@@ -147,7 +151,7 @@ struct VerifyArgs {
   int* n = nullptr;                       // [B][kVerifyLine] first draft found not to stand
   int2* req = nullptr;                    // [B] first row, drafts
   int* done = nullptr;                    // [B][kVerifyLine] workgroups of the choice that are done
-  unsigned long long* keys = nullptr;     // [B][kVerifyLine / 2] best (score, token), and the best in doubt
+  unsigned long long* keys = nullptr;     // [B][verify_key_stride] of each piece of the choice: best (score, token), bounds
   int pieces_t = 0, pieces_d = 0, pieces_r = 0;
 };
 constexpr int kVerifyPiece = 32768;   // bytes of a row that a workgroup takes at a time, all its loads under way together

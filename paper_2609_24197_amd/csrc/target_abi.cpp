@@ -226,7 +226,7 @@ static void plan_verify(Arena& ar, const hspec_verify_cfg& c, hspec::VerifyArgs&
   hspec::verify_bounds(a);
   a.status = ar.take<int>(64);
   const size_t rows = (size_t)c.B * (c.k + 1);
-  a.keys = ar.take<unsigned long long>((size_t)c.B * hspec::kVerifyLine / 2);
+  a.keys = ar.take<unsigned long long>((size_t)c.B * hspec::verify_key_stride(a.pieces_r));
   a.stat_t = ar.take<unsigned long long>((size_t)c.rows * a.pieces_t);
   a.stat_d = ar.take<unsigned long long>((size_t)c.B * c.k * a.pieces_d);
   a.row = ar.take<hspec::VerifyRow>(rows);

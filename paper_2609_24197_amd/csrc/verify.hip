@@ -31,6 +31,7 @@ constexpr int ST_NONFINITE = 8;
 constexpr int VF_PIECE = kVerifyPiece;
 constexpr int VF_GRID = 16384;    // (90 us at 64 x 16 x 131072 with 4096, 76 with 8192, then 74)
 constexpr float VF_LOWEST = -1074.f;   // log2 of the least probability that is not 0, as 64 bits have it
+constexpr float VF_ERR = 1.25f * 0x1p-23f, VF_ERR0 = 20.f * 0x1p-23f;   // see verify_pick
 constexpr float LN2 = 0.6931471805599453f;
 
 // A logit as the definition wants it: NaN counts as -inf and +inf as the largest float; both flag.
@@ -207,7 +208,6 @@ __global__ void verify_init(VerifyArgs a) {
     a.n[i * kVerifyLine] = r.n - 1;   // (-1: no rows)
     a.req[i] = int2{r.row0, r.n - 1};
     a.done[i * kVerifyLine] = 0;
-    a.keys[i * kVerifyLine / 2] = a.keys[i * kVerifyLine / 2 + 1] = 0;
   }
 }
 
@@ -374,12 +374,56 @@ __device__ __forceinline__ void load_n(const V* p, V (&v)[N]) {
   }
 }
 
+// The best of some tokens: its score and token as a key (0: none), the most that its score can be without the
+// roundings of 32 bits, and the most that any other's can be.
+struct Pick {
+  unsigned long long key;
+  float hi, rival;
+  __device__ __forceinline__ void join(unsigned long long k2, float h2, float r2) {
+    rival = fmaxf(fmaxf(rival, r2), k2 > key ? hi : h2);
+    hi = k2 > key ? h2 : hi;
+    key = k2 > key ? k2 : key;
+  }
+  // Over the wave: neighbours, then pairs, quads, halves and rows of 16 lanes by moves between registers.
+  template <int CTRL>
+  __device__ __forceinline__ void join_dpp() {
+    auto far = [](unsigned v) { return (unsigned)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xf, 0xf, true); };
+    const unsigned long long k = ((unsigned long long)far((unsigned)(key >> 32)) << 32) | far((unsigned)key);
+    const float h = __uint_as_float(far(__float_as_uint(hi))), r = __uint_as_float(far(__float_as_uint(rival)));
+    join(k, h, r);
+  }
+  template <class SWAP>
+  __device__ __forceinline__ void join_rows(SWAP swap) {
+    const auto kh = swap((unsigned)(key >> 32)), kl = swap((unsigned)key), h = swap(__float_as_uint(hi)), r = swap(__float_as_uint(rival));
+    *this = Pick{((unsigned long long)kh[0] << 32) | kl[0], __uint_as_float(h[0]), __uint_as_float(r[0])};
+    join(((unsigned long long)kh[1] << 32) | kl[1], __uint_as_float(h[1]), __uint_as_float(r[1]));
+  }
+  __device__ __forceinline__ void join_wave() {
+    join_dpp<0xb1>();    // lane ^ 1
+    join_dpp<0x4e>();    // lane ^ 2
+    join_dpp<0x141>();   // 7 - lane of 8
+    join_dpp<0x140>();   // 15 - lane of 16
+    join_rows([](unsigned v) { return __builtin_amdgcn_permlane16_swap(v, v, false, false); });
+    join_rows([](unsigned v) { return __builtin_amdgcn_permlane32_swap(v, v, false, false); });
+  }
+  // Whether another token's score could reach this one's.  With ln(d + e) - ln d below 0.4, ln(d - e) lies above
+  // ln d - 2 (ln(d + e) - ln d).
+  __device__ __forceinline__ bool doubtful() const {
+    if (!key) return true;
+    const unsigned u = (unsigned)(key >> 32);
+    const float best = __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u), up = hi - best;
+    const float lo = best == INFINITY ? best : up < 0.4f ? best - 2.f * up : -INFINITY;
+    return rival > -INFINITY && rival >= lo;
+  }
+};
+
 // One workgroup per (request, piece of the vocabulary); greedy takes one piece and needs no row.
 template <class T, bool GREEDY>
 __global__ void __launch_bounds__(VF_THREADS) verify_pick(VerifyArgs a) {
   __shared__ int s_flags, s_last;
   __shared__ unsigned long long s_key[VF_THREADS / 64];
   __shared__ int s_who[VF_THREADS / 64];
+  __shared__ Pick s_pick[VF_THREADS / 64];
   const int b = blockIdx.x / a.pieces_r, piece = blockIdx.x % a.pieces_r;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const ChunkRows cr = request_rows(a, b);
@@ -423,10 +467,12 @@ __global__ void __launch_bounds__(VF_THREADS) verify_pick(VerifyArgs a) {
       const int d = a.t2d ? a.t2d[v] : v < a.Vd ? v : -1;
       return d < a.Vd ? max(d, -1) : -1;
     };
-    // The thread's best (score, token), and the most that a token could score whose p and q agree in their first ten
-    // bits, so that little of their difference is left in 32.
-    float best = -INFINITY, doubt = -INFINITY;
+    // log2 of p is off by at most 2^-24 of (l - m) / T for the difference, for the scale and for the result, and what
+    // the sum's logarithm is off by, so p by VF_ERR |log2 p| + VF_ERR0 of itself, the rounding of the score included.
+    // log2(p - q) = log2 p + log2(1 - r), r = q / p, which holds where 32 bits hold neither p nor q.
+    float best = -INFINITY;
     int at = -1;
+    Pick pick{0, -INFINITY, -INFINITY};
     const int2 e = piece_range(a.V, a.pieces_r, piece);
     each_piece(row, e.x, e.y, [&](int v0, const float* x, auto cnt) {
       constexpr int N = decltype(cnt)::value;
@@ -450,56 +496,53 @@ __global__ void __launch_bounds__(VF_THREADS) verify_pick(VerifyArgs a) {
         bool ignore = false;
         float lp = __builtin_fmaf(x[i] - rn.p.m, a.c_t, -rn.p.log_s);
         if (careful) lp = log_prob(clean(x[i], ignore), rn.p, a.c_t);
-        float lg = lp;
+        const float err = __builtin_fmaf(fabsf(lp), VF_ERR, VF_ERR0);
+        float lg = lp, up = lp;
         if (drow) {
           float lq = __builtin_fmaf(y[i] - rn.q.m, a.c_d, -rn.q.log_s);
           if (careful) lq = log_prob(clean(y[i], ignore), rn.q, a.c_d);
-          const float p = __builtin_amdgcn_exp2f(lp), q = __builtin_amdgcn_exp2f(lq);
           // (of a difference below 0 the logarithm is NaN, which no comparison lets through)
-          if (q > 0.f) {
-            lg = __builtin_amdgcn_logf(p - q);
-            if (fabsf(p - q) < 0x1p-10f * p) doubt = fmaxf(doubt, __builtin_fmaf(lp - 10.f, LN2, gn[i]));
-          }
+          const float r = __builtin_amdgcn_exp2f(lq - lp), d1 = 1.f - r;
+          lg += __builtin_amdgcn_logf(d1);
+          up += __builtin_amdgcn_logf(__builtin_fmaf(1.f + r, err, d1));
         }
         const float sc = __builtin_fmaf(lg, LN2, gn[i]);
+        const float hi = v0 + i == hot ? -INFINITY : __builtin_fmaf(up, LN2, gn[i]) + err;
         bad_noise |= !(gn[i] == gn[i]);
         const bool better = sc > best && v0 + i != hot;
+        pick.rival = fmaxf(pick.rival, better ? pick.hi : hi);
+        pick.hi = better ? hi : pick.hi;
         best = better ? sc : best;
         at = better ? v0 + i : at;
       }
     });
-    auto all_best = [&](unsigned long long k) {   // the largest of the workgroup, in every thread
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) {
-        const unsigned long long v = ((unsigned long long)__shfl_xor((unsigned)(k >> 32), o) << 32) | __shfl_xor((unsigned)k, o);
-        k = v > k ? v : k;
-      }
-      __syncthreads();
-      if (lane == 0) s_key[wave] = k;
-      __syncthreads();
-      k = s_key[0];
-#pragma unroll
-      for (int w = 1; w < VF_THREADS / 64; ++w) k = s_key[w] > k ? s_key[w] : k;
-      return k;
-    };
-    const unsigned long long mine =
-        all_best(at < 0 ? 0ull : ((unsigned long long)score_ord(best + 0.f) << 32) | ~(unsigned)at);
-    const unsigned long long most = all_best((unsigned long long)score_ord(doubt) << 32);
+    if (at >= 0) pick.key = ((unsigned long long)score_ord(best + 0.f) << 32) | ~(unsigned)at;
+    pick.join_wave();
     const int f = (__any(bad_noise) ? ST_NONFINITE : 0) | (__any(bad_map) ? ST_BAD_TOKEN : 0);
     if (f && lane == 0) set_status(a.status, f);
-    unsigned long long* keys = a.keys + b * kVerifyLine / 2;
+    if (lane == 0) s_pick[wave] = pick;
+    __syncthreads();
+    unsigned long long* keys = a.keys + (size_t)b * verify_key_stride(a.pieces_r);
     if (tid == 0) {
-      if (mine) __hip_atomic_fetch_max(keys, mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      __hip_atomic_fetch_max(keys + 1, most, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      wait_vmcnt<0>();   // done before the counter is raised
+#pragma unroll
+      for (int w = 1; w < VF_THREADS / 64; ++w) pick.join(s_pick[w].key, s_pick[w].hi, s_pick[w].rival);
+      publish(keys + 2 * piece, pick.key);
+      publish(keys + 2 * piece + 1, ((unsigned long long)__float_as_uint(pick.hi) << 32) | __float_as_uint(pick.rival));
       s_last = atomicAdd(a.done + b * kVerifyLine, 1) == a.pieces_r - 1;
     }
     __syncthreads();
     if (!s_last) return;
-    const unsigned long long top = fetch(keys);
-    if (drow && (!top || fetch(keys + 1) >> 32 >= top >> 32)) {
-      // Rare: the difference that decides is below what 32 bits hold of p and q.  The row once more in 64 (0.85 ms at
-      // 131072 tokens).
+    pick = Pick{0, -INFINITY, -INFINITY};
+    if (lane < a.pieces_r) {   // (at most 64)
+      const unsigned long long v = fetch(keys + 2 * lane + 1);
+      pick = Pick{fetch(keys + 2 * lane), __uint_as_float((unsigned)(v >> 32)), __uint_as_float((unsigned)v)};
+    }
+    pick.join_wave();
+    if (!pick.doubtful()) {
+      next = key_token(pick.key);
+    } else {
+      // Rare: scores that lie closer together than 32 bits tell (about 10^-5 of the choices), or no positive difference.
+      // The row once more in 64 (0.46 ms at 131072 tokens and 32000 of the drafter's).
       auto sum_of = [&](auto value, int count, double m, double c) {
         double t = 0.;
         for (int v = tid; v < count; v += VF_THREADS) t += exp2((value(v) - m) * c);
@@ -516,16 +559,18 @@ __global__ void __launch_bounds__(VF_THREADS) verify_pick(VerifyArgs a) {
       bool ignore = false;
       auto target = [&](int v) { return (double)clean(to_f32(row[v]), ignore); };
       auto draft = [&](int d) { return (double)clean(drow[d], ignore); };
-      const double sp = sum_of(target, a.V, rn.p.m, a.c64_t), sq = sum_of(draft, a.Vd, rn.q.m, a.c64_d);
+      // (p alone: the sum changes no order)
+      const double sp = drow ? sum_of(target, a.V, rn.p.m, a.c64_t) : 1.;
+      const double sq = drow ? sum_of(draft, a.Vd, rn.q.m, a.c64_d) : 1.;
       for (int own = 0; own < 2; ++own) {   // (own: no difference is positive)
         double hi = -INFINITY;
         int who = INT_MAX;
         for (int v = tid; v < a.V; v += VF_THREADS) {
           double p = exp2((target(v) - rn.p.m) * a.c64_t) / sp;
-          const int d = draft_of(v);
-          if (!own && d >= 0) p -= exp2((draft(d) - rn.q.m) * a.c64_d) / sq;
+          const int d = !own && drow ? draft_of(v) : -1;
+          if (d >= 0) p -= exp2((draft(d) - rn.q.m) * a.c64_d) / sq;
           const double sc = log(p) + noise[v];   // (NaN below 0)
-          if (sc > hi) {
+          if (sc > hi && (own || v != hot)) {
             hi = sc;
             who = v;
           }
@@ -555,11 +600,6 @@ __global__ void __launch_bounds__(VF_THREADS) verify_pick(VerifyArgs a) {
         next = who == INT_MAX ? 0 : who;
         if (who != INT_MAX) break;
       }
-    } else if (top) {
-      next = key_token(top);
-    } else {   // (p is all on the draft too, or nothing is above -inf: the lowest token)
-      bool ignore = false;
-      next = hot >= 0 && clean(to_f32(row[hot]), ignore) > -INFINITY && noise[hot] > -INFINITY ? hot : 0;
     }
   }
   for (int i = tid; i <= a.k; i += VF_THREADS)

@@ -44,3 +44,58 @@ def test_drafts_of_probabilities_below_32_bits(mode, p, q, u, stands, dtype):
     if dtype == "f32":                                        # (e^-95 and the like are no bf16 values, the steps between them are)
         rt, ra = _tv()._ref(s)
         assert torch.equal(acc, ra) and torch.equal(tok, rt)
+
+
+def _softmax(x):
+    """In 64 bits (torch.softmax of rows above 1024 keeps 24 of them on the GPU)."""
+    e = (x - x.amax(-1, keepdim=True)).exp()
+    return e / e.sum(-1, keepdim=True)
+
+
+def _near(B, V, Vd, mode, spread, gap, seed):
+    """Requests of one draft that is rejected (or none, mode "last"), targets within `spread` of the draft's logits, and
+    noise that leaves the two best scores about `gap` apart, in either order.  Temperatures that 32 bits hold."""
+    import torch
+    s = _tv()._make(B, 1, V, Vd, "f32", "onehot" if mode == "onehot" else "sample", seed=seed)
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    r = lambda *n: torch.randn(*n, generator=g, device="cuda")  # noqa: E731
+    s["T"], s["Td"] = 0.75, 0.75
+    ids = s["d2t"].long() if s["d2t"] is not None else torch.arange(Vd, device="cuda")
+    tok = s["tok"][:, 0].long()
+    if s["draft"] is not None:
+        s["draft"] = 2 * r(B, 1, Vd)
+        s["target"].normal_(-3.0, 1.0, generator=g)
+        s["target"][0::2, ids] = s["draft"][:, 0] + spread * r(B, Vd)
+    at = torch.arange(B, device="cuda")
+    s["target"][2 * at, ids[tok]] -= 3.0                       # (p(t) below q(t))
+    s["u"].fill_(1 - 2.0 ** -24)
+    if mode == "last":
+        s["n"], s["rows"], s["cu"] = [0] * B, B, torch.arange(B + 1, dtype=torch.int32, device="cuda")
+        s["target"] = s["target"][1::2].contiguous()
+    x = (s["target"] if mode == "last" else s["target"][0::2]).double() / s["T"]
+    p = _softmax(x)
+    q = torch.zeros_like(p)
+    if mode == "onehot":
+        q[at, ids[tok]] = 1.0
+    elif mode == "sample":
+        q[:, ids] = _softmax(s["draft"][:, 0].double() / s["Td"])
+    rest = (p - q).clamp(min=0).log()
+    best = (rest + s["gumbel"].double()).topk(2, -1)
+    move = best.values[:, 0] - best.values[:, 1] + gap * r(B).double()
+    s["gumbel"][at, best.indices[:, 1]] += move.float()
+    score = rest + s["gumbel"].double()
+    top = score.topk(2, -1)
+    return s, top.indices[:, 0], top.values[:, 0] - top.values[:, 1]
+
+
+@pytest.mark.parametrize("spread,gap", [(2.0 ** -8, 2e-4), (2.0 ** -6, 5e-5), (0.5, 1e-6), (1e-4, 1e-2)])
+@pytest.mark.parametrize("mode", ["sample", "onehot", "last"])
+@pytest.mark.parametrize("V,Vd", [(64, 64), (3000, 1000)])
+def test_choices_among_close_scores(V, Vd, mode, spread, gap):
+    """The choice is that of 64 bits, also where the scores of two tokens differ by less than their roundings in 32."""
+    import torch
+    s, want, margin = _near(500, V, Vd, mode, spread, gap, V)
+    tok, acc, ws = _tv()._run(s)
+    assert (acc == 0).all() and hspec.read_status(ws) == 0
+    wrong = (tok[:, 0] != want) & (margin > 1e-11)             # (64 bits of another order of summation)
+    assert not wrong.any(), (int(wrong.sum()), margin[wrong].tolist()[:5])
