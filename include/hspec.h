@@ -473,9 +473,12 @@ size_t hspec_chunk_append_workspace(const hspec_chunk_cfg* cfg);
  * o[r, h] = softmax over the visible positions s <= ctx_len + i of scale q[r, h] . K[s], times V:
  * q, o [T, Hq, D], the caches hold the new tokens' K and V already (hspec_chunk_append).  max_len:
  * host upper bound of ctx_lens[b] + new tokens of b (bounds the split of long caches).  A slot that
- * a row does not see never changes it, whatever it holds (NaN and infinities included); pages
- * outside the pool read as zeros and set HSPEC_DEV_BAD_PAGE; a row that sees no position is zero.
- * Results are bitwise reproducible and independent of where pages live.
+ * a row does not see never changes it, not in its last bit, whatever it holds (NaN and infinities
+ * included); pages outside the pool read as zeros and set HSPEC_DEV_BAD_PAGE; a row that sees no
+ * position is zero.  Scores, maxima, sums and the output are held in 32 bits until the output's one
+ * rounding; the softmax weights enter the product with V in the storage dtype (bf16 caches: each weight
+ * off by at most 2^-8 of itself), as in the drafting attention.  Results are bitwise reproducible and
+ * independent of where pages live.
  */
 hspec_status hspec_chunk_attn(const hspec_chunk_cfg* cfg, const void* q, const int32_t* cu_new, const void* k_cache,
                               const void* v_cache, const int32_t* page_table, const int32_t* ctx_lens, int max_len,
@@ -498,6 +501,8 @@ size_t hspec_chunk_attn_workspace(const hspec_chunk_cfg* cfg, int max_len);
  *   that does not, or n;
  *   next = argmax_v log max(p_a(v) - q_a(v), 0) + gumbel[b, v], q = 0 for a = n (p_a alone where no
  *   difference is positive).
+ *   p and q of a decision are those of 32-bit sums (u q within about 2^-16 of p may go either way); the
+ *   choice is that of 64 bits.
  * Greedy (u and gumbel NULL, draft_logits NULL): draft j stands while it is the argmax of row j;
  *   next = argmax of row a.  A tie goes to the lowest id.
  * tokens [B, k+1] int32: the a drafts that stand (target ids), next, then -1; n_accepted [B] = a.

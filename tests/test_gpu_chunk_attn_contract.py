@@ -123,3 +123,26 @@ def test_values_of_no_weight_show(ctx, dtype, what):
     x["v_cache"][_at(x, 0, 5)] = what
     o, _ = u.attend(x)
     assert not torch.isfinite(o[0].float()).any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("window", [0, 200])
+def test_a_request_alone_and_in_its_batch(window, dtype):
+    """The same rows, pages and lengths: each output within its bound of the definition, so within two of each other (the
+    cache may be split elsewhere)."""
+    import torch
+    u = _u()
+    ctx, new = [900, 4000, 0, 33], [17, 17, 300, 1]
+    x = u.batch(ctx, new, 8, 2, 128, dtype=dtype, window=window, seed=3)
+    o, _ = u.check_attend(x)
+    _, tol = u.attend_ref(x)
+    row = 0
+    for b, n in enumerate(new):
+        y = {**x, "ctx": [ctx[b]], "new": [n], "T": n, "q": x["q"][row:row + n].contiguous(), "table": x["table"][b:b + 1].contiguous(),
+             "lens": x["lens"][b:b + 1].contiguous(), "cu": torch.tensor([0, n], dtype=torch.int32, device="cuda"),
+             "max_len": ctx[b] + n}
+        y["cfg"] = hspec.chunk_cfg(1, n, n, 8, 2, 128, x["ps"], x["table"].shape[1], x["pages"],
+                                   hspec.F32 if dtype == "f32" else hspec.BF16, window=window)
+        alone, _ = u.attend(y)
+        assert ((alone.double() - o[row:row + n].double()).abs() <= 2 * tol[row:row + n]).all(), b
+        row += n
