@@ -6,7 +6,7 @@
 // Bound by memory: every element is read once and written once.  A lane holds E elements of both halves
 // of a head, so a head's sum of squares is a shuffle over D / 2E lanes and a pair is turned in registers.
 // The angle is taken in 64 bits: at position 10^6 an fp32 product is off by 2^-5 of a radian.
-// 8000 rows of 80 heads, bf16, no norm: 63 us, 4.9 TB/s, what a copy of as many bytes takes; with the norm 67 (147 with
+// 8000 rows of 80 heads, bf16, no norm: 63 us, 4.9 TB/s, what a copy of as many bytes takes; with the norm 65 (147 with
 // the gains read and the heads divided anew each round); 1088 rows of 48 heads from fp32: 10.5 us.
 #include "common.h"
 #include "target.h"
@@ -16,7 +16,7 @@ namespace hspec {
 namespace {
 
 constexpr int AP_THREADS = 256;
-constexpr int AP_ROWS = 2;   // (with 1 and 4: 8000 bf16 rows of 48 heads 57 and 43 us, 44 here; 1088 fp32 rows 13.1 and 15.2, 12.4)
+constexpr int AP_ROWS = 2;   // (with 1 and 4: 8000 bf16 rows of 48 heads 58 and 44 us, 45 here; 1088 fp32 rows 11.8 and 16, 11.7 on that box)
 
 template <class T, int E>
 __device__ __forceinline__ void load_e(const T* p, float (&v)[E]) {

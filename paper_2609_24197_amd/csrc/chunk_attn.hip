@@ -20,8 +20,9 @@
 // fp32 storage takes the fp32 matrix products (32 x 32 x 2), so nothing is rounded below 32 bits.
 //
 // Bound by reading K and V where requests have few rows (64 requests x 1 token, 512..8192 cached, 32 and 8 heads of
-// 128: 212 us for 1.2 GB; x 17 tokens 256), by the matrix and vector units, busy in 52 % and 46 % of the cycles, in
-// prompts (three of about 6000 tokens 1277 us, 1065 TFLOP/s; 2000 tokens behind 30000, 64 heads, 1840 us, 1104).
+// 128: 212 us for 1.2 GB; x 17 tokens 255), by the matrix and vector units in prompts, busy in 52 % and 46 % of the
+// cycles and mostly in turn (three of about 6000 tokens 1278 us, 1064 TFLOP/s; 2000 tokens behind 30000, 64 heads,
+// 1834 us, 1107; boxes differ by up to 4 %, so where a rule below has two figures, both are of one box).
 #include <algorithm>
 #include <atomic>
 #include <cfloat>
@@ -48,9 +49,9 @@ constexpr int BUFFER_FLAGS = 0x00027000;   // 32-bit data, no swizzle
 constexpr float CHUNK_SLACK = 8.f;
 
 // NW waves, KT keys per tile.  ONCE: a request's rows fit one tile, so its K and V are read once: non-temporal loads,
-// and a die takes all heads of its units, so that it reads whole rows of the cache (64 requests of 1 row 212 us, 237
-// the other way); otherwise a die keeps to its KV heads, whose K and V the tiles of a request share in its L2 (three
-// prompts 1284 us, 1766 the other way).
+// and a die takes all heads of its units, so that it reads whole rows of the cache (64 requests of 17 tokens 256 us, 264
+// the other way; of 1 token 212 either way); otherwise a die keeps to its KV heads, whose K and V the tiles of a
+// request share in its L2 (three prompts 1325 us, 1440 the other way; 2000 tokens behind 30000 1905 and 1990).
 template <class T_, int D_, int NW_, int KT_, bool ONCE_>
 struct Chunk {
   typedef T_ T;
@@ -296,8 +297,8 @@ __device__ __forceinline__ bool chunk_unit(const ChunkAttnArgs& a, const ChunkUn
 
     // O^T += V^T P^T.  P enters as bf16 with bf16 storage (half a step is 2^-8 of each weight, and the output's own
     // rounding is as large); the sum above takes the unrounded weights.  This wave first while it has products to
-    // issue: the other wave of the SIMD has its softmax to fill in (three prompts 1443 -> 1379 us, a chunk of 2000
-    // tokens behind 30000 2170 -> 1992).
+    // issue: the other wave of the SIMD has its softmax to fill in (three prompts 1350 -> 1325 us, a chunk of 2000
+    // tokens behind 30000 2008 -> 1905).
     __builtin_amdgcn_s_setprio(1);
     auto add_values = [&](auto masked_) {
       constexpr bool FIX = ODD && decltype(masked_)::value;
@@ -505,8 +506,8 @@ constexpr int MG_THREADS = 256;
 // o = sum_i O_i 2^(m_i - m*) / sum_i l_i 2^(m_i - m*) over a row's pieces, in an order of their own (not of time).
 // Bound by the round trips of a row's loads: a workgroup takes one row, with its pieces spread over groups of D / 4
 // threads, where that makes few workgroups (few rows, so perhaps many pieces each: 1 request of 32768 tokens, 64 pieces,
-// 47 us for the whole call, 60 with a thread for all of a row's pieces), else 1024 / D rows (64 requests of
-// 68 rows 255 us for the whole call, 288 with a row each).
+// 43 us for the whole call, 56 with a thread for all of a row's pieces), else 1024 / D rows (64 requests of
+// 68 rows 256 us for the whole call, 291 with a row each).
 constexpr int MG_FEW = 4096;   // workgroups up to which each takes one row
 
 template <class T, int D>

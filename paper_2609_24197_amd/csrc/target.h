@@ -67,8 +67,8 @@ constexpr int kChunkMinSplit = 64;   // keys a piece of a split tile has at leas
 constexpr int kMaxPositions = INT_MAX - 65536;   // of a request: places past the end of a tile stay inside 31 bits
 
 // Keys a unit takes at most, in whole key tiles, for `keys` keys of `tiles` tiles of rows: where the tiles leave most of
-// the chip free, what makes one round of units (so every piece starts at once: 1 request of 32768 tokens 47 us, 60 in
-// two short rounds), else 13/8 rounds, which the queue evens out.  At least keys Hkv / target, which the workspace
+// the chip free, what makes one round of units (so every piece starts at once: 1 request of 32768 tokens 43 us, 54 in
+// two short rounds; 8 of 4000 tokens 39 and 45), else 13/8 rounds, which the queue evens out.  At least keys Hkv / target, which the workspace
 // counts on (the factor covers the float roundings).
 __host__ __device__ inline int chunk_unit_keys(const ChunkAttnArgs& a, unsigned long long keys, int tiles) {
   const float spare = (float)a.slots - (float)tiles * (float)a.Hkv;
@@ -90,10 +90,10 @@ __host__ __device__ inline int chunk_pieces(int len, int S, int key_tile, int& q
 // Tile of the units, and the most units, partial slots and split tiles the plan can make of any lengths.  32 rows per
 // wave; past four waves a request has several tiles (once = 0).  fp32 takes one, two or four waves by the rows a request
 // can have (n g): its key tile and LDS are the same for all, so waves without rows only keep others out (64 requests of
-// 1 row of 16 heads 275 us, 491 with four; of 12 rows 262 and 503).  bf16 takes four, whose idle waves still load
-// (64 requests of 14 rows 257 us, 273 with two; 1 request of 1 row and 16000 cached 36 us, 44 with one), but one for
-// up to 32 rows over many long caches, where small workgroups keep more of them reading (64 requests of 1 row and
-// 512..8192 cached 212 us, 221 with four; 200 of at most 3000 cached, with one, 228 us, 218 with four).
+// 512..8192 cached, 16 and 4 heads of 128: 1 token 484 us, 888 with four; 3 tokens 489 and 895).  bf16 takes four, whose
+// idle waves still load (32 and 8 heads of 128: 1 request of 1 token and 16000 cached 32 us, 36 with one; 200 of at most
+// 3000 cached 218 and 224), but one for up to 32 rows over many long caches, where small workgroups keep more of them
+// reading (64 requests of 1 token and 512..8192 cached 212 us, 223 with four).
 inline void chunk_bounds(ChunkAttnArgs& a) {
   const long long g = a.Hq / a.Hkv, R = a.max_new * g;
   const bool many_long = a.cap >= 4096 && (long long)a.B * a.Hkv >= 32;

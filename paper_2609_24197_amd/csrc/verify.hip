@@ -11,8 +11,8 @@
 // is comes out of the rows before it: the pieces of all rows are taken in the order of j by a grid that holds little
 // more than one j of every request at a time; the workgroup that finishes a row decides its draft, and pieces of rows
 // past a request's decision are left out.  Then row n is read once more for the choice.  64 requests x 16 drafts,
-// 131072 bf16 logits: 162 us when every row was read first, now 66; where every draft stands 112 us (467 MB, 4.2 TB/s),
-// greedy 72 (285 MB, 4.0 TB/s).
+// 131072 bf16 logits: 162 us when every row was read first, now 67; where every draft stands 112 us (467 MB, 4.2 TB/s),
+// greedy 71 (285 MB, 4.0 TB/s).
 #include <algorithm>
 #include <cfloat>
 #include <climits>
@@ -29,7 +29,7 @@ constexpr int VF_THREADS = 256;
 constexpr int ST_BAD_TOKEN = 4;
 constexpr int ST_NONFINITE = 8;
 constexpr int VF_PIECE = kVerifyPiece;
-constexpr int VF_GRID = 16384;    // (90 us at 64 x 16 x 131072 with 4096, 76 with 8192, then 74)
+constexpr int VF_GRID = 16384;    // (64 x 16 x 131072: 67 us, 77 with 4096, 74 with 8192)
 constexpr float VF_LOWEST = -1074.f;   // log2 of the least probability that is not 0, as 64 bits have it
 constexpr float VF_ERR = 1.25f * 0x1p-23f, VF_ERR0 = 20.f * 0x1p-23f;   // see verify_pick
 constexpr float LN2 = 0.6931471805599453f;
