@@ -16,7 +16,7 @@ namespace hspec {
 namespace {
 
 constexpr int AP_THREADS = 256;
-constexpr int AP_ROWS = 2;   // (with 1 and 4: 8000 bf16 rows of 48 heads 58 and 44 us, 45 here; 1088 fp32 rows 11.8 and 16, 11.7 on that box)
+constexpr int AP_ROWS = 2;   // (with 1 and 4: 8000 bf16 rows of 48 heads 58 and 44 us, 45 here; 1088 fp32 rows 11.8 and 16, 11.7 on that card)
 
 template <class T, int E>
 __device__ __forceinline__ void load_e(const T* p, float (&v)[E]) {

@@ -146,3 +146,12 @@ def test_a_request_alone_and_in_its_batch(window, dtype):
         alone, _ = u.attend(y)
         assert ((alone.double() - o[row:row + n].double()).abs() <= 2 * tol[row:row + n]).all(), b
         row += n
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [1, 3])
+def test_a_cache_in_more_pieces_than_a_merge_takes_at_once(new, dtype):
+    """One KV head and 90000 positions: more than 256 pieces."""
+    u = _u()
+    _, ws = u.check_attend(u.batch([90001], [new], 4, 1, 64, dtype=dtype, seed=new))
+    assert hspec.read_status(ws) == 0
