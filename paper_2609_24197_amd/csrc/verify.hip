@@ -468,7 +468,7 @@ __global__ void __launch_bounds__(VF_THREADS) verify_pick(VerifyArgs a) {
       return d < a.Vd ? max(d, -1) : -1;
     };
     // log2 of p is off by at most 2^-24 of (l - m) / T for the difference, for the scale and for the result, and what
-    // the sum's logarithm is off by, so p by VF_ERR |log2 p| + VF_ERR0 of itself, the rounding of the score included.
+    // the sum's logarithm is off by, so p by VF_ERR |log2 p| + VF_ERR0 of itself; the score is rounded once more.
     // log2(p - q) = log2 p + log2(1 - r), r = q / p, which holds where 32 bits hold neither p nor q.
     float best = -INFINITY;
     int at = -1;
@@ -507,7 +507,8 @@ __global__ void __launch_bounds__(VF_THREADS) verify_pick(VerifyArgs a) {
           up += __builtin_amdgcn_logf(__builtin_fmaf(1.f + r, err, d1));
         }
         const float sc = __builtin_fmaf(lg, LN2, gn[i]);
-        const float hi = v0 + i == hot ? -INFINITY : __builtin_fmaf(up, LN2, gn[i]) + err;
+        const float top = __builtin_fmaf(up, LN2, gn[i]);
+        const float hi = v0 + i == hot ? -INFINITY : __builtin_fmaf(fabsf(top), 0x1p-23f, top + err);
         bad_noise |= !(gn[i] == gn[i]);
         const bool better = sc > best && v0 + i != hot;
         pick.rival = fmaxf(pick.rival, better ? pick.hi : hi);

@@ -52,7 +52,7 @@ def _softmax(x):
     return e / e.sum(-1, keepdim=True)
 
 
-def _near(B, V, Vd, mode, spread, gap, seed):
+def _near(B, V, Vd, mode, spread, gap, seed, shift=0.0):
     """Requests of one draft that is rejected (or none, mode "last"), targets within `spread` of the draft's logits, and
     noise that leaves the two best scores about `gap` apart, in either order.  Temperatures that 32 bits hold."""
     import torch
@@ -66,6 +66,7 @@ def _near(B, V, Vd, mode, spread, gap, seed):
         s["draft"] = 2 * r(B, 1, Vd)
         s["target"].normal_(-3.0, 1.0, generator=g)
         s["target"][0::2, ids] = s["draft"][:, 0] + spread * r(B, Vd)
+    s["gumbel"] += shift
     at = torch.arange(B, device="cuda")
     s["target"][2 * at, ids[tok]] -= 3.0                       # (p(t) below q(t))
     s["u"].fill_(1 - 2.0 ** -24)
@@ -99,3 +100,14 @@ def test_choices_among_close_scores(V, Vd, mode, spread, gap):
     assert (acc == 0).all() and hspec.read_status(ws) == 0
     wrong = (tok[:, 0] != want) & (margin > 1e-11)             # (64 bits of another order of summation)
     assert not wrong.any(), (int(wrong.sum()), margin[wrong].tolist()[:5])
+
+
+@pytest.mark.parametrize("mode", ["sample", "onehot", "last"])
+@pytest.mark.parametrize("shift", [3000.0, -3000.0])
+def test_choices_under_noise_far_from_zero(mode, shift):
+    """Noise moved by a constant, which changes no choice: a score's rounding is as large as the noise."""
+    import torch
+    s, want, margin = _near(500, 700, 300, mode, 0.1, 2e-4, 7, shift)
+    tok, acc, ws = _tv()._run(s)
+    wrong = (tok[:, 0] != want) & (margin > 1e-11)
+    assert (acc == 0).all() and not wrong.any(), (int(wrong.sum()), margin[wrong].tolist()[:5])
