@@ -22,7 +22,7 @@
 // Bound by reading K and V where requests have few rows (64 requests x 1 token, 512..8192 cached, 32 and 8 heads of
 // 128: 212 us for 1.2 GB; x 17 tokens 255), by the matrix and vector units in prompts, busy in 52 % and 46 % of the
 // cycles and mostly in turn (three of about 6000 tokens 1278 us, 1064 TFLOP/s; 2000 tokens behind 30000, 64 heads,
-// 1834 us, 1107; cards differ by up to 4 %; where a rule below has two figures, both are of one card).
+// 1834 us, 1107; cards differ by up to 6 %; where a rule below has two figures, both are of one card).
 #include <algorithm>
 #include <atomic>
 #include <cfloat>
