@@ -1,0 +1,649 @@
+"""The target's cache in 4 bits and its logits before verification, as cases that can be timed and compared.
+
+  append  hspec_chunk_append_q4: norm and RoPE of the new tokens' q and k, K and V rounded to 4-bit floats
+          with a power-of-two scale for every 32 channels, into the pages; then hspec_chunk_read_q4 of the
+          same tokens, which gives what the cache now holds of them
+  read    hspec_chunk_read_q4: cached positions as dense rows
+  attn    hspec_chunk_attn_q4: attention of a ragged batch of new tokens over that cache; their own K and V
+          are in the cache, or beside it in full precision ("dense": the drafter's block, where every
+          token of a block sees every other, or a causal one)
+  adjust  hspec_adjust_logits: bias, penalties for tokens that were said before (the drafts ahead of a row
+          among them) and a grammar's mask
+
+A cache holds, for every page and KV head, page_size rows of D/2 bytes (channel 2i in the low half of
+byte i) and then page_size rows of D/32 scale bytes.  A scale byte s stands for 2^(s-127); it is the
+smallest for which the block's largest magnitude stays below 7 scales.
+
+With ``own`` false, ``run`` is the plain form in elementary torch operations; with ``own`` true it makes
+the library's calls.  Head layouts are those of the serving configurations ("8b": 32 query and 8 KV heads
+of 128, "large": 64 and 8, "tiny": the small fp32 configuration), the drafter's pruned vocabulary has
+32000 tokens, the target's is generic.
+"""
+from __future__ import annotations
+
+import math
+import random
+
+import torch
+
+own = False
+
+HEADS = {
+    "tiny": dict(Hq=4, Hkv=1, D=64, dtype="f32"),
+    "8b": dict(Hq=32, Hkv=8, D=128, dtype="bf16"),
+    "large": dict(Hq=64, Hkv=8, D=128, dtype="bf16"),
+    "mha": dict(Hq=12, Hkv=12, D=64, dtype="bf16"),
+    "odd": dict(Hq=15, Hkv=5, D=128, dtype="bf16"),
+    "f32": dict(Hq=16, Hkv=4, D=128, dtype="f32"),
+}
+DRAFT_VOCAB = 32000
+THETA, EPS = 1e6, 1e-6
+BLOCK = 32                                             # channels that share a scale
+
+
+def listed():
+    return [
+        # one request's verification rows in the small fp32 configuration: launches are all that counts
+        dict(name="append-tiny-verify", kind="append", shape="tiny", B=1, ctx="64:64", new="5:5", page=16, rows="f32"),
+        # the rows of the serving batch's verification step
+        dict(name="append-8b-verify-b64", kind="append", shape="8b", B=64, ctx="512:8192", new="17:17", page=16, rows="f32"),
+        # a prompt's rows, from a bf16 projection, no norms
+        dict(name="append-large-prompt-8k", kind="append", shape="large", B=2, ctx="0:100", new="3001:5003", page=32,
+             rows="bf16", norm=False),
+        # one request's last pages on their way into a cache of another type
+        dict(name="read-8b-tail", kind="read", shape="8b", B=1, ctx="1000:1000", new="117:117", page=16),
+        # sixteen whole requests that move
+        dict(name="read-8b-move-b16", kind="read", shape="8b", B=16, ctx="0:0", new="300:8191", page=16),
+        # one request decoding in the small fp32 configuration
+        dict(name="attn-tiny-decode", kind="attn", shape="tiny", B=1, ctx="64:64", new="1:1", page=16, window=0),
+        # plain decoding of the serving batch: one token each, the cache is what is read
+        dict(name="attn-8b-decode-b64", kind="attn", shape="8b", B=64, ctx="512:8192", new="1:1", page=16, window=0),
+        # the target's verification pass over 16 drafts and the last token of each request
+        dict(name="attn-8b-verify-b64", kind="attn", shape="8b", B=64, ctx="512:8192", new="17:17", page=16, window=0),
+        # the drafter's block of 16 over the target's cache, its own K and V beside it
+        dict(name="attn-8b-draft-b64", kind="attn", shape="8b", B=64, ctx="512:8192", new="16:16", page=16, window=0,
+             dense="block"),
+        # three prompts of odd lengths at once, nothing cached yet
+        dict(name="attn-8b-prompt-3x6k", kind="attn", shape="8b", B=3, ctx="0:0", new="4097:8191", page=32, window=0),
+        # one request's next token over the drafter's own vocabulary
+        dict(name="adjust-b1", kind="adjust", B=1, k=0, V=DRAFT_VOCAB, hist="700:700", bias=3, mask=True, dtype="f32",
+             out="f32", pruned=False),
+        # the serving batch's verification rows, bf16 logits, pruned draft vocabulary
+        dict(name="adjust-verify-b64", kind="adjust", B=64, k=16, V=131072, hist="512:8192", bias=40, mask=True,
+             dtype="bf16", out="bf16", pruned=True),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def draw(rng):
+    kind = rng.choice(["attn", "attn", "attn", "attn", "append", "read", "adjust", "adjust"])
+    if kind == "adjust":
+        V, B = _log_int(rng, 1000, 131072), _log_int(rng, 1, 64)
+        top = _log_int(rng, 1, 32768 if B < 8 else 8192)
+        return dict(kind=kind, B=B, k=rng.choice([0, rng.randint(1, 16)]), V=V, hist=f"{rng.randint(0, top)}:{top}",
+                    bias=rng.choice([0, _log_int(rng, 1, 300)]), mask=rng.random() < 0.6,
+                    dtype=rng.choice(["bf16", "bf16", "f32"]), out=rng.choice(["bf16", "f32"]),
+                    pruned=V > DRAFT_VOCAB and rng.random() < 0.7)
+    shape = rng.choice(["tiny", "8b", "8b", "large", "mha", "odd", "f32"])
+    page = rng.choice([16, 16, 32, 64, 128])
+    if kind in ("append", "read"):
+        B = _log_int(rng, 1, 64)
+        top = _log_int(rng, 1, max(1, (8000 if kind == "append" else 60000) // B))
+        c = dict(kind=kind, shape=shape, B=B, ctx=f"0:{_log_int(rng, 1, 8192)}", new=f"{rng.randint(1, top)}:{top}", page=page)
+        if kind == "append":
+            c.update(rows=rng.choice(["f32", "bf16"]), norm=rng.random() < 0.7)
+        return c
+    use = rng.choice(["decode", "verify", "verify", "draft", "prompt", "mixed"])
+    window = rng.choice([0, 0, 0, 2048, rng.randint(1, 5000)])
+    if use in ("decode", "verify", "draft"):
+        B = _log_int(rng, 1, 64)
+        top = _log_int(rng, 1, min(32768, 250000 // B))
+        n = 1 if use == "decode" else rng.randint(2, 17)
+        c = dict(kind=kind, shape=shape, B=B, ctx=f"{rng.randint(0, top)}:{top}", new=f"{n}:{n}", page=page, window=window)
+        if use == "draft":
+            c.update(dense=rng.choice(["block", "causal"]), window=window and max(window, n))
+        return c
+    if use == "prompt":
+        B = rng.randint(1, 4)
+        top = _log_int(rng, 16, 6000 // B)
+        return dict(kind=kind, shape=shape, B=B, ctx="0:0", new=f"{rng.randint(1, top)}:{top}", page=page, window=window)
+    B = _log_int(rng, 1, 24)
+    top = _log_int(rng, 1, 6000 // B)
+    return dict(kind=kind, shape=shape, B=B, ctx=f"0:{_log_int(rng, 1, 8192)}", new=f"1:{top}", page=page, window=window)
+
+
+# ------------------------------------------------------------------------------- inputs
+
+
+def _lengths(n, text, salt):
+    """n whole numbers between the two of `text`, the same for every seed: a case's sizes are its own."""
+    lo, hi = (int(v) for v in text.split(":"))
+    rng = random.Random(f"{salt} {n} {text}")
+    return [rng.randint(lo, hi) for _ in range(n)]
+
+
+def _requests(case):
+    """(cached, new) tokens of each request."""
+    return list(zip(_lengths(case["B"], case["ctx"], "cached"), _lengths(case["B"], case["new"], "new")))
+
+
+def _drafts(case):
+    """Drafted tokens of each request; in odd batches all but one may have fewer than k."""
+    if case["B"] % 2 == 0:
+        return [case["k"]] * case["B"]
+    return [case["k"]] + _lengths(case["B"] - 1, f"0:{case['k']}", "drafts")
+
+
+class _Rand:
+    """Seeded draws, in a fixed order."""
+
+    def __init__(self, seed):
+        self.g = torch.Generator(device="cuda").manual_seed(int(seed))
+        self.h = torch.Generator().manual_seed(int(seed) + 1)
+
+    def normal(self, *shape, dtype=torch.float32, std=1.0, mean=0.0):
+        return torch.empty(shape, dtype=dtype, device="cuda").normal_(mean, std, generator=self.g)
+
+    def uniform(self, *shape):
+        return torch.rand(shape, device="cuda", generator=self.g)
+
+    def ints(self, lo, hi, *shape):
+        return torch.randint(lo, hi, shape, device="cuda", generator=self.g, dtype=torch.int32)
+
+    def shuffled(self, rows):
+        return torch.tensor(rows, dtype=torch.int32)[torch.randperm(len(rows), generator=self.h)]
+
+    def perm(self, n, on="cpu"):
+        return torch.randperm(n, generator=self.h if on == "cpu" else self.g, device=on)
+
+
+def _dtype(name):
+    return torch.float32 if name == "f32" else torch.bfloat16
+
+
+def _batch(r, case):
+    """Ragged rows, lengths and a shuffled page table; the batch is padded by three rows past the last
+    request.  Where the new tokens' K and V are beside the cache, the table has pages for the old ones only."""
+    B, ps = case["B"], case["page"]
+    ctx, new = (t.contiguous() for t in r.shuffled(_requests(case)).unbind(1))
+    cu = torch.zeros(B + 1, dtype=torch.int32)
+    cu[1:] = new.cumsum(0)
+    total = ctx + new
+    npg = ((ctx if case.get("dense") else total) + ps - 1) // ps
+    pages = int(npg.sum()) + 2
+    order = r.perm(pages).int()
+    table = torch.full((B, max(1, int(npg.max()))), -1, dtype=torch.int32)
+    at = 0
+    for b, n in enumerate(npg.tolist()):
+        table[b, :n] = order[at:at + n]
+        at += n
+    return dict(ctx=ctx, new=new, rows=int(cu[-1]) + 3, max_new=int(new.max()), max_len=int(total.max()), pages=pages,
+                cu_new=cu.cuda(), ctx_lens=ctx.cuda(), page_table=table.cuda())
+
+
+def _pool(r, pages, ps, Hkv, D, std):
+    """A cache of 4-bit values as attention meets them: some channels larger than others."""
+    out = torch.empty((pages, Hkv, ps * (D // 2 + D // BLOCK)), dtype=torch.uint8, device="cuda")
+    gain = torch.exp(r.normal(Hkv, 1, D, std=0.4)) * std
+    for p0 in range(0, pages, 2048):
+        n = min(2048, pages - p0)
+        codes, scales = _quantise(r.normal(n, Hkv, ps, D) * gain)
+        out[p0:p0 + n] = torch.cat([codes.reshape(n, Hkv, -1), scales.reshape(n, Hkv, -1)], -1)
+    return out
+
+
+def _prepare_chunk(case, seed):
+    r, h = _Rand(seed), HEADS[case["shape"]]
+    t, Hq, Hkv, D = _dtype(h["dtype"]), h["Hq"], h["Hkv"], h["D"]
+    x = _batch(r, case)
+    x.update(case=case, k_cache=_pool(r, x["pages"], case["page"], Hkv, D, 0.9),
+             v_cache=_pool(r, x["pages"], case["page"], Hkv, D, 0.9))
+    if case["kind"] == "attn":
+        x["q"] = r.normal(x["rows"], Hq, D, dtype=t)
+        x["o"] = torch.zeros_like(x["q"])
+        x["k_new"] = x["v_new"] = None
+        if case.get("dense"):
+            x["k_new"], x["v_new"] = r.normal(x["rows"], Hkv, D, dtype=t), r.normal(x["rows"], Hkv, D, dtype=t)
+        return x
+    x["k_out"] = torch.zeros((x["rows"], Hkv, D), dtype=t, device="cuda")
+    x["v_out"] = torch.zeros_like(x["k_out"])
+    if case["kind"] == "append":
+        x["qkv"] = r.normal(x["rows"], (Hq + 2 * Hkv) * D, dtype=_dtype(case["rows"]), std=0.7)
+        norm = case.get("norm", True)
+        x["q_norm_w"] = r.normal(D, std=0.1, mean=1.0) if norm else None
+        x["k_norm_w"] = r.normal(D, std=0.1, mean=1.0) if norm else None
+        x["q"] = torch.zeros((x["rows"], Hq, D), dtype=t, device="cuda")
+    return x
+
+
+def _prepare_adjust(case, seed):
+    r, B, k, V = _Rand(seed), case["B"], case["k"], case["V"]
+    Vd = DRAFT_VOCAB if case["pruned"] else V
+    n = r.shuffled(_drafts(case))
+    cu = torch.zeros(B + 1, dtype=torch.int32)
+    cu[1:] = (n + 1).cumsum(0)
+    rows = int(cu[-1])
+    lens = torch.tensor(_lengths(B, case["hist"], "history"), dtype=torch.int32)
+    top = max(1, int(lens.max()))
+    # words come with very different frequencies, and texts repeat themselves
+    said = (V * r.uniform(B, top) ** 6).int().clamp(max=V - 1)
+    st = dict(case=case, rows=rows, cu_rows=cu.cuda(), logits=r.normal(rows, V, std=3.0).to(_dtype(case["dtype"])),
+              history=said, hist_lens=lens.cuda(), prompt_lens=(lens * 3 // 5).cuda(), d2t=None, draft_tokens=None,
+              repetition=1.0 + 0.3 * r.uniform(B), frequency=0.5 * r.uniform(B), presence=0.7 * r.uniform(B),
+              bias_ids=None, bias=None, mask=None, mask_rows=None,
+              out=torch.zeros((rows, V), dtype=_dtype(case["out"]), device="cuda"))
+    if case["pruned"]:
+        st["d2t"] = r.perm(V, "cuda")[:Vd].sort().values.int()
+    if k:
+        st["draft_tokens"] = (Vd * r.uniform(B, k) ** 4).int().clamp(max=Vd - 1)
+    if case["bias"]:
+        st["bias_ids"] = torch.stack([r.perm(V, "cuda")[:case["bias"]] for _ in range(B)]).int()
+        st["bias"] = r.normal(B, case["bias"], std=4.0)
+    if case["mask"]:
+        # some rows are free (-1), the others take one of a grammar's states: from a few tokens to most of them
+        words = (V + 31) // 32
+        states = max(2, rows // 3)
+        share = r.uniform(states, 1) ** 2
+        bits = r.uniform(states, words * 32) < share + 0.001
+        weight = (1 << torch.arange(32, device="cuda", dtype=torch.int64))
+        word = (bits.view(states, words, 32) * weight).sum(-1)
+        st["mask"] = torch.where(word >= 1 << 31, word - (1 << 32), word).int()
+        st["mask_rows"] = r.ints(-(states // 3) - 1, states, rows).clamp(min=-1)
+    return st
+
+
+def prepare(case, seed):
+    st = _prepare_adjust(case, seed) if case["kind"] == "adjust" else _prepare_chunk(case, seed)
+    if own:
+        _plan(st)
+    return st
+
+
+def _plan(st):
+    """Configuration and workspace, which a program keeps from step to step."""
+    from paper_2609_24197_amd import hspec
+
+    case = st["case"]
+    code = lambda name: hspec.F32 if name == "f32" else hspec.BF16  # noqa: E731
+    if case["kind"] == "adjust":
+        Vd = DRAFT_VOCAB if case["pruned"] else case["V"]
+        st["cfg"] = hspec.adjust_cfg(case["B"], case["k"], st["rows"], case["V"], Vd, max_hist=st["history"].shape[1],
+                                     n_bias=case["bias"], masks=0 if st["mask"] is None else st["mask"].shape[0],
+                                     dtype=code(case["dtype"]), out_dtype=code(case["out"]))
+        st["ws"] = hspec.workspace(hspec.adjust_logits_workspace(st["cfg"]))
+        return
+    h = HEADS[case["shape"]]
+    st["cfg"] = hspec.chunk_cfg(case["B"], st["rows"], st["max_new"], h["Hq"], h["Hkv"], h["D"], case["page"],
+                                st["page_table"].shape[1], st["pages"], code(h["dtype"]), window=case.get("window", 0),
+                                eps=EPS, rope_theta=THETA)
+    if case["kind"] == "attn":
+        need = hspec.chunk_attn_q4_workspace(st["cfg"], st["max_len"])
+    else:
+        need = max(hspec.chunk_append_q4_workspace(st["cfg"]), hspec.chunk_read_q4_workspace(st["cfg"]))
+    st["ws"] = hspec.workspace(need)
+
+
+# --------------------------------------------------------------------------- one pass
+
+
+def run(st):
+    kind = st["case"]["kind"]
+    if own:
+        return _RUN_OWN[kind](st)
+    return _RUN_PLAIN[kind](st)
+
+
+def _own_append(st):
+    from paper_2609_24197_amd import hspec
+    hspec.chunk_append_q4(st["cfg"], st["qkv"], st["cu_new"], st["ctx_lens"], st["q"], st["k_cache"], st["v_cache"],
+                          st["page_table"], st["ws"], q_norm_w=st["q_norm_w"], k_norm_w=st["k_norm_w"])
+    return dict(q=st["q"], **_own_read(st))
+
+
+def _own_read(st):
+    from paper_2609_24197_amd import hspec
+    hspec.chunk_read_q4(st["cfg"], st["cu_new"], st["ctx_lens"], st["k_cache"], st["v_cache"], st["page_table"],
+                        st["k_out"], st["v_out"], st["ws"])
+    return dict(k=st["k_out"], v=st["v_out"])
+
+
+def _own_attn(st):
+    from paper_2609_24197_amd import hspec
+    hspec.chunk_attn_q4(st["cfg"], st["q"], st["cu_new"], st["k_cache"], st["v_cache"], st["page_table"], st["ctx_lens"],
+                        st["max_len"], st["o"], st["ws"], k_new=st["k_new"], v_new=st["v_new"],
+                        block=st["case"].get("dense") == "block")
+    return st["o"]
+
+
+def _own_adjust(st):
+    from paper_2609_24197_amd import hspec
+    hspec.adjust_logits(st["cfg"], st["logits"], st["out"], st["ws"], cu_rows=st["cu_rows"],
+                        draft_tokens=st["draft_tokens"], d2t=st["d2t"], history=st["history"], hist_lens=st["hist_lens"],
+                        prompt_lens=st["prompt_lens"], repetition=st["repetition"], frequency=st["frequency"],
+                        presence=st["presence"], bias_ids=st["bias_ids"], bias=st["bias"], mask=st["mask"],
+                        mask_rows=st["mask_rows"])
+    return st["out"]
+
+
+def _quantise(y):
+    """(codes [.., D/2], scales [.., D/32]) of y [.., D]; in 64 bits, where values next to a border stay on their side."""
+    y = y.double().unflatten(-1, (-1, BLOCK))
+    m, e = torch.frexp(y.abs().amax(-1, keepdim=True))             # amax = m 2^e, 1/2 <= m < 1
+    e = torch.where(m == 0, -126, (e - 3 + (m >= 0.875)).clamp(min=-126))
+    t = torch.ldexp(y.abs(), -e)
+    code = (t > 0.25).to(torch.uint8)
+    code += t >= 0.75
+    code += t > 1.25
+    code += t >= 1.75
+    code += t > 2.5
+    code += t >= 3.5
+    code += t > 5.0
+    code = (code + 8 * (y < 0)).flatten(-2).unflatten(-1, (-1, 2)).to(torch.uint8)
+    return code[..., 0] | (code[..., 1] << 4), (e[..., 0] + 127).to(torch.uint8)
+
+
+def _values(codes, scales):
+    """fp32 values of codes [.., D/2] and scales [.., D/32]."""
+    table = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], device="cuda")
+    c = torch.stack([codes & 15, codes >> 4], -1).flatten(-2)
+    v = table[(c & 7).long()] * (1.0 - 2.0 * (c >> 3))
+    s = (scales.int() << 23).view(torch.float32)                   # 2^(s - 127)
+    return (v.unflatten(-1, (-1, BLOCK)) * s[..., None]).flatten(-2)
+
+
+def _cached(cache, ids, ps, D):
+    """fp32 [positions, Hkv, D] of the pages `ids`."""
+    c = cache[ids]
+    codes = c[..., :ps * D // 2].unflatten(-1, (ps, -1))
+    scales = c[..., ps * D // 2:].unflatten(-1, (ps, -1))
+    return _values(codes, scales).transpose(1, 2).flatten(0, 1)
+
+
+def _places(st):
+    """(page, place in it) of every new token."""
+    case = st["case"]
+    N = int(st["new"].sum())
+    req = torch.repeat_interleave(torch.arange(case["B"], device="cuda"), st["new"].cuda())
+    pos = torch.arange(N, device="cuda") - st["cu_new"].long()[req] + st["ctx_lens"].long()[req]
+    return N, pos, st["page_table"].long()[req, pos // case["page"]], pos % case["page"]
+
+
+def _split_cache(cache, ps, D):
+    """The codes [pages, Hkv, ps, D/2] and scales [pages, Hkv, ps, D/32] of a cache, in place."""
+    n = ps * D // 2
+    return cache[..., :n].unflatten(-1, (ps, -1)), cache[..., n:].unflatten(-1, (ps, -1))
+
+
+def _plain_read(st):
+    D, ps = HEADS[st["case"]["shape"]]["D"], st["case"]["page"]
+    N, _, page, at = _places(st)
+    for name in "kv":
+        codes, scales = _split_cache(st[name + "_cache"], ps, D)
+        st[name + "_out"][:N] = _values(codes[page, :, at], scales[page, :, at]).to(st[name + "_out"].dtype)
+    return dict(k=st["k_out"], v=st["v_out"])
+
+
+def _plain_append(st):
+    case, h = st["case"], HEADS[st["case"]["shape"]]
+    Hq, Hkv, D, ps = h["Hq"], h["Hkv"], h["D"], case["page"]
+    N, pos, page, at = _places(st)
+    x = st["qkv"][:N].view(N, Hq + 2 * Hkv, D)
+    freq = torch.exp(-math.log(THETA) * 2.0 / D * torch.arange(D // 2, device="cuda", dtype=torch.float64))
+    phi = pos.double()[:, None] * freq
+    cos, sin = torch.cos(phi)[:, None], torch.sin(phi)[:, None]
+
+    def turned(y, w, c, s):
+        if w is not None:
+            y = y * torch.rsqrt((y * y).mean(-1, keepdim=True) + EPS) * w
+        a, b = y[..., :D // 2], y[..., D // 2:]
+        return torch.cat([a * c - b * s, b * c + a * s], -1)
+
+    st["q"][:N] = turned(x[:, :Hq].float(), st["q_norm_w"], cos.float(), sin.float()).to(st["q"].dtype)
+    k = turned(x[:, Hq:Hq + Hkv].double(), st["k_norm_w"], cos, sin)
+    for name, y in (("k", k), ("v", x[:, Hq + Hkv:])):
+        codes, scales = _split_cache(st[name + "_cache"], ps, D)
+        codes[page, :, at], scales[page, :, at] = _quantise(y)
+    return dict(q=st["q"], **_plain_read(st))
+
+
+def _plain_attn(st):
+    case, h = st["case"], HEADS[st["case"]["shape"]]
+    Hq, Hkv, D, ps = h["Hq"], h["Hkv"], h["D"], case["page"]
+    g, window, row = Hq // Hkv, case["window"], 0
+    for b, (L, n) in enumerate(zip(st["ctx"].tolist(), st["new"].tolist())):
+        held = L if case.get("dense") else L + n
+        ids = st["page_table"][b, :(held + ps - 1) // ps].long()
+        K, V = _cached(st["k_cache"], ids, ps, D)[:held], _cached(st["v_cache"], ids, ps, D)[:held]
+        if case.get("dense"):
+            K = torch.cat([K, st["k_new"][row:row + n].float()])
+            V = torch.cat([V, st["v_new"][row:row + n].float()])
+        K, V = K.permute(1, 2, 0).contiguous(), V.permute(1, 0, 2).contiguous()
+        s = torch.arange(L + n, device="cuda")
+        for i0 in range(0, n, 1024):
+            m = min(1024, n - i0)
+            pos = torch.arange(L + i0, L + i0 + m, device="cuda")[:, None]
+            seen = (s <= pos) | (case.get("dense") == "block")
+            if window:
+                seen &= s > pos - window
+            q = st["q"][row + i0:row + i0 + m].float().view(m, Hkv, g, D).permute(1, 2, 0, 3).reshape(Hkv, g * m, D)
+            sc = (torch.matmul(q, K) * D ** -0.5).view(Hkv, g, m, L + n).masked_fill_(~seen, float("-inf"))
+            e = torch.exp(sc - sc.amax(-1, keepdim=True))
+            o = torch.matmul(e.view(Hkv, g * m, L + n), V).view(Hkv, g, m, D) / e.sum(-1, keepdim=True)
+            st["o"][row + i0:row + i0 + m] = o.permute(2, 0, 1, 3).reshape(m, Hq, D).to(st["o"].dtype)
+        row += n
+    return st["o"]
+
+
+def _plain_adjust(st):
+    case, B, k, V, rows = st["case"], st["case"]["B"], st["case"]["k"], st["case"]["V"], st["rows"]
+    cu = st["cu_rows"].long()
+    req = torch.repeat_interleave(torch.arange(B, device="cuda"), cu[1:] - cu[:-1], output_size=rows)
+    at = torch.arange(st["history"].shape[1], device="cuda")
+    hist, one = st["history"].long(), torch.ones((), dtype=torch.int32, device="cuda")
+    old = at < st["prompt_lens"][:, None]
+    gen = ~old & (at < st["hist_lens"][:, None])
+    prompt = torch.zeros((B, V), dtype=torch.int32, device="cuda").scatter_add_(1, hist, (one * old))
+    said = torch.zeros((B, V), dtype=torch.int32, device="cuda").scatter_add_(1, hist, (one * gen))
+    count = said[req]
+    if k:
+        ids = st["draft_tokens"].long()
+        ids = ids if st["d2t"] is None else st["d2t"].long()[ids]
+        ahead = torch.arange(k, device="cuda") < (torch.arange(rows, device="cuda") - cu[req])[:, None]
+        count.scatter_add_(1, ids[req], one * ahead)
+    x = st["logits"].float()
+    if st["bias"] is not None:
+        full = torch.zeros((B, V), device="cuda").scatter_(1, st["bias_ids"].long(), st["bias"])
+        x = x + full[req]
+    rho = st["repetition"][req, None]
+    x = torch.where((count > 0) | (prompt[req] > 0), torch.where(x > 0, x / rho, x * rho), x)
+    x = x - st["frequency"][req, None] * count - st["presence"][req, None] * (count > 0)
+    if st["mask"] is not None:
+        state = st["mask_rows"].long()
+        word = st["mask"][state.clamp(min=0)]
+        bit = (word[..., None] >> torch.arange(32, device="cuda", dtype=torch.int32)) & 1
+        x = x.masked_fill((bit.flatten(-2)[:, :V] == 0) & (state >= 0)[:, None], float("-inf"))
+    st["out"][:rows] = x.to(st["out"].dtype)
+    return st["out"]
+
+
+_RUN_OWN = dict(attn=_own_attn, append=_own_append, read=_own_read, adjust=_own_adjust)
+_RUN_PLAIN = dict(attn=_plain_attn, append=_plain_append, read=_plain_read, adjust=_plain_adjust)
+
+
+# ------------------------------------------------------------------------- bounds, truth
+
+
+def _pairs(L, n, window, block):
+    """Visible (row, key) pairs of n new tokens behind L cached ones, and the cached keys any of them sees."""
+    w = window or 1 << 40
+    if block:
+        return sum(min(L, max(w - 1 - i, 0)) for i in range(n)) + n * n, min(L, w - 1)
+    if not window:
+        return n * L + n * (n + 1) / 2, L
+    full = max(0.0, min(n, window - L))                # rows that still see everything
+    return full * L + full * (full + 1) / 2 + (n - full) * window, min(L, window - 1)
+
+
+def work(case):
+    if case["kind"] == "adjust":
+        B, V = case["B"], case["V"]
+        rows = sum(_drafts(case)) + B
+        size = lambda name: 4 if name == "f32" else 2  # noqa: E731
+        b = rows * V * (size(case["dtype"]) + size(case["out"])) + 4 * sum(_lengths(B, case["hist"], "history"))
+        b += B * (8 * case["bias"] + 4 * case["k"] + 20)
+        if case["mask"]:
+            b += max(2, rows // 3) * ((V + 31) // 32) * 4 + rows * 4
+        return dict(bytes=b, flops=6 * rows * V)
+    h = HEADS[case["shape"]]
+    Hq, Hkv, D, e = h["Hq"], h["Hkv"], h["D"], 4 if h["dtype"] == "f32" else 2
+    reqs, held = _requests(case), 2 * Hkv * (D // 2 + D // BLOCK)   # bytes of a position in the cache
+    rows = sum(n for _, n in reqs)
+    if case["kind"] == "read":
+        return dict(bytes=rows * (held + 2 * Hkv * D * e), flops=rows * 2 * Hkv * D)
+    if case["kind"] == "append":
+        wide = (Hq + 2 * Hkv) * D
+        return dict(bytes=rows * (wide * (4 if case["rows"] == "f32" else 2) + (Hq + 2 * Hkv) * D * e + held),
+                    flops=rows * wide * 12)
+    dense = case.get("dense")
+    seen = [_pairs(L, n, case["window"], dense == "block") for L, n in reqs]
+    keys = sum(k for _, k in seen)
+    new = rows * 2 * Hkv * D * e if dense else rows * held
+    return dict(bytes=2 * rows * Hq * D * e + keys * (held + 4 / case["page"]) + new,
+                flops=4 * Hq * D * sum(pairs for pairs, _ in seen))
+
+
+def exact(case, seed):
+    if case["kind"] == "attn" and work(case)["flops"] > 4e12:
+        return None
+    with torch.no_grad():
+        return _EXACT[case["kind"]](prepare(case, seed))
+
+
+GRID = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
+
+
+def _unpack64(cache, page, at, ps, D):
+    """float64 [.., Hkv, D] of places (page, at)."""
+    grid = torch.tensor(GRID + tuple(-v for v in GRID), dtype=torch.float64, device="cuda")
+    raw = cache[page]
+    j = torch.arange(D, device="cuda")
+    byte = raw.gather(-1, (at[:, None, None] * (D // 2) + j // 2).expand(-1, raw.shape[1], -1)).int()
+    s = raw.gather(-1, (ps * (D // 2) + at[:, None, None] * (D // 32) + j // 32).expand(-1, raw.shape[1], -1)).double()
+    nib = torch.where(j % 2 == 1, torch.div(byte, 16, rounding_mode="floor"), byte % 16)
+    return grid[nib] * torch.pow(2.0, s - 127)
+
+
+def _round64(y):
+    """What 4 bits keep of y: the nearest multiple of each value's step, in scales of its 32 channels."""
+    b = y.reshape(*y.shape[:-1], -1, 32)
+    top = b.abs().amax(-1, keepdim=True)
+    e = torch.where(top > 0, torch.floor(torch.log2(top / 7)) + 1, torch.full_like(top, -126)).clamp(min=-126)
+    scale = torch.pow(2.0, e)
+    t = b / scale
+    step = torch.where(t.abs() < 2, 0.5, torch.where(t.abs() < 4, 1.0, 2.0))
+    return (torch.round(t / step) * step).clamp(-6, 6).mul(scale).reshape(y.shape)
+
+
+def _exact_rows(st):
+    ps, cu = st["case"]["page"], st["cu_new"].tolist()
+    for b in range(st["case"]["B"]):
+        pos = int(st["ctx_lens"][b]) + torch.arange(cu[b + 1] - cu[b], device="cuda")
+        yield b, slice(cu[b], cu[b + 1]), pos, st["page_table"][b].long()[torch.div(pos, ps, rounding_mode="floor")]
+
+
+def _exact_read(st):
+    D, ps = HEADS[st["case"]["shape"]]["D"], st["case"]["page"]
+    out = dict(k=st["k_out"].double(), v=st["v_out"].double())
+    for _, rows, pos, page in _exact_rows(st):
+        for name in "kv":
+            out[name][rows] = _unpack64(st[name + "_cache"], page, pos % ps, ps, D)
+    return out
+
+
+def _exact_append(st):
+    h = HEADS[st["case"]["shape"]]
+    Hq, Hkv, D = h["Hq"], h["Hkv"], h["D"]
+    out, half = dict(q=st["q"].double(), k=st["k_out"].double(), v=st["v_out"].double()), h["D"] // 2
+    rate = torch.tensor([THETA ** (-2.0 * p / D) for p in range(half)], dtype=torch.float64, device="cuda")
+    for _, rows, pos, _ in _exact_rows(st):
+        qkv = st["qkv"][rows].double().split([Hq * D, Hkv * D, Hkv * D], dim=1)
+        n = len(pos)
+        turn = torch.polar(torch.ones(n, half, dtype=torch.float64, device="cuda"), pos[:, None] * rate[None])
+        res = []
+        for part, heads, gain in ((qkv[0], Hq, st["q_norm_w"]), (qkv[1], Hkv, st["k_norm_w"])):
+            y = part.reshape(n, heads, D)
+            if gain is not None:
+                y = y / torch.sqrt(y.square().sum(-1, keepdim=True) / D + EPS) * gain.double()
+            z = torch.complex(y[..., :half], y[..., half:]) * turn[:, None, :]
+            res.append(torch.cat([z.real, z.imag], dim=-1))
+        out["q"][rows] = res[0]
+        out["k"][rows] = _round64(res[1])
+        out["v"][rows] = _round64(qkv[2].reshape(n, Hkv, D))
+    return out
+
+
+def _exact_attn(st):
+    case, h = st["case"], HEADS[st["case"]["shape"]]
+    Hq, Hkv, D, ps = h["Hq"], h["Hkv"], h["D"], case["page"]
+    g, w = Hq // Hkv, case["window"] or 1 << 40
+    out = st["o"].double()
+    cu = st["cu_new"].tolist()
+    for b in range(case["B"]):
+        n, L = cu[b + 1] - cu[b], int(st["ctx_lens"][b])
+        held = torch.arange(L if case.get("dense") else L + n, device="cuda")
+        page = st["page_table"][b].long()[torch.div(held, ps, rounding_mode="floor")]
+        Kall, Vall = (_unpack64(st[c], page, held % ps, ps, D) for c in ("k_cache", "v_cache"))
+        if case.get("dense"):
+            Kall, Vall = (torch.cat([x, st[c][cu[b]:cu[b + 1]].double()])
+                          for x, c in ((Kall, "k_new"), (Vall, "v_new")))
+        at = torch.arange(L + n, device="cuda")
+        step = max(1, (1 << 27) // (L + n))
+        for h0 in range(Hkv):
+            K, V = Kall[:, h0], Vall[:, h0]
+            for i in range(0, n, step):
+                j = min(n, i + step)
+                t = L + torch.arange(i, j, device="cuda")
+                hidden = at[None] <= t[:, None] - w
+                if case.get("dense") != "block":
+                    hidden |= at[None] > t[:, None]
+                for e in range(g):
+                    lg = torch.mm(st["q"][cu[b] + i:cu[b] + j, h0 * g + e].double(), K.t()) / math.sqrt(D)
+                    lg[hidden] = -math.inf
+                    out[cu[b] + i:cu[b] + j, h0 * g + e] = torch.mm(torch.softmax(lg, dim=-1), V)
+    return out
+
+
+def _exact_adjust(st):
+    case, B, V = st["case"], st["case"]["B"], st["case"]["V"]
+    cu, lens, old = st["cu_rows"].tolist(), st["hist_lens"].tolist(), st["prompt_lens"].tolist()
+    out = torch.empty((st["rows"], V), dtype=torch.float64, device="cuda")
+    for b in range(B):
+        said = st["history"][b, :lens[b]].long()
+        in_prompt = torch.zeros(V, dtype=torch.bool, device="cuda")
+        in_prompt[said[:old[b]]] = True
+        count = torch.bincount(said[old[b]:], minlength=V).double()
+        shift = torch.zeros(V, dtype=torch.float64, device="cuda")
+        if st["bias"] is not None:
+            shift[st["bias_ids"][b].long()] = st["bias"][b].double()
+        rho, phi, pi = (float(st[c][b]) for c in ("repetition", "frequency", "presence"))
+        for j in range(cu[b + 1] - cu[b]):
+            if j:
+                t = int(st["draft_tokens"][b, j - 1])
+                count[t if st["d2t"] is None else int(st["d2t"][t])] += 1
+            x = st["logits"][cu[b] + j].double() + shift
+            seen = in_prompt | (count > 0)
+            x[seen] = torch.where(x[seen] > 0, x[seen] / rho, x[seen] * rho)
+            x -= phi * count
+            x[count > 0] -= pi
+            if st["mask"] is not None and int(st["mask_rows"][cu[b] + j]) >= 0:
+                word = st["mask"][int(st["mask_rows"][cu[b] + j])].long() & 0xffffffff
+                bit = torch.bitwise_right_shift(word[:, None], torch.arange(32, device="cuda")) % 2
+                x[bit.reshape(-1)[:V] == 0] = -math.inf
+            out[cu[b] + j] = x
+    return out
+
+
+_EXACT = dict(attn=_exact_attn, append=_exact_append, read=_exact_read, adjust=_exact_adjust)
