@@ -1,10 +1,10 @@
 """The target's cache in 4 bits and its logits before verification, as cases that can be timed and compared.
 
-  append  hspec_chunk_append_q4: norm and RoPE of the new tokens' q and k, K and V rounded to 4-bit floats
-          with a power-of-two scale for every 32 channels, into the pages; then hspec_chunk_read_q4 of the
+  append  hspec_chunk_append_mx: norm and RoPE of the new tokens' q and k, K and V rounded to 4-bit floats
+          with a power-of-two scale for every 32 channels, into the pages; then hspec_chunk_read_mx of the
           same tokens, which gives what the cache now holds of them
-  read    hspec_chunk_read_q4: cached positions as dense rows
-  attn    hspec_chunk_attn_q4: attention of a ragged batch of new tokens over that cache; their own K and V
+  read    hspec_chunk_read_mx: cached positions as dense rows
+  attn    hspec_chunk_attn_mx: attention of a ragged batch of new tokens over that cache; their own K and V
           are in the cache, or beside it in full precision ("dense": the drafter's block, where every
           token of a block sees every other, or a causal one)
   adjust  hspec_adjust_logits: bias, penalties for tokens that were said before (the drafts ahead of a row
@@ -280,9 +280,9 @@ def _plan(st):
                                 st["page_table"].shape[1], st["pages"], code(h["dtype"]), window=case.get("window", 0),
                                 eps=EPS, rope_theta=THETA)
     if case["kind"] == "attn":
-        need = hspec.chunk_attn_q4_workspace(st["cfg"], st["max_len"])
+        need = hspec.chunk_attn_mx_workspace(st["cfg"], st["max_len"])
     else:
-        need = max(hspec.chunk_append_q4_workspace(st["cfg"]), hspec.chunk_read_q4_workspace(st["cfg"]))
+        need = max(hspec.chunk_append_mx_workspace(st["cfg"]), hspec.chunk_read_mx_workspace(st["cfg"]))
     st["ws"] = hspec.workspace(need)
 
 
@@ -298,21 +298,21 @@ def run(st):
 
 def _own_append(st):
     from paper_2609_24197_amd import hspec
-    hspec.chunk_append_q4(st["cfg"], st["qkv"], st["cu_new"], st["ctx_lens"], st["q"], st["k_cache"], st["v_cache"],
+    hspec.chunk_append_mx(st["cfg"], st["qkv"], st["cu_new"], st["ctx_lens"], st["q"], st["k_cache"], st["v_cache"],
                           st["page_table"], st["ws"], q_norm_w=st["q_norm_w"], k_norm_w=st["k_norm_w"])
     return dict(q=st["q"], **_own_read(st))
 
 
 def _own_read(st):
     from paper_2609_24197_amd import hspec
-    hspec.chunk_read_q4(st["cfg"], st["cu_new"], st["ctx_lens"], st["k_cache"], st["v_cache"], st["page_table"],
+    hspec.chunk_read_mx(st["cfg"], st["cu_new"], st["ctx_lens"], st["k_cache"], st["v_cache"], st["page_table"],
                         st["k_out"], st["v_out"], st["ws"])
     return dict(k=st["k_out"], v=st["v_out"])
 
 
 def _own_attn(st):
     from paper_2609_24197_amd import hspec
-    hspec.chunk_attn_q4(st["cfg"], st["q"], st["cu_new"], st["k_cache"], st["v_cache"], st["page_table"], st["ctx_lens"],
+    hspec.chunk_attn_mx(st["cfg"], st["q"], st["cu_new"], st["k_cache"], st["v_cache"], st["page_table"], st["ctx_lens"],
                         st["max_len"], st["o"], st["ws"], k_new=st["k_new"], v_new=st["v_new"],
                         block=st["case"].get("dense") == "block")
     return st["o"]
