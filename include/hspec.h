@@ -524,6 +524,99 @@ hspec_status hspec_verify(const hspec_verify_cfg* cfg, const void* target_logits
                           size_t ws_bytes, void* stream);
 size_t hspec_verify_workspace(const hspec_verify_cfg* cfg);
 
+/* ------------------------------------------------------------ the target's cache in 4 bits */
+
+/*
+ * Caches that hold K and V as 4-bit floats (0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign) in blocks of 32
+ * channels with a power-of-two scale each: 17 bytes per 32 channels instead of 64 in bf16.  Each of
+ * k_cache and v_cache is hspec_mx_cache_bytes(cfg) bytes, 16-byte aligned: [num_pages, Hkv] parts of
+ * page_size rows of D/2 bytes (channel 2i in the low half of byte i, code = index of the magnitude + 8
+ * if negative) and then page_size rows of D/32 scale bytes s: 2^(s - 127), 255 for a block of NaN.
+ * Pages, page tables, the batch's arrays, their checks and the errors are those of the target's side
+ * above; cfg.dtype is the type of q, o and the dense rows.
+ */
+size_t hspec_mx_cache_bytes(const hspec_chunk_cfg* cfg);
+
+/*
+ * hspec_chunk_append into such caches.  A block's scale is the smallest 2^e for which its largest
+ * magnitude is below 7 2^e, from 2^-126 to 2^125; each value becomes the nearest of those above, ties to the even
+ * code, the largest magnitudes 6 2^e.  K's norm and RoPE are 64-bit up to that rounding, and V enters as
+ * it is, so the codes are those of the formula.  A block with a value that is NaN or not finite in
+ * 32 bits becomes NaN.  Other arguments, q and errors as hspec_chunk_append.
+ */
+hspec_status hspec_chunk_append_mx(const hspec_chunk_cfg* cfg, hspec_dtype qkv_dtype, const void* qkv,
+                                   const float* q_norm_w, const float* k_norm_w, const int32_t* cu_new,
+                                   const int32_t* ctx_lens, void* q, void* k_cache, void* v_cache,
+                                   const int32_t* page_table, void* workspace, size_t ws_bytes, void* stream);
+size_t hspec_chunk_append_mx_workspace(const hspec_chunk_cfg* cfg);
+
+/*
+ * What the caches hold, as dense rows: k, v [T, Hkv, D] out, row i of request b the position ctx_lens[b] + i
+ * (append's tokens again, or any cached range with ctx_lens as its first position).  Values of a bf16 row are
+ * exact.  Positions whose page id is outside the pool read as zeros and set HSPEC_DEV_BAD_PAGE.
+ */
+hspec_status hspec_chunk_read_mx(const hspec_chunk_cfg* cfg, const int32_t* cu_new, const int32_t* ctx_lens,
+                                 const void* k_cache, const void* v_cache, const int32_t* page_table, void* k, void* v,
+                                 void* workspace, size_t ws_bytes, void* stream);
+size_t hspec_chunk_read_mx_workspace(const hspec_chunk_cfg* cfg);
+
+/*
+ * hspec_chunk_attn over such caches.  k_new, v_new NULL: the caches hold the new tokens already
+ * (hspec_chunk_append_mx).  Else [T, Hkv, D] in the storage dtype: the new tokens' K (after RoPE) and V,
+ * which are attended as they are, as positions ctx_lens[b] on, and of which the caches need hold nothing
+ * (max_pages * page_size bounds ctx_lens[b] alone): the drafter's block, for one.  flags:
+ * HSPEC_CHUNK_BLOCK, every new token of a request sees all of them, as the block of
+ * hspec_paged_attn does (needs k_new, v_new, and max_new <= window where there is one).  Precision, masked
+ * slots, rows that see nothing and the other arguments as hspec_chunk_attn: with bf16 storage the 4-bit values are
+ * widened exactly and multiplied as bf16, with fp32 as fp32.
+ */
+enum { HSPEC_CHUNK_BLOCK = 1u << 0 };
+hspec_status hspec_chunk_attn_mx(const hspec_chunk_cfg* cfg, const void* q, const int32_t* cu_new, const void* k_new,
+                                 const void* v_new, unsigned flags, const void* k_cache, const void* v_cache,
+                                 const int32_t* page_table, const int32_t* ctx_lens, int max_len, void* o,
+                                 void* workspace, size_t ws_bytes, void* stream);
+size_t hspec_chunk_attn_mx_workspace(const hspec_chunk_cfg* cfg, int max_len);
+
+/* ------------------------------------------------------------- logits before verification */
+
+/*
+ * Logits of the rows that hspec_verify takes, with the request's settings applied: request b has rows
+ * cu_rows[b] .. cu_rows[b+1]-1 of logits and out [rows, vocab] (or b (k+1) .. with cu_rows NULL), row j
+ * after j of its drafts.  For every token v, in 32 bits, rounded once to out_dtype:
+ *   x = logits[r, v] + bias                          (where v is in the request's list)
+ *   x = x > 0 ? x / repetition[b] : x repetition[b]  (where v was said, or stands in the prompt; a quotient is
+ *                                                     that by the rounded reciprocal)
+ *   x = x - (frequency[b] n + presence[b])           (where v was said n > 0 times)
+ *   x = -inf                                         (where the row's mask has no bit for v)
+ * Said are the tokens of the history behind the prompt, and the row's first j drafts.
+ *   history [B, max_hist] int32 with hist_lens [B], of which the first prompt_lens [B] (NULL: none) are the
+ *   prompt; ids outside [0, vocab) are skipped (padding).  draft_tokens [B, k], d2t as in hspec_verify.
+ *   repetition, frequency, presence [B] fp32, each may be NULL (1, 0, 0).  bias_ids, bias [B, n_bias]: ids
+ *   outside [0, vocab) are skipped; where an id stands several times, its last entry counts.
+ *   mask [masks, ceil(vocab/32)] int32, bit v % 32 of word v / 32 set where v may follow; mask_rows
+ *   [rows]: the row's line of it, below 0: none (NULL: row r has line r, masks = rows).
+ * NULL with a count of 0 leaves history, drafts, bias or mask out.  out may be logits (same dtype), and
+ * otherwise lies over no other argument.  Rows past cu_rows[B] are left as they were.  Checked on the device:
+ * cu_rows as in hspec_verify (HSPEC_DEV_BAD_ROWS; a row of several ranges is one of their requests'); a length
+ * outside [0, max_hist], or a prompt's outside [0, its history's], is clamped (HSPEC_DEV_BAD_CTX_LEN); a draft
+ * ahead of some row without a target id is not counted (HSPEC_DEV_BAD_TOKEN); mask_rows >= masks is none
+ * (HSPEC_DEV_BAD_ROWS); a repetition outside [2^-64, 2^64], or another penalty that is NaN or beyond +-2^64,
+ * counts as none (HSPEC_DEV_NONFINITE).  Logits that are not finite follow the arithmetic.  Limits as
+ * hspec_verify; k may be 0.
+ */
+typedef struct {
+  int B, k, rows, vocab, draft_vocab, max_hist, n_bias, masks;
+  hspec_dtype dtype, out_dtype;
+} hspec_adjust_cfg;
+
+hspec_status hspec_adjust_logits(const hspec_adjust_cfg* cfg, const void* logits, const int32_t* cu_rows,
+                                 const int32_t* draft_tokens, const int32_t* d2t, const int32_t* history,
+                                 const int32_t* hist_lens, const int32_t* prompt_lens, const float* repetition,
+                                 const float* frequency, const float* presence, const int32_t* bias_ids,
+                                 const float* bias, const int32_t* mask, const int32_t* mask_rows, void* out,
+                                 void* workspace, size_t ws_bytes, void* stream);
+size_t hspec_adjust_logits_workspace(const hspec_adjust_cfg* cfg);
+
 /* ------------------------------------------------------------------------- utilities */
 
 /* Copies the device status word of `workspace` to *status after synchronising `stream`. */

@@ -1,0 +1,33 @@
+// Attention of a ragged chunk of new tokens over the 4-bit paged cache (mx.h): the units, tiles and merge of the other
+// caches' (chunk_tile.h), with K and V widened to the type of q on their way into LDS.  The new tokens' own K and V are
+// in the cache, or beside it as they are, where their keys follow the cached ones.
+#include "chunk_tile.h"
+
+namespace hspec {
+namespace {
+
+template <class F>
+auto with_variant(const ChunkAttnArgs& a, F f) {
+  auto by_rows = [&](auto t, auto d) {
+    typedef typename decltype(t)::type T;
+    constexpr int D = decltype(d)::value;
+    constexpr bool F32 = sizeof(T) == 4;
+    constexpr int KT4 = chunk_key_tile(4, F32);
+    if (a.tile_rows == 32) return f(Chunk<T, D, 1, chunk_key_tile(1, F32), true, true>{});
+    if constexpr (F32)
+      if (a.tile_rows == 64) return f(Chunk<T, D, 2, chunk_key_tile(2, F32), true, true>{});
+    return a.once ? f(Chunk<T, D, 4, KT4, true, true>{}) : f(Chunk<T, D, 4, KT4, false, true>{});
+  };
+  if (a.f32) return a.D == 128 ? by_rows(std::common_type<float>{}, Int<128>{}) : by_rows(std::common_type<float>{}, Int<64>{});
+  return a.D == 128 ? by_rows(std::common_type<bf16>{}, Int<128>{}) : by_rows(std::common_type<bf16>{}, Int<64>{});
+}
+
+}  // namespace
+
+hipError_t launch_chunk_attn_mx(const ChunkAttnArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL(chunk_plan, dim3(1), dim3(PL_THREADS), 0, s, a);
+  if (hipError_t e = hipGetLastError()) return e;
+  return with_variant(a, [&](auto c) { return launch_units<decltype(c)>(a, s); });
+}
+
+}  // namespace hspec

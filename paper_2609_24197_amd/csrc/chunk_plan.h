@@ -30,7 +30,7 @@ __device__ __forceinline__ TileKeys tile_keys(const ChunkAttnArgs& a, int g, int
   const int c0 = tile * a.tile_rows;
   const int t0 = c0 / g, t1 = (int)min((long long)c0 + a.tile_rows, (long long)n * g) - 1;
   TileKeys r;
-  r.k1 = min(L + t1 / g + 1, a.cap);
+  r.k1 = min(L + (a.block ? n : t1 / g + 1), a.cap);
   r.k0 = a.window > 0 ? max(L + t0 - a.window + 1, 0) / a.key_tile * a.key_tile : 0;
   return r;
 }
@@ -66,7 +66,7 @@ __global__ void __launch_bounds__(PL_THREADS) chunk_plan(ChunkAttnArgs a) {
       if (b < a.B) {
         ChunkRows r = clamp_rows(start, max(to, start), a.T, a.max_new);
         r.ok = r.ok && start == from && to >= from && (b > 0 || from == 0);
-        const ChunkPos p = chunk_pos(len, r.n, a.cap);
+        const ChunkPos p = chunk_pos(len, r.n, a.cap, a.held);
         if (!r.ok || !p.ok) atomicOr(&s.bits, (r.ok ? 0 : ST_BAD_ROWS) | (p.ok ? 0 : ST_BAD_CTX_LEN));
         s.row0[tid] = r.row0;
         s.n[tid] = r.n;

@@ -1,0 +1,72 @@
+// The 4-bit cache: K and V as 4-bit floats (sign, 0 0.5 1 1.5 2 3 4 6) in blocks of 32 channels that share a power of
+// two.  For each page and KV head: page_size rows of D / 2 bytes (channel 2i in the low half of byte i), then page_size
+// rows of D / 32 scale bytes s, 2^(s - 127), 255 for a block that is NaN.  A head's part of a page is one run of memory,
+// so that a unit of attention, which takes one head, reads whole lines.
+#pragma once
+#include "common.h"
+
+namespace hspec {
+namespace {
+
+constexpr int MX_BLOCK = 32;
+
+__host__ __device__ inline size_t mx_head_bytes(int ps, int D) { return (size_t)ps * (D / 2 + D / MX_BLOCK); }
+
+struct MxBlock {
+  u32x4 code;        // 8 channels a word
+  unsigned scale;    // the byte
+};
+// Block c of row `row` of a head's part of a page.
+__device__ __forceinline__ MxBlock mx_load(const uint8_t* p, int ps, int D, int row, int c) {
+  MxBlock b;
+  b.code = *reinterpret_cast<const u32x4*>(p + row * (D / 2) + c * (MX_BLOCK / 2));
+  b.scale = p[ps * (D / 2) + row * (D / MX_BLOCK) + c];
+  return b;
+}
+
+// 8 channels of a word as bf16 and as fp32: exact (the conversions take 2^(s - 127) as the exponent of a float, 0 and 255
+// too).
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ bf16x8 mx_widen(unsigned code, unsigned scale) {
+  const float s = __uint_as_float(scale << 23);
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 1);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 3);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+__device__ __forceinline__ void mx_widen(unsigned code, unsigned scale, f32x4& lo, f32x4& hi) {
+  const float s = __uint_as_float(scale << 23);
+  const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, s, 1);
+  const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, s, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, s, 3);
+  lo = f32x4{a[0], a[1], b[0], b[1]};
+  hi = f32x4{c[0], c[1], d[0], d[1]};
+}
+
+// Scale byte of a block whose largest magnitude is `top` (finite): the smallest 2^e with top < 7 2^e, so that no value
+// is cut by more than half a step of the next binade; from 2^-126 to 2^125, so that what is finite in 32 bits stays it.
+// Only top's bits decide.
+__device__ __forceinline__ unsigned mx_scale(float top) {
+  const unsigned u = __float_as_uint(top);
+  const int s = (int)(u >> 23) - 2 + ((u & 0x7fffff) >= 0x600000 ? 1 : 0);   // top = 1.m 2^(E - 127)
+  return (unsigned)(s < 1 ? 1 : s > 252 ? 252 : s);
+}
+__device__ __forceinline__ unsigned mx_scale(double top) {
+  const unsigned long long u = (unsigned long long)__double_as_longlong(top);
+  const int s = (int)(u >> 52) - 1023 + 127 - 2 + ((u & 0xfffffffffffffULL) >= 0xc000000000000ULL ? 1 : 0);
+  return (unsigned)(s < 1 ? 1 : s > 252 ? 252 : s);
+}
+// Code of y under the scale byte s: the nearest value, ties to the even code.  (Scaling by a power of two is exact, or
+// the result is far below the first border.)
+__device__ __forceinline__ unsigned mx_code(float y, unsigned s) {
+  const float t = fabsf(y) * __uint_as_float((254u - s) << 23);
+  const unsigned c = (t > 0.25f) + (t >= 0.75f) + (t > 1.25f) + (t >= 1.75f) + (t > 2.5f) + (t >= 3.5f) + (t > 5.f);
+  return c | (__float_as_uint(y) >> 31 << 3);
+}
+__device__ __forceinline__ unsigned mx_code(double y, unsigned s) {
+  const double t = fabs(y) * __longlong_as_double((long long)(1023 + 127 - (int)s) << 52);
+  const unsigned c = (t > 0.25) + (t >= 0.75) + (t > 1.25) + (t >= 1.75) + (t > 2.5) + (t >= 3.5) + (t > 5.);
+  return c | ((unsigned)(__double_as_longlong(y) >> 63) & 8u);
+}
+
+}  // namespace
+}  // namespace hspec

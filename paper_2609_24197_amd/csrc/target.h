@@ -25,6 +25,9 @@ struct ChunkAppendArgs {
   int in_f32 = 1, out_f32 = 0;
 };
 hipError_t launch_chunk_append(const ChunkAppendArgs& a, hipStream_t s);
+// 4-bit caches: append; rows of the cache out to k, v [T, Hkv, D] (of `a`: the batch, the caches, out_f32)
+hipError_t launch_chunk_append_mx(const ChunkAppendArgs& a, hipStream_t s);
+hipError_t launch_chunk_read_mx(const ChunkAppendArgs& a, void* k, void* v, hipStream_t s);
 
 // --------------------------------------------------------------------------- attention
 // One piece of work of every KV head: `row0`, `n`, `L` are the request's checked first row, number of new
@@ -49,6 +52,10 @@ struct ChunkAttnArgs {
   int window = 0, f32 = 0;
   int cap = 0;                        // positions a request can have: min(max_len, max_pages ps)
   float scale_log2 = 0.f;
+  // 4-bit caches: K and V of the new tokens [T, Hkv, D] beside the cache, or null; `block`: every new token of a
+  // request sees every other; `held`: positions the cache has room for
+  const void *k_new = nullptr, *v_new = nullptr;
+  int block = 0, held = INT_MAX;
   int* status = nullptr;              // [0] status, [1] units, [2] split tiles, [3] items to do again
   int* queue = nullptr;               // [kChunkClasses * kChunkQueueStride]
   ChunkUnit* units = nullptr;
@@ -118,6 +125,7 @@ inline void chunk_bounds(ChunkAttnArgs& a) {
   a.max_redo = a.max_units * a.Hkv * waves;   // an entry for every wave
 }
 hipError_t launch_chunk_attn(const ChunkAttnArgs& a, hipStream_t s);
+hipError_t launch_chunk_attn_mx(const ChunkAttnArgs& a, hipStream_t s);
 
 // ------------------------------------------------------------------------ verification
 // A row's largest logit, and log2 of the sum of 2^((l - m) c).
@@ -163,5 +171,22 @@ inline void verify_bounds(VerifyArgs& a) {
   a.pieces_r = (int)std::max(1LL, std::min({1024LL / a.B, a.V / 4096LL, 64LL}));
 }
 hipError_t launch_verify(const VerifyArgs& a, hipStream_t s);
+
+// -------------------------------------------------------------------------- adjustment
+struct AdjustArgs {
+  const void* logits = nullptr;       // [rows, V]
+  void* out = nullptr;
+  const int32_t *cu = nullptr, *draft_tokens = nullptr, *d2t = nullptr;
+  const int32_t *history = nullptr, *hist_lens = nullptr, *prompt_lens = nullptr;   // [B, max_hist], [B]
+  const float *repetition = nullptr, *frequency = nullptr, *presence = nullptr;     // [B] or null
+  const int32_t* bias_ids = nullptr;  // [B, n_bias]
+  const float* bias = nullptr;
+  const uint32_t* mask = nullptr;     // [masks, words of V bits]
+  const int32_t* mask_rows = nullptr; // [rows] or null: row r's is r
+  int B = 0, k = 0, rows = 0, V = 0, Vd = 0, max_hist = 0, n_bias = 0, masks = 0;
+  int in_f32 = 0, out_f32 = 0;
+  int* status = nullptr;
+};
+hipError_t launch_adjust(const AdjustArgs& a, hipStream_t s);
 
 }  // namespace hspec

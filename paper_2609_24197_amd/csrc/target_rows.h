@@ -1,6 +1,7 @@
 // Which rows of a ragged batch belong to which request, checked: shared by the kernels that take one.
 #pragma once
 #include <hip/hip_runtime.h>
+#include <limits.h>
 #include <stdint.h>
 
 namespace hspec {
@@ -25,14 +26,14 @@ __device__ __forceinline__ ChunkRows chunk_rows(const int32_t* cu, int b, int T,
   return r;
 }
 
-// Cached length of a request that takes n new tokens, in a cache that holds cap positions.
+// Cached length of a request that takes n new tokens: at most cap positions in all, and `held` of them cached.
 struct ChunkPos {
   int L;
   bool ok;
 };
-__device__ __forceinline__ ChunkPos chunk_pos(int L, int n, int cap) {
+__device__ __forceinline__ ChunkPos chunk_pos(int L, int n, int cap, int held = INT_MAX) {
   ChunkPos p;
-  const int top = max(cap - n, 0);
+  const int top = min(max(cap - n, 0), held);
   p.ok = L >= 0 && n <= cap && L <= top;
   p.L = min(max(L, 0), top);
   return p;

@@ -20,6 +20,7 @@ _lib = None
 BF16, F32 = 0, 1
 BLOCK_CAUSAL = 1
 ATTN_PRECISE_IO = 2
+CHUNK_BLOCK = 1
 W_DS_PACKED = 1
 MAMBA_PRECISE_IO = 2
 DEV_BAD_PAGE, DEV_BAD_CTX_LEN, DEV_BAD_TOKEN, DEV_NONFINITE, DEV_BAD_ROWS = 1, 2, 4, 8, 16
@@ -72,6 +73,11 @@ class ChunkCfg(C.Structure):
 class VerifyCfg(C.Structure):
     _fields_ = [(n, C.c_int) for n in ("B", "k", "rows", "vocab", "draft_vocab")] + [
         ("dtype", C.c_int), ("temperature", C.c_float), ("draft_temperature", C.c_float)]
+
+
+class AdjustCfg(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("B", "k", "rows", "vocab", "draft_vocab", "max_hist", "n_bias", "masks", "dtype",
+                                        "out_dtype")]
 
 
 class HspecError(RuntimeError):
@@ -127,6 +133,16 @@ EXPORTS = {
     "hspec_chunk_attn_workspace": (C.c_size_t, [C.POINTER(ChunkCfg), C.c_int]),
     "hspec_verify": (C.c_int, [C.POINTER(VerifyCfg)] + [C.c_void_p] * 11 + [C.c_size_t, C.c_void_p]),
     "hspec_verify_workspace": (C.c_size_t, [C.POINTER(VerifyCfg)]),
+    "hspec_mx_cache_bytes": (C.c_size_t, [C.POINTER(ChunkCfg)]),
+    "hspec_chunk_append_mx": (C.c_int, [C.POINTER(ChunkCfg), C.c_int] + [C.c_void_p] * 10 + [C.c_size_t, C.c_void_p]),
+    "hspec_chunk_append_mx_workspace": (C.c_size_t, [C.POINTER(ChunkCfg)]),
+    "hspec_chunk_read_mx": (C.c_int, [C.POINTER(ChunkCfg)] + [C.c_void_p] * 8 + [C.c_size_t, C.c_void_p]),
+    "hspec_chunk_read_mx_workspace": (C.c_size_t, [C.POINTER(ChunkCfg)]),
+    "hspec_chunk_attn_mx": (C.c_int, [C.POINTER(ChunkCfg)] + [C.c_void_p] * 4 + [C.c_uint] + [C.c_void_p] * 4 +
+                            [C.c_int, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "hspec_chunk_attn_mx_workspace": (C.c_size_t, [C.POINTER(ChunkCfg), C.c_int]),
+    "hspec_adjust_logits": (C.c_int, [C.POINTER(AdjustCfg)] + [C.c_void_p] * 16 + [C.c_size_t, C.c_void_p]),
+    "hspec_adjust_logits_workspace": (C.c_size_t, [C.POINTER(AdjustCfg)]),
     "hspec_pack_w_ds_bytes": (C.c_size_t, [C.c_int, C.c_int]),
     "hspec_pack_w_ds": (C.c_int, [C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p]),
     "hspec_read_status": (C.c_int, [C.c_void_p, C.POINTER(C.c_int32), C.c_void_p]),
@@ -510,3 +526,88 @@ def verify(vc: VerifyCfg, target_logits, draft_tokens, tokens, n_accepted, ws, d
          _arg("cu_rows", cu_rows, i32, (B + 1,), dev), _arg("d2t", d2t, i32, (Vd,), dev), _arg("t2d", t2d, i32, (V,), dev),
          _arg("u", u, f32, (B, k), dev), _arg("gumbel", gumbel, f32, (B, V), dev),
          _arg("tokens", tokens, i32, (B, k + 1), dev), _arg("n_accepted", n_accepted, i32, (B,), dev))
+
+
+# ------------------------------------------------------------ the target's cache in 4 bits
+
+def mx_cache_shape(cc: ChunkCfg) -> tuple:
+    """Shape of a 4-bit cache (uint8): for each page and KV head the rows' codes, then their scales."""
+    return cc.num_pages, cc.Hkv, cc.page_size * (cc.D // 2 + cc.D // 32)
+
+
+def chunk_append_mx_workspace(cc: ChunkCfg) -> int:
+    return lib().hspec_chunk_append_mx_workspace(C.byref(cc))
+
+
+def chunk_append_mx(cc: ChunkCfg, qkv, cu_new, ctx_lens, q, k_cache, v_cache, page_table, ws, q_norm_w=None, k_norm_w=None):
+    """Norm and RoPE of the new tokens' q and k; q out, K and V in 4 bits into the pages (hspec_chunk_append_mx)."""
+    torch = _torch()
+    dev, i32, f32, u8, st = _dev(), torch.int32, torch.float32, torch.uint8, _storage(cc.dtype)
+    B, T, Hq, Hkv, D, pool = cc.B, cc.T, cc.Hq, cc.Hkv, cc.D, mx_cache_shape(cc)
+    code = F32 if qkv.dtype is f32 else BF16
+    _run(lib().hspec_chunk_append_mx, dev, ws, C.byref(cc), code,
+         _arg("qkv", qkv, _storage(code), (T, (Hq + 2 * Hkv) * D), dev), _arg("q_norm_w", q_norm_w, f32, (D,), dev),
+         _arg("k_norm_w", k_norm_w, f32, (D,), dev), _arg("cu_new", cu_new, i32, (B + 1,), dev),
+         _arg("ctx_lens", ctx_lens, i32, (B,), dev), _arg("q", q, st, (T, Hq, D), dev),
+         _arg("k_cache", k_cache, u8, pool, dev), _arg("v_cache", v_cache, u8, pool, dev),
+         _arg("page_table", page_table, i32, (B, cc.max_pages), dev))
+
+
+def chunk_read_mx_workspace(cc: ChunkCfg) -> int:
+    return lib().hspec_chunk_read_mx_workspace(C.byref(cc))
+
+
+def chunk_read_mx(cc: ChunkCfg, cu_new, ctx_lens, k_cache, v_cache, page_table, k, v, ws):
+    """k, v [T, Hkv, D] = what the 4-bit caches hold at the rows' positions (hspec_chunk_read_mx)."""
+    torch = _torch()
+    dev, i32, u8, st = _dev(), torch.int32, torch.uint8, _storage(cc.dtype)
+    B, pool, rows = cc.B, mx_cache_shape(cc), (cc.T, cc.Hkv, cc.D)
+    _run(lib().hspec_chunk_read_mx, dev, ws, C.byref(cc), _arg("cu_new", cu_new, i32, (B + 1,), dev),
+         _arg("ctx_lens", ctx_lens, i32, (B,), dev), _arg("k_cache", k_cache, u8, pool, dev),
+         _arg("v_cache", v_cache, u8, pool, dev), _arg("page_table", page_table, i32, (B, cc.max_pages), dev),
+         _arg("k", k, st, rows, dev), _arg("v", v, st, rows, dev))
+
+
+def chunk_attn_mx_workspace(cc: ChunkCfg, max_len: int) -> int:
+    return lib().hspec_chunk_attn_mx_workspace(C.byref(cc), int(max_len))
+
+
+def chunk_attn_mx(cc: ChunkCfg, q, cu_new, k_cache, v_cache, page_table, ctx_lens, max_len: int, o, ws, k_new=None,
+                  v_new=None, block=False):
+    """o [T, Hq, D] = attention of the new tokens over the 4-bit paged cache, their own K and V in it or beside it
+    (hspec_chunk_attn_mx); block: every new token of a request sees all of them."""
+    torch = _torch()
+    dev, i32, u8, st = _dev(), torch.int32, torch.uint8, _storage(cc.dtype)
+    B, rows, new, pool = cc.B, (cc.T, cc.Hq, cc.D), (cc.T, cc.Hkv, cc.D), mx_cache_shape(cc)
+    _run(lib().hspec_chunk_attn_mx, dev, ws, C.byref(cc), _arg("q", q, st, rows, dev),
+         _arg("cu_new", cu_new, i32, (B + 1,), dev), _arg("k_new", k_new, st, new, dev), _arg("v_new", v_new, st, new, dev),
+         CHUNK_BLOCK if block else 0, _arg("k_cache", k_cache, u8, pool, dev), _arg("v_cache", v_cache, u8, pool, dev),
+         _arg("page_table", page_table, i32, (B, cc.max_pages), dev), _arg("ctx_lens", ctx_lens, i32, (B,), dev),
+         int(max_len), _arg("o", o, st, rows, dev))
+
+
+# ------------------------------------------------------------- logits before verification
+
+def adjust_cfg(B, k, rows, vocab, draft_vocab=0, max_hist=0, n_bias=0, masks=0, dtype=BF16, out_dtype=BF16) -> AdjustCfg:
+    return AdjustCfg(B, k, rows, vocab, draft_vocab, max_hist, n_bias, masks, dtype, out_dtype)
+
+
+def adjust_logits_workspace(ac: AdjustCfg) -> int:
+    return lib().hspec_adjust_logits_workspace(C.byref(ac))
+
+
+def adjust_logits(ac: AdjustCfg, logits, out, ws, cu_rows=None, draft_tokens=None, d2t=None, history=None, hist_lens=None,
+                  prompt_lens=None, repetition=None, frequency=None, presence=None, bias_ids=None, bias=None, mask=None,
+                  mask_rows=None):
+    """out [rows, vocab] = logits with bias, penalties and mask (hspec_adjust_logits); out may be logits."""
+    torch = _torch()
+    dev, i32, f32 = _dev(), torch.int32, torch.float32
+    B, V = ac.B, ac.vocab
+    _run(lib().hspec_adjust_logits, dev, ws, C.byref(ac), _arg("logits", logits, _storage(ac.dtype), (ac.rows, V), dev),
+         _arg("cu_rows", cu_rows, i32, (B + 1,), dev), _arg("draft_tokens", draft_tokens, i32, (B, ac.k), dev),
+         _arg("d2t", d2t, i32, (ac.draft_vocab,), dev), _arg("history", history, i32, (B, ac.max_hist), dev),
+         _arg("hist_lens", hist_lens, i32, (B,), dev), _arg("prompt_lens", prompt_lens, i32, (B,), dev),
+         _arg("repetition", repetition, f32, (B,), dev), _arg("frequency", frequency, f32, (B,), dev),
+         _arg("presence", presence, f32, (B,), dev), _arg("bias_ids", bias_ids, i32, (B, ac.n_bias), dev),
+         _arg("bias", bias, f32, (B, ac.n_bias), dev), _arg("mask", mask, i32, (ac.masks, (V + 31) // 32), dev),
+         _arg("mask_rows", mask_rows, i32, (ac.rows,), dev), _arg("out", out, _storage(ac.out_dtype), (ac.rows, V), dev))
