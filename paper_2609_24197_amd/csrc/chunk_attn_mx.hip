@@ -1,6 +1,7 @@
 // Attention of a ragged chunk of new tokens over the 4-bit paged cache (mx.h): the units, tiles and merge of the other
 // caches' (chunk_tile.h), with K and V widened to the type of q on their way into LDS.  The new tokens' own K and V are
 // in the cache, or beside it as they are, where their keys follow the cached ones.
+#include "chunk_few.h"
 #include "chunk_tile.h"
 
 namespace hspec {
@@ -13,11 +14,19 @@ auto with_variant(const ChunkAttnArgs& a, F f) {
     constexpr int D = decltype(d)::value;
     constexpr bool F32 = sizeof(T) == 4;
     constexpr int KT4 = chunk_key_tile(4, F32);
-    if (a.tile_rows == 32) return f(Chunk<T, D, 1, chunk_key_tile(1, F32), true, true>{});
-    if constexpr (F32)
+    if constexpr (F32) {   // (bf16 has more rows than that)
+      if (a.tile_rows == 32) return f(Chunk<T, D, 1, chunk_key_tile(1, F32), true, true>{});
       if (a.tile_rows == 64) return f(Chunk<T, D, 2, chunk_key_tile(2, F32), true, true>{});
+    }
     return a.once ? f(Chunk<T, D, 4, KT4, true, true>{}) : f(Chunk<T, D, 4, KT4, false, true>{});
   };
+  auto few = [&](auto d) {
+    constexpr int D = decltype(d)::value;
+    const MxTile t = mx_tile(a);
+    if (t.waves == 1) return t.ct == 1 ? f(Few<D, 1, 1, true>{}) : t.ct == 2 ? f(Few<D, 2, 1, true>{}) : f(Few<D, 3, 1, true>{});
+    return t.ct == 2 ? f(Few<D, 2, 2, true>{}) : f(Few<D, 3, 2, true>{});
+  };
+  if (mx_tile(a).ct) return a.D == 128 ? few(Int<128>{}) : few(Int<64>{});
   if (a.f32) return a.D == 128 ? by_rows(std::common_type<float>{}, Int<128>{}) : by_rows(std::common_type<float>{}, Int<64>{});
   return a.D == 128 ? by_rows(std::common_type<bf16>{}, Int<128>{}) : by_rows(std::common_type<bf16>{}, Int<64>{});
 }

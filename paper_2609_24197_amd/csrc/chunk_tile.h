@@ -50,6 +50,7 @@ struct Chunk {
   static constexpr int GR = WROWS < 16 ? WROWS : 16;   // of them in one page for certain
   static constexpr int NG = WROWS / GR;
   static constexpr int NI = GR * CPR / 64;         // DMA instructions per group and tensor
+  static constexpr int STAGE = 2 * TILE, STAGE1 = 2 * TILE;   // elements of LDS: K and V of two tiles
   static constexpr int WPE = chunk_waves_per_simd(sizeof(T) == 4, D);   // waves per SIMD the registers are sized for
   static_assert(KT % 32 == 0 && GR * CPR % 64 == 0 && WROWS % GR == 0, "tile shape");
 };
@@ -479,14 +480,20 @@ __device__ __forceinline__ bool chunk_unit(const ChunkAttnArgs& a, const ChunkUn
   return bad;
 }
 
+template <bool ODD, class T, int D, int NW, int KT, bool ONCE, bool MX>
+__device__ __forceinline__ bool run_unit(Chunk<T, D, NW, KT, ONCE, MX>, const ChunkAttnArgs& a, const ChunkUnit& u, int h, T* st0,
+                                         T* st1) {
+  return chunk_unit<Chunk<T, D, NW, KT, ONCE, MX>, ODD>(a, u, h, st0, st1);
+}
+
 template <class C>
 // (256 threads for every NW: with fewer the compiler counts on one wave per SIMD and puts O into accumulation
 // registers, which costs a copy of it both ways in every tile)
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(C::WPE)))
 chunk_attn_kernel(ChunkAttnArgs a) {
   // one LDS object per stage, so that the compiler can tell the one being read from the one whose DMA is in flight
-  __shared__ __align__(16) typename C::T st0[2 * C::TILE];
-  __shared__ __align__(16) typename C::T st1[2 * C::TILE];
+  __shared__ __align__(16) typename C::T st0[C::STAGE];
+  __shared__ __align__(16) typename C::T st1[C::STAGE1];
   __shared__ int s_item[2];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -539,7 +546,7 @@ chunk_attn_kernel(ChunkAttnArgs a) {
     int ticket = 0;
     if (tid == 0 && !one_each) ticket = atomicAdd(counter(cls), 1);
     const int h = item % a.Hkv;
-    const bool bad = chunk_unit<C, false>(a, u, h, st0, st1);
+    const bool bad = run_unit<false>(C{}, a, u, h, st0, st1);
     // (one entry a wave at most: the same item twice is done twice, with the same result)
     if (a.redo && __any(bad) && lane == 0) {
       const int at = atomicAdd(a.status + 3, 1);
@@ -560,13 +567,13 @@ chunk_attn_kernel(ChunkAttnArgs a) {
 // empty where V is finite and nothing overflows).
 template <class C>
 __global__ void __launch_bounds__(C::NT) chunk_redo_kernel(ChunkAttnArgs a) {
-  __shared__ __align__(16) typename C::T st0[2 * C::TILE];
-  __shared__ __align__(16) typename C::T st1[2 * C::TILE];
+  __shared__ __align__(16) typename C::T st0[C::STAGE];
+  __shared__ __align__(16) typename C::T st1[C::STAGE1];
   const int n = min(a.status[3], a.max_redo);
   for (int i = blockIdx.x; i < n; i += gridDim.x) {
     const int item = a.redo[i];
     const ChunkUnit u = a.units[item / a.Hkv];
-    chunk_unit<C, true>(a, u, item % a.Hkv, st0, st1);
+    run_unit<true>(C{}, a, u, item % a.Hkv, st0, st1);
     __syncthreads();
   }
 }

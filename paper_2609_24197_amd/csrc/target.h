@@ -94,23 +94,10 @@ __host__ __device__ inline int chunk_pieces(int len, int S, int key_tile, int& q
   return (int)(((unsigned)len + q - 1) / (unsigned)q);
 }
 
-// Tile of the units, and the most units, partial slots and split tiles the plan can make of any lengths.  32 rows per
-// wave; past four waves a request has several tiles (once = 0).  fp32 takes one, two or four waves by the rows a request
-// can have (n g): its key tile and LDS are the same for all, so waves without rows only keep others out (64 requests of
-// 512..8192 cached, 16 and 4 heads of 128: 1 token 484 us, 888 with four; 3 tokens 489 and 895).  bf16 takes four, whose
-// idle waves still load (32 and 8 heads of 128: 1 request of 1 token and 16000 cached 32 us, 36 with one; 200 of at most
-// 3000 cached 218 and 224), but one for up to 32 rows over many long caches, where small workgroups keep more of them
-// reading (64 requests of 1 token and 512..8192 cached 212 us, 223 with four).
-inline void chunk_bounds(ChunkAttnArgs& a) {
+// What the plan's bounds come to for a tile and its workgroups (chunk_bounds and mx_bounds).
+inline void plan_bounds(ChunkAttnArgs& a, int waves) {
   const long long g = a.Hq / a.Hkv, R = a.max_new * g;
-  const bool many_long = a.cap >= 4096 && (long long)a.B * a.Hkv >= 32;
-  const int waves = R <= 32 && (a.f32 || many_long) ? 1 : R <= 64 && a.f32 ? 2 : 4;
-  a.tile_rows = 32 * waves;
   a.once = R <= a.tile_rows;
-  a.key_tile = chunk_key_tile(waves, a.f32);
-  // workgroups that run at once on 256 compute units: LDS (two stages of K and V) goes in 128 pieces of 1280 bytes
-  const int lds = (4 * a.key_tile * a.D * (a.f32 ? 4 : 2) + 8 + 1279) / 1280;
-  a.slots = std::min(128 / lds, 4 * chunk_waves_per_simd(a.f32, a.D) / waves) * 256;
   a.target = a.slots * 13 / 8;
   a.min_split = kChunkMinSplit;
   const long long per_req = (R + a.tile_rows - 1) / a.tile_rows;
@@ -123,6 +110,43 @@ inline void chunk_bounds(ChunkAttnArgs& a) {
   a.max_slots = cuts > 1 ? (int)std::min(tiles * cuts, 2 * extra) : 0;
   a.max_splits = (int)std::min(tiles, (long long)a.max_slots / 2);
   a.max_redo = a.max_units * a.Hkv * waves;   // an entry for every wave
+}
+// Tile of the units, and the most units, partial slots and split tiles the plan can make of any lengths.  32 rows per
+// wave; past four waves a request has several tiles (once = 0).  fp32 takes one, two or four waves by the rows a request
+// can have (n g): its key tile and LDS are the same for all, so waves without rows only keep others out (64 requests of
+// 512..8192 cached, 16 and 4 heads of 128: 1 token 484 us, 888 with four; 3 tokens 489 and 895).  bf16 takes four, whose
+// idle waves still load (32 and 8 heads of 128: 1 request of 1 token and 16000 cached 32 us, 36 with one; 200 of at most
+// 3000 cached 218 and 224), but one for up to 32 rows over many long caches, where small workgroups keep more of them
+// reading (64 requests of 1 token and 512..8192 cached 212 us, 223 with four).
+inline void chunk_bounds(ChunkAttnArgs& a) {
+  const long long g = a.Hq / a.Hkv, R = a.max_new * g;
+  const bool many_long = a.cap >= 4096 && (long long)a.B * a.Hkv >= 32;
+  const int waves = R <= 32 && (a.f32 || many_long) ? 1 : R <= 64 && a.f32 ? 2 : 4;
+  a.tile_rows = 32 * waves;
+  a.key_tile = chunk_key_tile(waves, a.f32);
+  // workgroups that run at once on 256 compute units: LDS (two stages of K and V) goes in 128 pieces of 1280 bytes
+  const int lds = (4 * a.key_tile * a.D * (a.f32 ? 4 : 2) + 8 + 1279) / 1280;
+  a.slots = std::min(128 / lds, 4 * chunk_waves_per_simd(a.f32, a.D) / waves) * 256;
+  plan_bounds(a, waves);
+}
+
+// Over the 4-bit cache.  bf16 rows up to 96 of a request take waves that walk the keys by themselves (chunk_few.h), 16,
+// 32 or 48 rows each: two of them share a workgroup past 48, so that the second finds its keys in the cache.
+struct MxTile {
+  int ct, waves;   // 16-row blocks of a wave, waves; ct = 0: the tiles of chunk_bounds
+};
+inline MxTile mx_tile(const ChunkAttnArgs& a) {
+  const long long R = (long long)a.max_new * (a.Hq / a.Hkv);
+  if (a.f32 || R > 96) return MxTile{0, 0};
+  return R <= 16 ? MxTile{1, 1} : R <= 32 ? MxTile{2, 1} : R <= 48 ? MxTile{3, 1} : R <= 64 ? MxTile{2, 2} : MxTile{3, 2};
+}
+inline void mx_bounds(ChunkAttnArgs& a) {
+  const MxTile t = mx_tile(a);
+  if (!t.ct) return chunk_bounds(a);
+  a.tile_rows = 16 * t.ct * t.waves;
+  a.key_tile = 64;
+  a.slots = (t.ct == 1 ? 12 : 8) / t.waves * 256;
+  plan_bounds(a, t.waves);
 }
 hipError_t launch_chunk_attn(const ChunkAttnArgs& a, hipStream_t s);
 hipError_t launch_chunk_attn_mx(const ChunkAttnArgs& a, hipStream_t s);

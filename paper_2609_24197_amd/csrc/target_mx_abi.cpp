@@ -91,7 +91,7 @@ static void plan_chunk_attn_mx(Arena& ar, const hspec_chunk_cfg& c, int max_len,
   a.window = c.window; a.f32 = c.dtype == HSPEC_F32;
   // (positions beside the cache have no page, so the table does not bound them; one workspace serves both ways)
   a.cap = std::min(max_len, hspec::kMaxPositions);
-  hspec::chunk_bounds(a);
+  hspec::mx_bounds(a);
   a.status = ar.take<int>(64);
   a.queue = ar.take<int>(hspec::kChunkClasses * hspec::kChunkQueueStride);
   a.units = ar.take<hspec::ChunkUnit>(a.max_units);
