@@ -20,15 +20,15 @@ auto with_variant(const ChunkAttnArgs& a, F f) {
     }
     return a.once ? f(Chunk<T, D, 4, KT4, true, true>{}) : f(Chunk<T, D, 4, KT4, false, true>{});
   };
-  auto few = [&](auto d) {
-    constexpr int D = decltype(d)::value;
-    const MxTile t = mx_tile(a);
-    if (t.waves == 1) return t.ct == 1 ? f(Few<D, 1, 1, true>{}) : t.ct == 2 ? f(Few<D, 2, 1, true>{}) : f(Few<D, 3, 1, true>{});
-    return t.ct == 2 ? f(Few<D, 2, 2, true>{}) : f(Few<D, 3, 2, true>{});
-  };
-  if (mx_tile(a).ct) return a.D == 128 ? few(Int<128>{}) : few(Int<64>{});
   if (a.f32) return a.D == 128 ? by_rows(std::common_type<float>{}, Int<128>{}) : by_rows(std::common_type<float>{}, Int<64>{});
   return a.D == 128 ? by_rows(std::common_type<bf16>{}, Int<128>{}) : by_rows(std::common_type<bf16>{}, Int<64>{});
+}
+
+template <int D>
+hipError_t launch_few_rows(const ChunkAttnArgs& a, hipStream_t s) {
+  const MxTile t = mx_tile(a);
+  if (t.waves == 1) return t.ct == 1 ? launch_few<Few<D, 1, 1>>(a, s) : t.ct == 2 ? launch_few<Few<D, 2, 1>>(a, s) : launch_few<Few<D, 3, 1>>(a, s);
+  return t.ct == 2 ? launch_few<Few<D, 2, 2>>(a, s) : launch_few<Few<D, 3, 2>>(a, s);
 }
 
 }  // namespace
@@ -36,6 +36,7 @@ auto with_variant(const ChunkAttnArgs& a, F f) {
 hipError_t launch_chunk_attn_mx(const ChunkAttnArgs& a, hipStream_t s) {
   hipLaunchKernelGGL(chunk_plan, dim3(1), dim3(PL_THREADS), 0, s, a);
   if (hipError_t e = hipGetLastError()) return e;
+  if (a.columns) return a.D == 128 ? launch_few_rows<128>(a, s) : launch_few_rows<64>(a, s);
   return with_variant(a, [&](auto c) { return launch_units<decltype(c)>(a, s); });
 }
 

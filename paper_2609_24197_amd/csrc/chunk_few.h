@@ -13,15 +13,14 @@
 namespace hspec {
 namespace {
 
-template <int D_, int NCT_, int NW_, bool ONCE_>
+template <int D_, int NCT_, int NW_>
 struct Few {
   typedef bf16 T;
   static constexpr int D = D_, NCT = NCT_, NW = NW_;
   static constexpr int KT = NCT > 2 ? 32 : 64;   // keys of a step (what three blocks of rows leave registers for)
-  static constexpr bool ONCE = ONCE_;
   static constexpr int NT = 64 * NW, ROWS = 16 * NCT * NW;
   static constexpr int WPE = NCT == 1 ? 3 : 2;   // waves per SIMD the registers are sized for
-  static constexpr int STAGE = NW * 32 * D, STAGE1 = 8;   // elements of LDS (32 keys of V of every wave)
+  static constexpr int STAGE = NW * 32 * D;   // elements of LDS: 32 keys of V of every wave
 };
 
 // Element offset of (key, channel d) in a wave's V: 16-byte piece p of a row lies at p ^ f, with f such that a
@@ -321,10 +320,44 @@ __device__ __forceinline__ bool few_unit(const ChunkAttnArgs& a, const ChunkUnit
   return bad;
 }
 
-template <bool ODD, int D, int NCT, int NW, bool ONCE>
-__device__ __forceinline__ bool run_unit(Few<D, NCT, NW, ONCE>, const ChunkAttnArgs& a, const ChunkUnit& u, int h, bf16* st0,
-                                         bf16*) {
-  return few_unit<ODD, Few<D, NCT, NW, ONCE>>(a, u, h, st0);
+// Workgroup (column, head) does the units of its column one after the other.  (256 threads: see chunk_attn_kernel)
+template <class C>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(C::WPE))) few_kernel(ChunkAttnArgs a) {
+  __shared__ __align__(16) bf16 stage[C::STAGE];
+  const int h = blockIdx.x % a.Hkv, w = blockIdx.x / a.Hkv;
+  const int end = a.first[w + 1];
+  for (int i = a.first[w]; i < end; ++i) {
+    const ChunkUnit u = a.units[i];
+    const bool bad = few_unit<false, C>(a, u, h, stage);
+    // (one entry a wave at most: the same item twice is done twice, with the same result)
+    if (a.redo && __any(bad) && (threadIdx.x & 63) == 0) {
+      const int at = atomicAdd(a.status + 3, 1);
+      if (at < a.max_redo) a.redo[at] = i * a.Hkv + h;
+    }
+  }
+}
+// The units some row of which came out infinite or NaN, once more with masked values kept apart.
+template <class C>
+__global__ void __launch_bounds__(C::NT) few_redo_kernel(ChunkAttnArgs a) {
+  __shared__ __align__(16) bf16 stage[C::STAGE];
+  const int n = min(a.status[3], a.max_redo);
+  for (int i = blockIdx.x; i < n; i += gridDim.x) {
+    const int item = a.redo[i];
+    const ChunkUnit u = a.units[item / a.Hkv];
+    few_unit<true, C>(a, u, item % a.Hkv, stage);
+  }
+}
+
+template <class C>
+hipError_t launch_few(const ChunkAttnArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL(few_kernel<C>, dim3((unsigned)a.columns * a.Hkv), dim3(C::NT), 0, s, a);
+  if (hipError_t e = hipGetLastError()) return e;
+  if (a.redo) {
+    const unsigned items = (unsigned)std::min(256LL, (long long)a.max_units * a.Hkv);
+    hipLaunchKernelGGL(few_redo_kernel<C>, dim3(items), dim3(C::NT), 0, s, a);
+    if (hipError_t e = hipGetLastError()) return e;
+  }
+  return launch_merge<bf16, C::D>(a, s);
 }
 
 }  // namespace

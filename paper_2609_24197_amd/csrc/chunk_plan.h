@@ -21,6 +21,9 @@ struct PlanLds {
   unsigned long long keys;            // keys of all tiles
   int longest, slots, n_splits, bits;
   int hist[PL_BUCKETS];
+  // in columns: of each tile of the chunk its range of keys, the steps and the units before it, its first slot
+  int k0[PL_THREADS], len[PL_THREADS], unit[PL_THREADS], slot[PL_THREADS];
+  unsigned long long step[PL_THREADS], wave_steps[PL_THREADS / 64];
 };
 
 struct TileKeys {
@@ -39,6 +42,10 @@ __device__ __forceinline__ TileKeys tile_keys(const ChunkAttnArgs& a, int g, int
 // target are cut into ceil(len / S) even pieces, so the pieces of all tiles number at most target / Hkv more than the
 // tiles, and the split ones twice that (what the workspace holds).  Units are written longest first (64 classes of
 // length), which keeps the queue's tail short.
+//
+// In columns (a.columns > 0, one tile a request): the steps of key_tile keys of all tiles, one tile behind the other, are
+// cut into columns of the same number of steps, so that as many workgroups as run at once have the same to do; a unit is what a
+// tile and a column have in common, and column w has units first[w] .. first[w + 1] - 1.
 __global__ void __launch_bounds__(PL_THREADS) chunk_plan(ChunkAttnArgs a) {
   __shared__ PlanLds s;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -133,10 +140,11 @@ __global__ void __launch_bounds__(PL_THREADS) chunk_plan(ChunkAttnArgs a) {
       }
     }
   };
+  auto steps_of = [&](int len) { return max((len + a.key_tile - 1) / a.key_tile, 1); };
   unsigned long long keys = 0;
   int longest = 0;
   each(false, [&](int, const Tile& x) {
-    keys += x.len;
+    keys += a.columns ? steps_of(x.len) : x.len;
     longest = max(longest, x.len);
   });
 #pragma unroll
@@ -149,6 +157,84 @@ __global__ void __launch_bounds__(PL_THREADS) chunk_plan(ChunkAttnArgs a) {
     atomicMax(&s.longest, longest);
   }
   __syncthreads();
+  if (a.columns) {
+    const unsigned long long all = s.keys;
+    const unsigned long long S = max((all + a.columns - 1) / a.columns, 1ULL);
+    const bool small = all >> 31 == 0;
+    auto column_of = [&](unsigned long long step) { return small ? (int)((unsigned)step / (unsigned)S) : (int)(step / S); };
+    unsigned long long done = 0;   // steps and units of the chunks before
+    int units = 0;
+    // sum of v over the threads before this one, and over all
+    auto before = [&](auto v, auto* sums, auto& total) {
+      auto sum = v;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const auto w = __shfl_up(sum, o);
+        if (lane >= o) sum += w;
+      }
+      __syncthreads();   // (the last use of sums is over)
+      if (lane == 63) sums[wave] = sum;
+      __syncthreads();
+      total = 0;
+      sum -= v;
+      for (int w = 0; w < PL_THREADS / 64; ++w) {
+        if (w < wave) sum += sums[w];
+        total += sums[w];
+      }
+      return sum;
+    };
+    for (int c = 0; c < chunks; ++c) {
+      if (chunks > 1) tiles = load(c * PL_THREADS);
+      const Tile x = tid < tiles ? (chunks == 1 ? mine : tile_of(tid)) : Tile{0, 0, 0, 0};
+      const unsigned long long n = tid < tiles ? steps_of(x.len) : 0;
+      unsigned long long steps;
+      int pieces;
+      const unsigned long long from = done + before(n, s.wave_steps, steps);
+      const int p = n ? column_of(from + n - 1) - column_of(from) + 1 : 0;
+      const int u0 = before(p, s.wave_sum, pieces);
+      if (n) {
+        int slot = -1;
+        if (p > 1) {
+          slot = atomicAdd(&s.slots, p);
+          a.splits[atomicAdd(&s.n_splits, 1)] =
+              ChunkSplit{c * PL_THREADS + x.r, x.tile, slot, p, s.row0[x.r], s.n[x.r], s.L[x.r], 0};
+        }
+        s.k0[tid] = x.k0;
+        s.len[tid] = x.len;
+        s.step[tid] = from;
+        s.slot[tid] = slot;
+      }
+      s.unit[tid] = u0;
+      __syncthreads();
+      for (int i = tid; i < pieces; i += PL_THREADS) {
+        int t = 0;   // the last tile with unit[t] <= i
+#pragma unroll
+        for (int st = PL_THREADS / 2; st > 0; st >>= 1)
+          if (t + st < tiles && s.unit[t + st] <= i) t += st;
+        const unsigned long long tile_from = s.step[t];
+        const int w = column_of(tile_from) + i - s.unit[t];
+        const unsigned long long col = w * S;
+        // keys of the tile before the column, and up to its end
+        const long long at0 = col > tile_from ? (long long)(col - tile_from) * a.key_tile : 0;
+        const long long at1 = min((long long)s.len[t], (long long)(col + S - tile_from) * a.key_tile);
+        const int r = request_of(t), slot = s.slot[t];
+        a.units[units + i] = ChunkUnit{c * PL_THREADS + r, t - s.first[r], s.k0[t] + (int)at0, s.k0[t] + (int)at1,
+                                       slot < 0 ? -1 : slot + i - s.unit[t], s.row0[r], s.n[r], s.L[r]};
+        if (col >= tile_from) a.first[w] = units + i;   // (a column begins in one unit)
+      }
+      done += steps;
+      units += pieces;
+      __syncthreads();
+    }
+    for (int w = column_of(done + S - 1) + tid; w <= a.columns; w += PL_THREADS) a.first[w] = units;
+    if (tid == 0) {
+      a.status[0] = s.bits;
+      a.status[1] = units;
+      a.status[2] = s.n_splits;
+      a.status[3] = 0;
+    }
+    return;
+  }
   const int S = chunk_unit_keys(a, s.keys, all_tiles);
   const int shift = max(26 - __builtin_clz(min(S, s.longest) | 1), 0);   // lengths >> shift are below 64
   auto bucket = [&](int len) -> int { return PL_BUCKETS - 1 - min(len >> shift, PL_BUCKETS - 1); };

@@ -50,7 +50,6 @@ struct Chunk {
   static constexpr int GR = WROWS < 16 ? WROWS : 16;   // of them in one page for certain
   static constexpr int NG = WROWS / GR;
   static constexpr int NI = GR * CPR / 64;         // DMA instructions per group and tensor
-  static constexpr int STAGE = 2 * TILE, STAGE1 = 2 * TILE;   // elements of LDS: K and V of two tiles
   static constexpr int WPE = chunk_waves_per_simd(sizeof(T) == 4, D);   // waves per SIMD the registers are sized for
   static_assert(KT % 32 == 0 && GR * CPR % 64 == 0 && WROWS % GR == 0, "tile shape");
 };
@@ -480,20 +479,14 @@ __device__ __forceinline__ bool chunk_unit(const ChunkAttnArgs& a, const ChunkUn
   return bad;
 }
 
-template <bool ODD, class T, int D, int NW, int KT, bool ONCE, bool MX>
-__device__ __forceinline__ bool run_unit(Chunk<T, D, NW, KT, ONCE, MX>, const ChunkAttnArgs& a, const ChunkUnit& u, int h, T* st0,
-                                         T* st1) {
-  return chunk_unit<Chunk<T, D, NW, KT, ONCE, MX>, ODD>(a, u, h, st0, st1);
-}
-
 template <class C>
 // (256 threads for every NW: with fewer the compiler counts on one wave per SIMD and puts O into accumulation
 // registers, which costs a copy of it both ways in every tile)
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(C::WPE)))
 chunk_attn_kernel(ChunkAttnArgs a) {
   // one LDS object per stage, so that the compiler can tell the one being read from the one whose DMA is in flight
-  __shared__ __align__(16) typename C::T st0[C::STAGE];
-  __shared__ __align__(16) typename C::T st1[C::STAGE1];
+  __shared__ __align__(16) typename C::T st0[2 * C::TILE];
+  __shared__ __align__(16) typename C::T st1[2 * C::TILE];
   __shared__ int s_item[2];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -546,7 +539,7 @@ chunk_attn_kernel(ChunkAttnArgs a) {
     int ticket = 0;
     if (tid == 0 && !one_each) ticket = atomicAdd(counter(cls), 1);
     const int h = item % a.Hkv;
-    const bool bad = run_unit<false>(C{}, a, u, h, st0, st1);
+    const bool bad = chunk_unit<C, false>(a, u, h, st0, st1);
     // (one entry a wave at most: the same item twice is done twice, with the same result)
     if (a.redo && __any(bad) && lane == 0) {
       const int at = atomicAdd(a.status + 3, 1);
@@ -567,13 +560,13 @@ chunk_attn_kernel(ChunkAttnArgs a) {
 // empty where V is finite and nothing overflows).
 template <class C>
 __global__ void __launch_bounds__(C::NT) chunk_redo_kernel(ChunkAttnArgs a) {
-  __shared__ __align__(16) typename C::T st0[C::STAGE];
-  __shared__ __align__(16) typename C::T st1[C::STAGE1];
+  __shared__ __align__(16) typename C::T st0[2 * C::TILE];
+  __shared__ __align__(16) typename C::T st1[2 * C::TILE];
   const int n = min(a.status[3], a.max_redo);
   for (int i = blockIdx.x; i < n; i += gridDim.x) {
     const int item = a.redo[i];
     const ChunkUnit u = a.units[item / a.Hkv];
-    run_unit<true>(C{}, a, u, item % a.Hkv, st0, st1);
+    chunk_unit<C, true>(a, u, item % a.Hkv, st0, st1);
     __syncthreads();
   }
 }
@@ -716,6 +709,22 @@ __global__ void __launch_bounds__(MG_THREADS) chunk_merge_row(ChunkAttnArgs a, i
 
 // ----------------------------------------------------------------------------- launch
 
+template <class T, int D>
+hipError_t launch_merge(const ChunkAttnArgs& a, hipStream_t s) {
+  if (a.max_splits > 0) {
+    const long long rows = std::min((long long)a.tile_rows, (long long)a.max_new * (a.Hq / a.Hkv));
+    const long long singles = (long long)a.max_splits * a.Hkv * rows;
+    if (singles <= MG_FEW) {
+      hipLaunchKernelGGL((chunk_merge_row<T, D>), dim3((unsigned)singles), dim3(MG_THREADS), 0, s, a, (int)rows);
+    } else {
+      const int blocks = (int)((rows * D / 4 + MG_THREADS - 1) / MG_THREADS);
+      const long long wgs = std::min((long long)a.max_splits * a.Hkv * blocks, 2048LL);
+      hipLaunchKernelGGL((chunk_merge_rows<T, D>), dim3((unsigned)wgs), dim3(MG_THREADS), 0, s, a, blocks);
+    }
+  }
+  return hipGetLastError();
+}
+
 // Launches behind the plan: the units, those of them that are done again, the merge.
 template <class C>
 hipError_t launch_units(const ChunkAttnArgs& a, hipStream_t s) {
@@ -740,18 +749,7 @@ hipError_t launch_units(const ChunkAttnArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((chunk_redo_kernel<C>), dim3((unsigned)std::min(items, 256LL)), dim3(64 * NW), 0, s, a);
     if (hipError_t e = hipGetLastError()) return e;
   }
-  if (a.max_splits > 0) {
-    const long long rows = std::min((long long)a.tile_rows, (long long)a.max_new * (a.Hq / a.Hkv));
-    const long long singles = (long long)a.max_splits * a.Hkv * rows;
-    if (singles <= MG_FEW) {
-      hipLaunchKernelGGL((chunk_merge_row<typename C::T, D>), dim3((unsigned)singles), dim3(MG_THREADS), 0, s, a, (int)rows);
-    } else {
-      const int blocks = (int)((rows * D / 4 + MG_THREADS - 1) / MG_THREADS);
-      const long long wgs = std::min((long long)a.max_splits * a.Hkv * blocks, 2048LL);
-      hipLaunchKernelGGL((chunk_merge_rows<typename C::T, D>), dim3((unsigned)wgs), dim3(MG_THREADS), 0, s, a, blocks);
-    }
-  }
-  return hipGetLastError();
+  return launch_merge<typename C::T, D>(a, s);
 }
 
 }  // namespace

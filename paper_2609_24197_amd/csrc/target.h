@@ -60,11 +60,13 @@ struct ChunkAttnArgs {
   int* queue = nullptr;               // [kChunkClasses * kChunkQueueStride]
   ChunkUnit* units = nullptr;
   ChunkSplit* splits = nullptr;
+  int* first = nullptr;               // [columns + 1] the first unit of each column
   int* redo = nullptr;                // items to do again, status[3] of them; null: rows of a request see the same keys
   float* part_o = nullptr;            // [slots][Hkv][tile rows][D]
   float* part_ml = nullptr;           // [slots][Hkv][tile rows][2]
   // chunk_bounds
   int tile_rows = 0, key_tile = 0, once = 0, slots = 0, target = 0, min_split = 0;
+  int columns = 0;                    // 0: units go by a queue
   int max_units = 0, max_slots = 0, max_splits = 0, max_redo = 0;
 };
 // Keys per tile, and waves per SIMD the registers are sized for, of a workgroup of `waves` waves.
@@ -94,11 +96,10 @@ __host__ __device__ inline int chunk_pieces(int len, int S, int key_tile, int& q
   return (int)(((unsigned)len + q - 1) / (unsigned)q);
 }
 
-// What the plan's bounds come to for a tile and its workgroups (chunk_bounds and mx_bounds).
+// What the plan's bounds come to for a tile, its workgroups of `waves` and the target (chunk_bounds and mx_bounds).
 inline void plan_bounds(ChunkAttnArgs& a, int waves) {
   const long long g = a.Hq / a.Hkv, R = a.max_new * g;
   a.once = R <= a.tile_rows;
-  a.target = a.slots * 13 / 8;
   a.min_split = kChunkMinSplit;
   const long long per_req = (R + a.tile_rows - 1) / a.tile_rows;
   const long long tiles = std::min(a.T * g / a.tile_rows + a.B, per_req * a.B);
@@ -127,6 +128,7 @@ inline void chunk_bounds(ChunkAttnArgs& a) {
   // workgroups that run at once on 256 compute units: LDS (two stages of K and V) goes in 128 pieces of 1280 bytes
   const int lds = (4 * a.key_tile * a.D * (a.f32 ? 4 : 2) + 8 + 1279) / 1280;
   a.slots = std::min(128 / lds, 4 * chunk_waves_per_simd(a.f32, a.D) / waves) * 256;
+  a.target = a.slots * 13 / 8;
   plan_bounds(a, waves);
 }
 
@@ -145,7 +147,11 @@ inline void mx_bounds(ChunkAttnArgs& a) {
   if (!t.ct) return chunk_bounds(a);
   a.tile_rows = 16 * t.ct * t.waves;
   a.key_tile = 64;
+  // as many columns as workgroups run at once, and no more than there can be steps
+  const long long most = std::min<long long>(a.T, a.B) * ((a.cap + 63LL) / 64 + 1);
   a.slots = (t.ct == 1 ? 12 : 8) / t.waves * 256;
+  a.columns = (int)std::max(1LL, std::min<long long>(a.slots / a.Hkv, most));
+  a.target = a.columns * a.Hkv;
   plan_bounds(a, t.waves);
 }
 hipError_t launch_chunk_attn(const ChunkAttnArgs& a, hipStream_t s);

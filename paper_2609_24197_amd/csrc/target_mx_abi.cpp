@@ -94,6 +94,7 @@ static void plan_chunk_attn_mx(Arena& ar, const hspec_chunk_cfg& c, int max_len,
   hspec::mx_bounds(a);
   a.status = ar.take<int>(64);
   a.queue = ar.take<int>(hspec::kChunkClasses * hspec::kChunkQueueStride);
+  if (a.columns) a.first = ar.take<int>((size_t)a.columns + 1);
   a.units = ar.take<hspec::ChunkUnit>(a.max_units);
   a.splits = ar.take<hspec::ChunkSplit>(a.max_splits);
   if (a.max_new > 1) a.redo = ar.take<int>(a.max_redo);   // (one new token: its rows see the same keys)
