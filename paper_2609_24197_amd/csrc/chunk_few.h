@@ -1,30 +1,26 @@
 // Units of attention over the 4-bit cache for requests of few rows (a token each, the last token and its drafts, a
 // drafted block), where reading the cache is what counts.
 //
-// A wave owns NCT x 16 rows (token, query head of the group) as columns and walks the unit's keys by itself, 64 at a time:
-//   S^T [keys x rows] = K Q^T   and   O^T [D x rows] += V^T P^T,   16 x 16 x 32 products.
-// Lane l holds channels [D/4 c, D/4 (c + 1)), c = l / 16, of key l % 16 of every 16: of K that is the product's operand as
-// it is, widened in registers (the channels are summed over, so any order of them serves, if Q has the same).  V^T wants
-// its keys side by side: V goes, widened, through a piece of LDS of the wave's own, from which it is read transposed in the
-// order in which S^T leaves a lane its keys.  No wave waits for another: there is no barrier in a unit.
+//   S^T [keys x rows] = K Q^T   and   O^T [D x rows] += V^T P^T,   16 x 16 x 32 products:
+// a wave owns NCT x 16 rows (token, query head of the group) as columns.  Lane l holds channels [D/4 c, D/4 (c + 1)),
+// c = l / 16, of key l % 16 of every 16 (the channels are summed over, so any order of them serves, if Q has the same); V^T
+// is read transposed from LDS in the order in which S^T leaves a lane its keys.
+//
+// Up to 32 rows (Few) a wave walks its keys by itself: K is the product's operand as it was loaded, widened in
+// registers, V goes through a piece of LDS of the wave's own, and there is no barrier in a unit.  Past that (Share)
+// the waves of a workgroup share what they widen: RW of them divide the rows, KW the keys of a step, and the KW results
+// are put together at the unit's end.
 #pragma once
 #include "chunk_tile.h"
 
 namespace hspec {
 namespace {
 
-template <int D_, int NCT_, int NW_>
-struct Few {
-  typedef bf16 T;
-  static constexpr int D = D_, NCT = NCT_, NW = NW_;
-  static constexpr int KT = NCT > 2 ? 32 : 64;   // keys of a step (what three blocks of rows leave registers for)
-  static constexpr int NT = 64 * NW, ROWS = 16 * NCT * NW;
-  static constexpr int WPE = NCT == 1 ? 3 : 2;   // waves per SIMD the registers are sized for
-  static constexpr int STAGE = NW * 32 * D;   // elements of LDS: 32 keys of V of every wave
-};
+// Bits of what a unit found: a row that came out infinite or NaN, a page outside the pool.
+enum : int { UNIT_ODD = 1, UNIT_BAD_PAGE = 2 };
 
-// Element offset of (key, channel d) in a wave's V: 16-byte piece p of a row lies at p ^ f, with f such that a
-// transposing read's 8 rows of two pieces, and a write's 16 rows of one, fall into different banks.
+// Element offset of (key, channel d) in LDS: 16-byte piece p of a row lies at p ^ f, with f such that a transposing
+// read's 8 rows of two pieces, a fragment's 16 rows of one, and a write's fall into different banks.
 template <int D>
 __device__ __forceinline__ int few_off(int key, int d) {
   const int f = (D == 128 ? 2 * (key & 7) : key & 6) ^ ((key >> 3) & 1);
@@ -37,123 +33,57 @@ __device__ __forceinline__ s16x4 few_v(const bf16* sV, int key0, int db, int lan
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(sV + few_off<D>(key, db * 16 + 4 * (lane & 3))));
 }
 
-template <bool ODD, class C>
-__device__ __forceinline__ bool few_unit(const ChunkAttnArgs& a, const ChunkUnit& u, int h, bf16* stage) {
-  constexpr int D = C::D, KT = C::KT, NCT = C::NCT;
-  constexpr int CH = D / 4, NS = CH / 8, NB = D / 16, NK = KT / 16;   // channels of a lane, products per 16 keys, d blocks, groups of keys
-  typedef typename std::conditional<D == 128, u32x4, uint2>::type Codes;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int c = lane >> 4, l16 = lane & 15;
-  const int lps = 31 - __builtin_clz(a.ps);
-  const int g = a.Hq / a.Hkv;
-  const int R = u.n * g;
-  const int c0 = u.tile * C::ROWS + wave * 16 * NCT;   // first row of this wave
-  if (c0 >= R) return false;
-  bf16* sV = stage + wave * 32 * D;
-  const int back = a.window > 0 ? a.window - 1 : INT_MAX;
-  auto sees_from = [&](int tok) { return max(u.L + tok - back, 0); };
-  auto sees_to = [&](int tok) { return min(min(u.L + (a.block ? u.n : tok + 1), a.cap), u.k1); };
-  const int t_first = c0 / g, t_last = min(c0 + 16 * NCT - 1, R - 1) / g;
-  const int any_lo = sees_from(t_first), any_hi = sees_to(t_last), all_lo = sees_from(t_last), all_hi = sees_to(t_first);
-  const int k_min = max(u.k0, any_lo);   // the first key that a row of this wave sees: those before it are not read
-  const int held = a.k_new ? min(u.L, u.k1) : u.k1;
-
-  // this lane's column of each 16: its token, its first element, the keys it sees
-  int lo[NCT], hi[NCT];
+// A wave's rows: what they see, Q, and the softmax's running maximum, sum and output.
+template <int D, int NCT, bool ODD>
+struct FewRows {
+  static constexpr int CH = D / 4, NS = CH / 8, NB = D / 16;   // channels of a lane, products per 16 keys, d blocks
+  int lo[NCT], hi[NCT];       // keys that this lane's column of each 16 sees
+  int any_lo, any_hi, all_lo, all_hi;   // keys that any and that all rows of the wave see
   size_t at_q[NCT];
   bool real[NCT];
   bf16x8 qf[NCT][NS];
-#pragma unroll
-  for (int ct = 0; ct < NCT; ++ct) {
-    const int r = c0 + 16 * ct + l16;
-    real[ct] = r < R;
-    const int tok = real[ct] ? r / g : u.n - 1, hq = h * g + (real[ct] ? r - tok * g : 0);
-    at_q[ct] = ((size_t)(u.row0 + tok) * a.Hq + hq) * D;
-    lo[ct] = sees_from(tok);
-    hi[ct] = real[ct] ? sees_to(tok) : 0;
-#pragma unroll
-    for (int s = 0; s < NS; ++s)
-      qf[ct][s] = real[ct] ? ld8(static_cast<const bf16*>(a.q) + at_q[ct] + CH * c + 8 * s) : zero8();
-  }
-  auto live = [&](int ct) { return ct == 0 || c0 + 16 * ct < R; };   // (uniform)
-
-  // Ids of pages [pg0, pg0 + 64) and the 64 behind them, lane by lane; a step's pages lie in one such window, since its
-  // keys and pg0 are aligned to steps.
-  const int32_t* ptab = a.page_table + (size_t)u.b * a.max_pages;
-  const int pg_end = held > k_min ? ((held - 1) >> lps) + 1 : 0;
-  const int from = k_min / KT * KT;   // (u.k0 is a multiple of 64 too, and 16 keys lie in one page)
-  int pg0 = (from >> lps) & ~3;
-  auto ids_at = [&](int pg) { return pg + lane < pg_end ? ptab[pg + lane] : -1; };
-  int ids = ids_at(pg0), ids_next = ids_at(pg0 + 64);
-  // KT keys on their way: where each 16 of them begin in a cache, and which of them this lane's key is
-  struct Place {
-    size_t off[NK];       // of the head's part of the page
-    unsigned bytes[NK];   // 0: no such page
-  };
-  const unsigned head_bytes = (unsigned)mx_head_bytes(a.ps, D), page_bytes = head_bytes * (unsigned)a.Hkv;
-  const size_t at_h = (size_t)h * head_bytes;
-  auto place = [&](int base) {
-    Place x;
-    if ((base >> lps) >= pg0 + 64) {
-      pg0 += 64;
-      ids = ids_next;
-      ids_next = ids_at(pg0 + 64);
-    }
-#pragma unroll
-    for (int t = 0; t < NK; ++t) {
-      const int pg = (base + 16 * t) >> lps;
-      const unsigned id = (unsigned)__builtin_amdgcn_readlane(ids, (pg - pg0) & 63);
-      const bool good = id < (unsigned)a.num_pages;
-      x.bytes[t] = good ? head_bytes : 0u;
-      x.off[t] = at_h + (size_t)(good ? id : 0u) * page_bytes;
-      if (!good && base + 16 * t < held && base + 16 * t + 16 > k_min && lane == 0) set_status(a.status, ST_BAD_PAGE);
-    }
-    return x;
-  };
-  struct Raw {
-    Codes code[NK];
-    unsigned scale[NK];
-  };
-  const unsigned at_code = l16 * (D / 2) + c * (CH / 2), at_scale = a.ps * (D / 2) + l16 * (D / MX_BLOCK) + c * CH / MX_BLOCK;
-  auto load = [&](const void* cache, int base, const Place& at, Raw& x) {
-#pragma unroll
-    for (int t = 0; t < NK; ++t) {
-      // (a key that no row sees reads as zeros, by an offset past the buffer)
-      const bool in = (unsigned)(base + 16 * t + l16 - k_min) < (unsigned)(held - k_min);
-      const unsigned row0 = (unsigned)(base + 16 * t) & (unsigned)(a.ps - 1);
-      const auto r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(static_cast<const uint8_t*>(cache) + at.off[t]), 0,
-                                                       at.bytes[t], BUFFER_FLAGS);
-      if constexpr (D == 128) {
-        x.code[t] = __builtin_bit_cast(Codes, __builtin_amdgcn_raw_buffer_load_b128(r, in ? at_code : BUF_OOB, row0 * (D / 2), 0));
-      } else {
-        x.code[t] = __builtin_bit_cast(Codes, __builtin_amdgcn_raw_buffer_load_b64(r, in ? at_code : BUF_OOB, row0 * (D / 2), 0));
-      }
-      x.scale[t] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(r, in ? at_scale : BUF_OOB, row0 * (D / MX_BLOCK), 0);
-    }
-  };
-  auto word = [](const Codes& x, int s) -> unsigned { return reinterpret_cast<const unsigned*>(&x)[s]; };
-
   f32x4 o[NCT][NB];
   float m_run[NCT], l_run[NCT];
-#pragma unroll
-  for (int ct = 0; ct < NCT; ++ct) {
-#pragma unroll
-    for (int db = 0; db < NB; ++db) o[ct][db] = f32x4{0.f, 0.f, 0.f, 0.f};
-    m_run[ct] = -INFINITY;
-    l_run[ct] = 0.f;
-  }
-  f32x4 st[NCT][NK];
-  // Softmax of the scores of keys [base, base + 64) below end, and their values' part of the output.
-  // value(t, s): channels 8 s .. of this lane's of V of its key of the t-th 16.
-  auto attend = [&](int base, int end, auto value) {
-    const bool full = base + KT <= min(all_hi, end) && base >= all_lo;
+  int c0, R, lane, c;
+
+  // (Columns past the last row go through all of it as zeros: branches around them would keep loads from running ahead.)
+
+  __device__ __forceinline__ void init(const ChunkAttnArgs& a, const ChunkUnit& u, int h, int c0_) {
+    const int g = a.Hq / a.Hkv, back = a.window > 0 ? a.window - 1 : INT_MAX;
+    lane = threadIdx.x & 63;
+    c = lane >> 4;
+    c0 = c0_;
+    R = u.n * g;
+    auto sees_from = [&](int tok) { return max(u.L + tok - back, 0); };
+    auto sees_to = [&](int tok) { return min(min(u.L + (a.block ? u.n : tok + 1), a.cap), u.k1); };
+    const int t_first = min(c0, R - 1) / g, t_last = min(c0 + 16 * NCT - 1, R - 1) / g;
+    any_lo = sees_from(t_first), any_hi = sees_to(t_last), all_lo = sees_from(t_last), all_hi = sees_to(t_first);
 #pragma unroll
     for (int ct = 0; ct < NCT; ++ct) {
-      if (!live(ct)) continue;
+      const int r = c0 + 16 * ct + (lane & 15);
+      real[ct] = r < R;
+      const int tok = real[ct] ? r / g : u.n - 1, hq = h * g + (real[ct] ? r - tok * g : 0);
+      at_q[ct] = ((size_t)(u.row0 + tok) * a.Hq + hq) * D;
+      lo[ct] = sees_from(tok);
+      hi[ct] = real[ct] ? sees_to(tok) : 0;
+#pragma unroll
+      for (int s = 0; s < NS; ++s)
+        qf[ct][s] = real[ct] ? ld8(static_cast<const bf16*>(a.q) + at_q[ct] + CH * c + 8 * s) : zero8();
+#pragma unroll
+      for (int db = 0; db < NB; ++db) o[ct][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+      m_run[ct] = -INFINITY;
+      l_run[ct] = 0.f;
+    }
+  }
+
+  // Softmax weights, in st, of the scores of keys [base, base + 16 NK) below end.
+  template <int NK>
+  __device__ __forceinline__ void weights(const ChunkAttnArgs& a, f32x4 (&st)[NCT][NK], int base, int end) {
+    const bool full = base + 16 * NK <= min(all_hi, end) && base >= all_lo;
+#pragma unroll
+    for (int ct = 0; ct < NCT; ++ct) {
       if (!full) {
-        const int top = min(hi[ct], end);
-        const unsigned span = (unsigned)max(top - lo[ct], 0);
+        const unsigned span = (unsigned)max(min(hi[ct], end) - lo[ct], 0);
 #pragma unroll
         for (int t = 0; t < NK; ++t)
 #pragma unroll
@@ -185,166 +115,573 @@ __device__ __forceinline__ bool few_unit(const ChunkAttnArgs& a, const ChunkUnit
           l_run[ct] += e;
         }
     }
-    // P enters as bf16: half a step is 2^-8 of each weight, as large as the output's own rounding; the sum above takes
-    // the unrounded weights
+  }
+
+  // O += of the 32 keys from base on, whose weights are st[.][t] and st[.][t + 1] and whose V begins at sV.  P enters as
+  // bf16: half a step is 2^-8 of each weight, as large as the output's own rounding; the sum takes the unrounded weights.
+  template <int NK>
+  __device__ __forceinline__ void values(const f32x4 (&st)[NCT][NK], int t, const bf16* sV, int base, int end) {
+    bf16x8 pf[NCT];
 #pragma unroll
-    for (int t = 0; t < NK; t += 2) {
+    for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
-      for (int t2 = 0; t2 < 2; ++t2)
+      for (int j = 0; j < 8; ++j) pf[ct][j] = f2bf(st[ct][t + j / 4][j % 4]);
 #pragma unroll
-        for (int s = 0; s < NS; ++s)
-          *reinterpret_cast<bf16x8*>(sV + few_off<D>(16 * t2 + l16, CH * c + 8 * s)) = value(t + t2, s);
-      bf16x8 pf[NCT];
+    for (int db = 0; db < NB; ++db) {
+      const s16x4 v0 = few_v<D>(sV, 0, db, lane), v1 = few_v<D>(sV, 16, db, lane);
+      bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+      if constexpr (ODD) {
+        // values that are not finite are kept out of the product, where 0 x them would reach rows that do not see
+        // them, and added to the rows that do, as sums that overflow (a NaN as +inf and -inf)
+        s16x8 bits = __builtin_bit_cast(s16x8, vf), up, dn;
 #pragma unroll
-      for (int ct = 0; ct < NCT; ++ct)
+        for (int j = 0; j < 8; ++j) {
+          const bool fin = (bits[j] & 0x7f80) != 0x7f80, nan = !fin && (bits[j] & 0x7f);
+          up[j] = (short)(!fin && (nan || bits[j] >= 0) ? 0x7f7f : 0);   // the largest bf16
+          dn[j] = (short)(!fin && (nan || bits[j] < 0) ? 0xff7f : 0);
+          if (!fin) bits[j] = 0;
+        }
+        vf = __builtin_bit_cast(bf16x8, bits);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) pf[ct][j] = f2bf(st[ct][t + j / 4][j % 4]);
-#pragma unroll
-      for (int db = 0; db < NB; ++db) {
-        const s16x4 v0 = few_v<D>(sV, 0, db, lane), v1 = few_v<D>(sV, 16, db, lane);
-        bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-        if constexpr (ODD) {
-          // values that are not finite are kept out of the product, where 0 x them would reach rows that do not see
-          // them, and added to the rows that do, as sums that overflow (a NaN as +inf and -inf)
-          s16x8 bits = __builtin_bit_cast(s16x8, vf), up, dn;
+        for (int ct = 0; ct < NCT; ++ct) {
+          s16x8 sees;
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const bool fin = (bits[j] & 0x7f80) != 0x7f80, nan = !fin && (bits[j] & 0x7f);
-            up[j] = (short)(!fin && (nan || bits[j] >= 0) ? 0x7f7f : 0);   // the largest bf16
-            dn[j] = (short)(!fin && (nan || bits[j] < 0) ? 0xff7f : 0);
-            if (!fin) bits[j] = 0;
+            const int key = base + 16 * (j / 4) + 4 * c + j % 4;
+            sees[j] = (short)(key >= lo[ct] && key < min(hi[ct], end) ? 0x7f7f : 0);
           }
-          vf = __builtin_bit_cast(bf16x8, bits);
-#pragma unroll
-          for (int ct = 0; ct < NCT; ++ct) {
-            s16x8 sees;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const int key = base + 16 * (t + j / 4) + 4 * c + j % 4;
-              sees[j] = (short)(key >= lo[ct] && key < min(hi[ct], end) ? 0x7f7f : 0);
-            }
-            const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-            o[ct][db] += mma16(__builtin_bit_cast(bf16x8, up), __builtin_bit_cast(bf16x8, sees), zero);
-            o[ct][db] += mma16(__builtin_bit_cast(bf16x8, dn), __builtin_bit_cast(bf16x8, sees), zero);
-          }
+          const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+          o[ct][db] += mma16(__builtin_bit_cast(bf16x8, up), __builtin_bit_cast(bf16x8, sees), zero);
+          o[ct][db] += mma16(__builtin_bit_cast(bf16x8, dn), __builtin_bit_cast(bf16x8, sees), zero);
         }
-#pragma unroll
-        for (int ct = 0; ct < NCT; ++ct)
-          if (live(ct)) o[ct][db] = mma16(vf, pf[ct], o[ct][db]);
       }
+#pragma unroll
+      for (int ct = 0; ct < NCT; ++ct)
+        o[ct][db] = mma16(vf, pf[ct], o[ct][db]);
+    }
+  }
+
+  // Lane holds O[row l16][d = 16 db + 4 c + i]: out, or as a partial result from row `part` of the unit's slot on.
+  __device__ __forceinline__ int finish(const ChunkAttnArgs& a, const ChunkUnit& u, int h, int rows, int part) {
+    bool bad = false;
+#pragma unroll
+    for (int ct = 0; ct < NCT; ++ct) {
+      const float l = wave_sum16x4(l_run[ct]);
+      if constexpr (!ODD) {
+#pragma unroll
+        for (int db = 0; db < NB; ++db)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) bad |= real[ct] && !(fabsf(o[ct][db][i]) < INFINITY);
+      }
+      if (!real[ct]) continue;
+      if (u.slot < 0) {
+        const float inv = hi[ct] > lo[ct] ? 1.f / l : 0.f;   // (a row that sees no key is zero)
+        bf16* dst = static_cast<bf16*>(a.o) + at_q[ct] + 4 * c;
+#pragma unroll
+        for (int db = 0; db < NB; ++db) {
+          const f32x4 v = o[ct][db] * inv;
+          *reinterpret_cast<bf16x4*>(dst + 16 * db) = bf16x4{f2bf(v[0]), f2bf(v[1]), f2bf(v[2]), f2bf(v[3])};
+        }
+      } else {
+        const size_t pr = ((size_t)u.slot * a.Hkv + h) * rows + part + 16 * ct + (lane & 15);
+        float* po = a.part_o + pr * D + 4 * c;
+#pragma unroll
+        for (int db = 0; db < NB; ++db) *reinterpret_cast<f32x4*>(po + 16 * db) = o[ct][db];
+        if (c == 0) *reinterpret_cast<float2*>(a.part_ml + pr * 2) = float2{m_run[ct], l};
+      }
+    }
+    return bad ? UNIT_ODD : 0;
+  }
+};
+
+// Where keys lie.  Ids of pages [pg0, pg0 + 64) and the 64 behind them, lane by lane; a step's pages lie in one such
+// window, since its keys and pg0 are aligned to 64 keys.
+struct FewPages {
+  const int32_t* tab;
+  int pg0, end, ids, next, lps, num;
+
+  __device__ __forceinline__ int at(int pg) const {
+    const int e = pg + (int)(threadIdx.x & 63);
+    return e < end ? tab[e] : -1;
+  }
+  __device__ __forceinline__ void init(const ChunkAttnArgs& a, int b, int from, int held) {
+    lps = 31 - __builtin_clz(a.ps);
+    num = a.num_pages;
+    tab = a.page_table + (size_t)b * a.max_pages;
+    end = held > from ? ((held - 1) >> lps) + 1 : 0;
+    pg0 = (from >> lps) & ~3;
+    ids = at(pg0);
+    next = at(pg0 + 64);
+  }
+  __device__ __forceinline__ void step(int base) {   // before the pages of the 64 keys from base on are looked up
+    if ((base >> lps) >= pg0 + 64) {
+      pg0 += 64;
+      ids = next;
+      next = at(pg0 + 64);
+    }
+  }
+  // id of the page of `key` (the same for the wave), or -1
+  __device__ __forceinline__ int page(int key) const {
+    const int id = __builtin_amdgcn_readlane(ids, ((key >> lps) - pg0) & 63);
+    return (unsigned)id < (unsigned)num ? id : -1;
+  }
+};
+
+// ---------------------------------------------------------------- a wave by itself
+
+template <int D_, int NCT_>
+struct Few {
+  static constexpr int D = D_, NCT = NCT_;
+  static constexpr int NW = 1, KT = 64, NT = 64, ROWS = 16 * NCT;
+  static constexpr int WPE = NCT == 1 ? 3 : 2;    // waves per SIMD the registers are sized for
+  static constexpr int VK = NCT == 1 ? 32 : KT;   // keys of V in LDS at a time
+  static constexpr int LDS = VK * D;              // elements
+};
+
+template <bool ODD, class C>
+__device__ __forceinline__ int few_unit(C, const ChunkAttnArgs& a, const ChunkUnit& u, int h, bf16* sV) {
+  constexpr int D = C::D, KT = C::KT, NCT = C::NCT, NK = KT / 16, VK = C::VK;
+  typedef FewRows<D, NCT, ODD> Rows;
+  constexpr int CH = Rows::CH, NS = Rows::NS;
+  typedef typename std::conditional<D == 128, u32x4, uint2>::type Codes;
+  const int lane = threadIdx.x & 63, c = lane >> 4, l16 = lane & 15;
+  const int held = a.k_new ? min(u.L, u.k1) : u.k1;
+  Rows x;
+  x.init(a, u, h, 0);
+  const int k_min = max(u.k0, x.any_lo);   // the first key that a row sees: those before it are not read
+  const int from = k_min / KT * KT;        // (u.k0 is a multiple of 64 too, so that 16 keys lie in one page)
+  FewPages pages;
+  pages.init(a, u.b, from, held);
+  int found = 0;
+
+  // KT keys on their way: where each 16 of them begin in a cache
+  struct Place {
+    size_t off[NK];       // of the head's part of the page
+    unsigned bytes[NK];   // 0: no such page
+  };
+  const unsigned head_bytes = (unsigned)mx_head_bytes(a.ps, D), page_bytes = head_bytes * (unsigned)a.Hkv;
+  const size_t at_h = (size_t)h * head_bytes;
+  auto place = [&](int base) {
+    Place p;
+    pages.step(base);
+#pragma unroll
+    for (int t = 0; t < NK; ++t) {
+      const int id = pages.page(base + 16 * t);
+      p.bytes[t] = id >= 0 ? head_bytes : 0u;
+      p.off[t] = at_h + (size_t)max(id, 0) * page_bytes;
+      if (id < 0 && base + 16 * t < held && base + 16 * t + 16 > k_min) found = UNIT_BAD_PAGE;
+    }
+    return p;
+  };
+  struct Raw {
+    Codes code[NK];
+    unsigned scale[NK];
+  };
+  const unsigned at_code = l16 * (D / 2) + c * (CH / 2), at_scale = a.ps * (D / 2) + l16 * (D / MX_BLOCK) + c * CH / MX_BLOCK;
+  auto load = [&](const void* cache, int base, const Place& p, Raw& w) {
+#pragma unroll
+    for (int t = 0; t < NK; ++t) {
+      // (a key that no row sees reads as zeros, by an offset past the buffer)
+      const bool in = (unsigned)(base + 16 * t + l16 - k_min) < (unsigned)(held - k_min);
+      const unsigned row0 = (unsigned)(base + 16 * t) & (unsigned)(a.ps - 1);
+      const auto r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(static_cast<const uint8_t*>(cache) + p.off[t]), 0,
+                                                       p.bytes[t], BUFFER_FLAGS);
+      if constexpr (D == 128) {
+        w.code[t] = __builtin_bit_cast(Codes, __builtin_amdgcn_raw_buffer_load_b128(r, in ? at_code : BUF_OOB, row0 * (D / 2), 0));
+      } else {
+        w.code[t] = __builtin_bit_cast(Codes, __builtin_amdgcn_raw_buffer_load_b64(r, in ? at_code : BUF_OOB, row0 * (D / 2), 0));
+      }
+      w.scale[t] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(r, in ? at_scale : BUF_OOB, row0 * (D / MX_BLOCK), 0);
+    }
+  };
+  auto wide = [](const Raw& w, int t, int s) { return mx_widen(reinterpret_cast<const unsigned*>(&w.code[t])[s], w.scale[t]); };
+
+  f32x4 st[NCT][NK];
+  auto clear = [&]() {
+#pragma unroll
+    for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+      for (int t = 0; t < NK; ++t) st[ct][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  };
+  // Groups [t0, t1) of V into LDS; value(t, s): channels 8 s .. of this lane's of its key of the t-th 16.
+  auto put = [&](int t0, int t1, auto value) {
+#pragma unroll
+    for (int t = t0; t < t1; ++t)
+#pragma unroll
+      for (int s = 0; s < NS; ++s)
+        *reinterpret_cast<bf16x8*>(sV + few_off<D>(16 * t % VK + l16, CH * c + 8 * s)) = value(t, s);
+  };
+  // (VK < KT: V goes into LDS here, 32 keys at a time)
+  auto attend = [&](int base, int end, auto value) {
+    x.weights(a, st, base, end);
+#pragma unroll
+    for (int t = 0; t < NK; t += 2) {
+      if constexpr (VK < KT) put(t, t + 2, value);
+      x.values(st, t, sV + 16 * t % VK * D, base + 16 * t, end);
     }
   };
 
-  // cached keys: the next step's K is on its way from where this one's is multiplied, its V from where this one's has
-  // gone into LDS
+  // cached keys: the next step's are on their way from where this one's are multiplied (K) or have gone into LDS (V)
   if (from < held) {
     Raw rk, rv;
-    Place at = place(from);
-    load(a.k_cache, from, at, rk);
-    load(a.v_cache, from, at, rv);
+    Place p = place(from);
+    load(a.k_cache, from, p, rk);
+    load(a.v_cache, from, p, rv);
     for (int base = from; base < held; base += KT) {
-      const bool more = base + KT < held;
+      auto value = [&](int t, int s) { return wide(rv, t, s); };
+      p = place(base + KT);   // (keys past the last read as zeros; a branch around a load would have the next one wait for all)
+      if constexpr (VK == KT) {
+        put(0, NK, value);
+        load(a.v_cache, base + KT, p, rv);
+      }
+      clear();
 #pragma unroll
-      for (int t = 0; t < NK; ++t) {
-#pragma unroll
-        for (int ct = 0; ct < NCT; ++ct) st[ct][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int t = 0; t < NK; ++t)
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
-          const bf16x8 kf = mx_widen(word(rk.code[t], s), rk.scale[t]);
+          const bf16x8 kf = wide(rk, t, s);
 #pragma unroll
           for (int ct = 0; ct < NCT; ++ct)
-            if (live(ct)) st[ct][t] = mma16(kf, qf[ct][s], st[ct][t]);
+            st[ct][t] = mma16(kf, x.qf[ct][s], st[ct][t]);
         }
-      }
-      if (more) {
-        at = place(base + KT);
-        load(a.k_cache, base + KT, at, rk);
-      }
-      attend(base, held, [&](int t, int s) { return mx_widen(word(rv.code[t], s), rv.scale[t]); });
-      if (more) load(a.v_cache, base + KT, at, rv);
+      load(a.k_cache, base + KT, p, rk);
+      attend(base, held, value);
+      if constexpr (VK < KT) load(a.v_cache, base + KT, p, rv);
     }
   }
   // the new tokens' keys beside the cache, as they are
   if (a.k_new && u.k1 > u.L) {
-    const int first = max(k_min, u.L);
     const size_t stride = (size_t)a.Hkv * D, at_new = (size_t)u.row0 * stride + h * D + CH * c;
-    for (int base = first; base < any_hi; base += KT) {
+    for (int base = max(k_min, u.L); base < x.any_hi; base += KT) {
       auto row = [&](const void* p, int t, int s) -> bf16x8 {
         const int key = base + 16 * t + l16;
         return key < u.k1 ? ld8(static_cast<const bf16*>(p) + at_new + (size_t)(key - u.L) * stride + 8 * s) : zero8();
       };
+      clear();
 #pragma unroll
-      for (int t = 0; t < NK; ++t) {
-#pragma unroll
-        for (int ct = 0; ct < NCT; ++ct) st[ct][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int t = 0; t < NK; ++t)
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
           const bf16x8 kf = row(a.k_new, t, s);
 #pragma unroll
-          for (int ct = 0; ct < NCT; ++ct) st[ct][t] = mma16(kf, qf[ct][s], st[ct][t]);
+          for (int ct = 0; ct < NCT; ++ct) st[ct][t] = mma16(kf, x.qf[ct][s], st[ct][t]);
         }
-      }
-      attend(base, INT_MAX, [&](int t, int s) { return row(a.v_new, t, s); });
+      auto value = [&](int t, int s) { return row(a.v_new, t, s); };
+      if constexpr (VK == KT) put(0, NK, value);
+      attend(base, INT_MAX, value);
     }
   }
-
-  // lane holds O[row l16][d = 16 db + 4 c + i]
-  bool bad = false;
-#pragma unroll
-  for (int ct = 0; ct < NCT; ++ct) {
-    if (!live(ct)) continue;
-    const float l = wave_sum16x4(l_run[ct]);
-    if constexpr (!ODD) {
-#pragma unroll
-      for (int db = 0; db < NB; ++db)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) bad |= real[ct] && !(fabsf(o[ct][db][i]) < INFINITY);
-    }
-    if (!real[ct]) continue;
-    if (u.slot < 0) {
-      const float inv = hi[ct] > lo[ct] ? 1.f / l : 0.f;   // (a row that sees no key is zero)
-      bf16* dst = static_cast<bf16*>(a.o) + at_q[ct] + 4 * c;
-#pragma unroll
-      for (int db = 0; db < NB; ++db) {
-        const f32x4 v = o[ct][db] * inv;
-        *reinterpret_cast<bf16x4*>(dst + 16 * db) = bf16x4{f2bf(v[0]), f2bf(v[1]), f2bf(v[2]), f2bf(v[3])};
-      }
-    } else {
-      const size_t pr = ((size_t)u.slot * a.Hkv + h) * C::ROWS + wave * 16 * NCT + 16 * ct + l16;
-      float* po = a.part_o + pr * D + 4 * c;
-#pragma unroll
-      for (int db = 0; db < NB; ++db) *reinterpret_cast<f32x4*>(po + 16 * db) = o[ct][db];
-      if (c == 0) *reinterpret_cast<float2*>(a.part_ml + pr * 2) = float2{m_run[ct], l};
-    }
-  }
-  return bad;
+  return found | x.finish(a, u, h, C::ROWS, 0);
 }
 
-// Workgroup (column, head) does the units of its column one after the other.  (256 threads: see chunk_attn_kernel)
+// ------------------------------------------------------------- waves share a step
+
+// RW x KW waves: wave (r, k) has rows 32 r .. of the tile and keys 32 k .. of every KT, 32 x 32 x 16 products (as
+// chunk_unit's, whose operands' layouts these are).
+template <int D_, int RW_, int KW_>
+struct Share {
+  static constexpr int D = D_, RW = RW_, KW = KW_;
+  static constexpr int NW = RW * KW, KT = 64, NT = 64 * NW, ROWS = 32 * RW;
+  static constexpr int WPE = 2;
+  static constexpr int TILE = KT * D, CPR = D / 8;
+  static constexpr int MERGE = KW > 1 ? ROWS * (D + 4) * 2 : 0;     // elements that results take on their way between waves
+  static constexpr int LDS = 4 * TILE > MERGE ? 4 * TILE : MERGE;   // two stages of K and V
+  static_assert(KW <= 2 && NW >= 4 && NW <= 8, "waves");
+};
+
+template <bool ODD, class C>
+__device__ __forceinline__ int share_unit(C, const ChunkAttnArgs& a, const ChunkUnit& u, int h, bf16* lds) {
+  constexpr int D = C::D, KT = C::KT, TILE = C::TILE, CPR = C::CPR;
+  constexpr int NQ = D / 16, NDB = D / 32, NKB = KT / 32 / C::KW;   // products per 32 keys, d blocks, 32-key blocks of a wave
+  constexpr int CH = D / 4, NS = CH / 8;
+  typedef typename std::conditional<D == 128, u32x4, uint2>::type Codes;
+  const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5, l32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rw = wave / C::KW, kw = wave % C::KW;
+  const int held = a.k_new ? min(u.L, u.k1) : u.k1;
+  const int g = a.Hq / a.Hkv, R = u.n * g, c0 = rw * 32, c = c0 + l32;
+  const bool live = c0 < R, real = c < R;
+  const int tok = real ? c / g : u.n - 1, hq = h * g + (real ? c - tok * g : 0);
+  const size_t at_q = ((size_t)(u.row0 + tok) * a.Hq + hq) * D;
+  const int back = a.window > 0 ? a.window - 1 : INT_MAX;
+  auto sees_from = [&](int t) { return max(u.L + t - back, 0); };
+  auto sees_to = [&](int t) { return min(min(u.L + (a.block ? u.n : t + 1), a.cap), u.k1); };
+  const int lo = sees_from(tok), hi0 = real ? sees_to(tok) : 0;
+  const int t_first = min(c0, R - 1) / g, t_last = min(c0 + 31, R - 1) / g;
+  const int any_lo = sees_from(t_first), any_hi0 = sees_to(t_last), all_lo = sees_from(t_last), all_hi0 = sees_to(t_first);
+  const int k_min = max(u.k0, sees_from(0));   // the first key that a row of the unit sees
+  const int from = k_min / KT * KT;
+  FewPages pages;
+  pages.init(a, u.b, from, held);
+  int found = 0;
+  bf16x8 qf[NQ];
+#pragma unroll
+  for (int s = 0; s < NQ; ++s) qf[s] = real ? ld8(static_cast<const bf16*>(a.q) + at_q + 16 * s + 8 * hf) : zero8();
+  f32x16 o[NDB];
+#pragma unroll
+  for (int db = 0; db < NDB; ++db) o[db] = zero16();
+  float m_run = -INFINITY, l_run = 0.f;
+
+  // A wave takes 16 keys of K, and of V, a step (of one of them with more than four waves), a lane channels
+  // [CH c4, CH (c4 + 1)) of one key.  Loads go through buffers, without branches: behind those the compiler would wait for every load
+  // under way.
+  const int l16 = lane & 15, c4 = lane >> 4;
+  const int k16[2] = {16 * wave, 16 * (wave - (C::NW - 4))};   // outside [0, 64): none
+  struct Raw {
+    Codes code[2];   // K, V
+    unsigned scale[2];
+  };
+  const unsigned head_bytes = (unsigned)mx_head_bytes(a.ps, D), page_bytes = head_bytes * (unsigned)a.Hkv;
+  const size_t at_h = (size_t)h * head_bytes;
+  const unsigned at_code = l16 * (D / 2) + c4 * (CH / 2), at_scale = a.ps * (D / 2) + l16 * (D / MX_BLOCK) + c4 * CH / MX_BLOCK;
+  auto load = [&](int base, Raw& w) {
+    pages.step(base);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int key0 = base + (k16[i] & (KT - 1));
+      const bool mine = C::NW == 4 || (unsigned)k16[i] < (unsigned)KT;
+      const int id = pages.page(key0);
+      if (mine && id < 0 && key0 < held && key0 + 16 > k_min) found = UNIT_BAD_PAGE;
+      const unsigned row0 = (unsigned)key0 & (unsigned)(a.ps - 1);
+      // (a key that no row sees reads as zeros, by an offset past the buffer)
+      const bool in = (unsigned)(key0 + l16 - k_min) < (unsigned)(held - k_min);
+      const uint8_t* p = static_cast<const uint8_t*>(i ? a.v_cache : a.k_cache) + at_h + (size_t)max(id, 0) * page_bytes;
+      const auto r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, mine && id >= 0 ? head_bytes : 0u, BUFFER_FLAGS);
+      if constexpr (D == 128) {
+        w.code[i] = __builtin_bit_cast(Codes, __builtin_amdgcn_raw_buffer_load_b128(r, in ? at_code : BUF_OOB, row0 * (D / 2), 0));
+      } else {
+        w.code[i] = __builtin_bit_cast(Codes, __builtin_amdgcn_raw_buffer_load_b64(r, in ? at_code : BUF_OOB, row0 * (D / 2), 0));
+      }
+      w.scale[i] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(r, in ? at_scale : BUF_OOB, row0 * (D / MX_BLOCK), 0);
+    }
+  };
+  auto store = [&](const Raw& w, bf16* st) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if (C::NW != 4 && (unsigned)k16[i] >= (unsigned)KT) continue;   // (uniform)
+#pragma unroll
+      for (int s = 0; s < NS; ++s)
+        *reinterpret_cast<bf16x8*>(st + i * TILE + kv_off<bf16, CPR>(k16[i] + l16, CH * c4 + 8 * s)) =
+            mx_widen(reinterpret_cast<const unsigned*>(&w.code[i])[s], w.scale[i]);
+    }
+  };
+  // keys [base, base + KT) below end of a stage
+  auto compute = [&](int base, int end, const bf16* stage) {
+    const int hi = min(hi0, end), all_hi = min(all_hi0, end), any_hi = min(any_hi0, end);
+    const unsigned span = (unsigned)max(hi - lo, 0);
+#pragma unroll
+    for (int kb = 0; kb < NKB; ++kb) {
+      const int key0 = 32 * (kw * NKB + kb), mine = base + key0;
+      if (!live || mine >= any_hi || mine + 32 <= any_lo) continue;   // (uniform)
+      bf16x8 kf[NQ];
+#pragma unroll
+      for (int s = 0; s < NQ; ++s) kf[s] = ld8(stage + kv_off<bf16, CPR>(key0 + l32, 16 * s + 8 * hf));
+      f32x16 st = zero16();
+#pragma unroll
+      for (int s = 0; s < NQ; ++s) st = mma32(kf[s], qf[s], st);
+      // V is on its way from LDS beside the products and the softmax (the scheduler would have each read right before its use)
+      bf16x8 vv[2][NDB];
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) vv[s][db] = v_frag<CPR>(stage + TILE, key0 / 16 + s, db, lane);
+      __builtin_amdgcn_sched_barrier(0);
+      if (!(mine + 32 <= all_hi && mine >= all_lo)) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if ((unsigned)(mine + 8 * (i / 4) + 4 * hf + i % 4 - lo) >= span) st[i] = -INFINITY;
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, st[i]);
+      mx = half_max(mx) * a.scale_log2;
+      if (__any(mx > m_run + CHUNK_SLACK)) {   // (a row's own scores alone decide)
+        const float m_new = mx > m_run + CHUNK_SLACK ? mx : m_run;
+        const float alpha = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
+        l_run *= alpha;
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) o[db] *= alpha;
+        m_run = m_new;
+      }
+      const float m_use = m_run == -INFINITY ? 0.f : m_run;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        st[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[i], a.scale_log2, -m_use));
+        l_run += st[i];
+      }
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {   // (P as bf16: see FewRows)
+        bf16x8 pf;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) pf[j] = f2bf(st[8 * s + j]);
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) {
+          bf16x8 vf = vv[s][db];
+          if constexpr (ODD) {   // (see FewRows)
+            s16x8 bits = __builtin_bit_cast(s16x8, vf), up, dn, sees;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const bool fin = (bits[j] & 0x7f80) != 0x7f80, nan = !fin && (bits[j] & 0x7f);
+              const int key = mine + 16 * s + 8 * (j / 4) + 4 * hf + j % 4;
+              up[j] = (short)(!fin && (nan || bits[j] >= 0) ? 0x7f7f : 0);
+              dn[j] = (short)(!fin && (nan || bits[j] < 0) ? 0xff7f : 0);
+              sees[j] = (short)(key >= lo && key < hi ? 0x7f7f : 0);
+              if (!fin) bits[j] = 0;
+            }
+            o[db] += mma32(__builtin_bit_cast(bf16x8, up), __builtin_bit_cast(bf16x8, sees), zero16());
+            o[db] += mma32(__builtin_bit_cast(bf16x8, dn), __builtin_bit_cast(bf16x8, sees), zero16());
+            vf = __builtin_bit_cast(bf16x8, bits);
+          }
+          o[db] = mma32(vf, pf, o[db]);
+        }
+      }
+    }
+  };
+  bf16 *st0 = lds, *st1 = lds + 2 * TILE;
+
+  // cached keys: step t is multiplied while step t + 1 goes into the other stage and the two behind it are on their way
+  // (keys past the last read as zeros)
+  const int n = held > from ? (held - from + KT - 1) / KT : 0;
+  if (n > 0) {
+    Raw r0, r1;
+    load(from, r0);
+    load(from + KT, r1);
+    wg_barrier();   // (the stages are free: another unit may have used them)
+    store(r0, st0);
+    load(from + 2 * KT, r0);
+    auto step = [&](int t, bf16* mine, bf16* other, Raw& w) {
+      wait_vm_lgkm0<63>();
+      wg_barrier();   // every wave's part of step t is in LDS, and every wave has left the other stage
+      store(w, other);
+      load(from + (t + 3) * KT, w);
+      compute(from + t * KT, held, mine);
+    };
+    for (int t = 0; t < n; t += 2) {
+      step(t, st0, st1, r1);
+      if (t + 1 < n) step(t + 1, st1, st0, r0);
+    }
+  }
+  // the new tokens' keys beside the cache, as they are
+  if (a.k_new && u.k1 > u.L) {
+    const size_t stride = (size_t)a.Hkv * D, at_new = (size_t)u.row0 * stride + h * D;
+    for (int base = max(k_min, u.L); base < u.k1; base += KT) {
+      wg_barrier();
+      for (int i = tid; i < 2 * KT * D / 8; i += C::NT) {
+        const bool is_k = i < KT * D / 8;
+        const int row = i / (D / 8) % KT, d = i % (D / 8) * 8, key = base + row;
+        const bf16* p = static_cast<const bf16*>(is_k ? a.k_new : a.v_new);
+        *reinterpret_cast<bf16x8*>(st0 + (is_k ? 0 : TILE) + kv_off<bf16, CPR>(row, d)) =
+            key < u.k1 ? ld8(p + at_new + (size_t)(key - u.L) * stride + d) : zero8();
+      }
+      wait_vm_lgkm0<63>();
+      wg_barrier();
+      compute(base, INT_MAX, st0);
+    }
+  }
+  float l = half_sum(l_run);
+  // the results of the two halves of the keys, put together by the first
+  if constexpr (C::KW > 1) {
+    wg_barrier();
+    float* row = reinterpret_cast<float*>(lds) + (size_t)c * (D + 4);
+    if (kw == 1) {
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *reinterpret_cast<f32x4*>(row + 32 * db + 8 * q + 4 * hf) =
+              f32x4{o[db][4 * q], o[db][4 * q + 1], o[db][4 * q + 2], o[db][4 * q + 3]};
+      if (hf == 0) *reinterpret_cast<float2*>(row + D) = float2{m_run, l};
+    }
+    wait_vm_lgkm0<63>();
+    wg_barrier();
+    if (kw == 0) {
+      const float2 ml = *reinterpret_cast<const float2*>(row + D);
+      const float m = fmaxf(m_run, ml.x), m_use = m == -INFINITY ? 0.f : m;
+      const float f0 = __builtin_amdgcn_exp2f(m_run - m_use), f1 = __builtin_amdgcn_exp2f(ml.x - m_use);
+      m_run = m;
+      l = l * f0 + ml.y * f1;
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const f32x4 other = *reinterpret_cast<const f32x4*>(row + 32 * db + 8 * q + 4 * hf);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[db][4 * q + i] = o[db][4 * q + i] * f0 + other[i] * f1;
+        }
+    }
+  }
+  if (!real || kw != 0) return found;
+  // lane holds O[row l32][d = 32 db + 8 q + 4 hf + i]
+  bool bad = false;
+  const float inv = hi0 > lo ? 1.f / l : 0.f;   // (a row that sees no key is zero)
+  bf16* dst = static_cast<bf16*>(a.o) + at_q + 4 * hf;
+  const size_t pr = ((size_t)max(u.slot, 0) * a.Hkv + h) * C::ROWS + c;
+  float* po = a.part_o + pr * D + 4 * hf;
+#pragma unroll
+  for (int db = 0; db < NDB; ++db)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      f32x4 v = {o[db][4 * q], o[db][4 * q + 1], o[db][4 * q + 2], o[db][4 * q + 3]};
+      if constexpr (!ODD) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) bad |= !(fabsf(v[i]) < INFINITY);
+      }
+      if (u.slot < 0) {
+        v *= inv;
+        *reinterpret_cast<bf16x4*>(dst + 32 * db + 8 * q) = bf16x4{f2bf(v[0]), f2bf(v[1]), f2bf(v[2]), f2bf(v[3])};
+      } else {
+        *reinterpret_cast<f32x4*>(po + 32 * db + 8 * q) = v;
+      }
+    }
+  if (u.slot >= 0 && hf == 0) *reinterpret_cast<float2*>(a.part_ml + pr * 2) = float2{m_run, l};
+  return found | (bad ? UNIT_ODD : 0);
+}
+
+// ----------------------------------------------------------------------------- launch
+
+template <bool ODD, int D, int NCT>
+__device__ __forceinline__ int run_unit(Few<D, NCT> v, const ChunkAttnArgs& a, const ChunkUnit& u, int h, bf16* lds) {
+  return few_unit<ODD>(v, a, u, h, lds);
+}
+template <bool ODD, int D, int RW, int KW>
+__device__ __forceinline__ int run_unit(Share<D, RW, KW> v, const ChunkAttnArgs& a, const ChunkUnit& u, int h, bf16* lds) {
+  return share_unit<ODD>(v, a, u, h, lds);
+}
+
+__device__ __forceinline__ ChunkUnit uniform(ChunkUnit u) {   // (the same in every lane, which the compiler cannot tell)
+  auto f = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+  return ChunkUnit{f(u.b), f(u.tile), f(u.k0), f(u.k1), f(u.slot), f(u.row0), f(u.n), f(u.L)};
+}
+
+// Workgroup (column, head) does the units of its column one after the other.  (256 threads at least: see chunk_attn_kernel)
 template <class C>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(C::WPE))) few_kernel(ChunkAttnArgs a) {
-  __shared__ __align__(16) bf16 stage[C::STAGE];
+__global__ void __launch_bounds__(C::NT > 256 ? C::NT : 256) __attribute__((amdgpu_waves_per_eu(C::WPE))) few_kernel(ChunkAttnArgs a) {
+  __shared__ __align__(16) bf16 lds[C::LDS];
   const int h = blockIdx.x % a.Hkv, w = blockIdx.x / a.Hkv;
   const int end = a.first[w + 1];
   for (int i = a.first[w]; i < end; ++i) {
-    const ChunkUnit u = a.units[i];
-    const bool bad = few_unit<false, C>(a, u, h, stage);
+    const ChunkUnit u = uniform(a.units[i]);
+    const int found = run_unit<false>(C{}, a, u, h, lds);
     // (one entry a wave at most: the same item twice is done twice, with the same result)
-    if (a.redo && __any(bad) && (threadIdx.x & 63) == 0) {
-      const int at = atomicAdd(a.status + 3, 1);
-      if (at < a.max_redo) a.redo[at] = i * a.Hkv + h;
+    const bool odd = __any(found & UNIT_ODD);
+    if ((threadIdx.x & 63) == 0) {
+      if (found & UNIT_BAD_PAGE) set_status(a.status, ST_BAD_PAGE);
+      if (a.redo && odd) {
+        const int at = atomicAdd(a.status + 3, 1);
+        if (at < a.max_redo) a.redo[at] = i * a.Hkv + h;
+      }
     }
   }
 }
 // The units some row of which came out infinite or NaN, once more with masked values kept apart.
 template <class C>
 __global__ void __launch_bounds__(C::NT) few_redo_kernel(ChunkAttnArgs a) {
-  __shared__ __align__(16) bf16 stage[C::STAGE];
+  __shared__ __align__(16) bf16 lds[C::LDS];
   const int n = min(a.status[3], a.max_redo);
   for (int i = blockIdx.x; i < n; i += gridDim.x) {
     const int item = a.redo[i];
-    const ChunkUnit u = a.units[item / a.Hkv];
-    few_unit<true, C>(a, u, item % a.Hkv, stage);
+    const ChunkUnit u = uniform(a.units[item / a.Hkv]);
+    run_unit<true>(C{}, a, u, item % a.Hkv, lds);
   }
 }
 

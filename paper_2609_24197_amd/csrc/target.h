@@ -132,27 +132,28 @@ inline void chunk_bounds(ChunkAttnArgs& a) {
   plan_bounds(a, waves);
 }
 
-// Over the 4-bit cache.  bf16 rows up to 96 of a request take waves that walk the keys by themselves (chunk_few.h), 16,
-// 32 or 48 rows each: two of them share a workgroup past 48, so that the second finds its keys in the cache.
+// Over the 4-bit cache, bf16 rows up to 128 of a request take the tiles of chunk_few.h: 16 or 32 rows are a wave's, more are
+// divided over the waves of a workgroup.
 struct MxTile {
-  int ct, waves;   // 16-row blocks of a wave, waves; ct = 0: the tiles of chunk_bounds
+  int ct, rw, kw;   // 16-row blocks of a wave, waves that divide the rows and a step's keys; ct = 0: the tiles of chunk_bounds
 };
 inline MxTile mx_tile(const ChunkAttnArgs& a) {
   const long long R = (long long)a.max_new * (a.Hq / a.Hkv);
-  if (a.f32 || R > 96) return MxTile{0, 0};
-  return R <= 16 ? MxTile{1, 1} : R <= 32 ? MxTile{2, 1} : R <= 48 ? MxTile{3, 1} : R <= 64 ? MxTile{2, 2} : MxTile{3, 2};
+  if (a.f32 || R > 128) return MxTile{0, 0, 0};
+  return R <= 16 ? MxTile{1, 1, 1} : R <= 32 ? MxTile{2, 1, 1} : R <= 64 ? MxTile{2, 2, 2} : R <= 96 ? MxTile{2, 3, 2} : MxTile{2, 4, 2};
 }
 inline void mx_bounds(ChunkAttnArgs& a) {
   const MxTile t = mx_tile(a);
   if (!t.ct) return chunk_bounds(a);
-  a.tile_rows = 16 * t.ct * t.waves;
+  a.tile_rows = 16 * t.ct * t.rw;
   a.key_tile = 64;
   // as many columns as workgroups run at once, and no more than there can be steps
   const long long most = std::min<long long>(a.T, a.B) * ((a.cap + 63LL) / 64 + 1);
-  a.slots = (t.ct == 1 ? 12 : 8) / t.waves * 256;
+  const int waves = t.rw * t.kw;
+  a.slots = std::max((t.ct == 1 ? 12 : 8) / waves, 1) * 256;
   a.columns = (int)std::max(1LL, std::min<long long>(a.slots / a.Hkv, most));
   a.target = a.columns * a.Hkv;
-  plan_bounds(a, t.waves);
+  plan_bounds(a, waves);
 }
 hipError_t launch_chunk_attn(const ChunkAttnArgs& a, hipStream_t s);
 hipError_t launch_chunk_attn_mx(const ChunkAttnArgs& a, hipStream_t s);
