@@ -17,6 +17,7 @@ namespace {
 
 constexpr int AJ_THREADS = 256;
 constexpr int AJ_VEC = 8;                     // tokens a thread takes side by side: a byte of the mask
+constexpr int AJ_PART = 64;                   // rows of a workgroup at most
 constexpr unsigned AJ_PROMPT = 0x80000000u;   // in a token's count: it stands in the prompt
 constexpr int ST_BAD_TOKEN = 4, ST_NONFINITE = 8;
 
@@ -123,12 +124,26 @@ __device__ __forceinline__ void store8(T* p, int n, const float (&v)[AJ_VEC]) {
   }
 }
 
+// A thread's tokens of a row on their way: their logits and, per group of 8, their byte of the mask.
+template <int G>
+struct RowRegs {
+  float x[G][AJ_VEC];
+  unsigned bits[G];
+};
+// What stays the same over a request's rows, of the thread's tokens, but for the drafts that come to it.
+template <int G>
+struct TokenRegs {
+  float bias[G][AJ_VEC], less[G][AJ_VEC];
+  unsigned seen[G];
+};
+
 // Slice blockIdx.x of the vocabulary, request blockIdx.y, part blockIdx.z of its rows.
 template <class Tin, class Tout, int G>
 __global__ void __launch_bounds__(AJ_THREADS) adjust_kernel(AdjustArgs a, int part) {
   constexpr int S = AJ_THREADS * AJ_VEC * G, GS = AJ_THREADS * AJ_VEC;
-  __shared__ unsigned s_cnt[S];
-  __shared__ int s_bias[S];   // entry of the bias list, from 1 on
+  __shared__ __align__(16) unsigned s_cnt[S];
+  __shared__ __align__(16) int s_bias[S];   // entry of the bias list, from 1 on
+  __shared__ int s_draft[AJ_PART], s_mask[AJ_PART];   // of each row: the draft that comes after it (-1: none), its line of the mask
   const int tid = threadIdx.x, b = blockIdx.y;
   if (blockIdx.x == gridDim.x - 1) {
     if (b == 0 && blockIdx.z == 0) check_call(a);
@@ -138,63 +153,60 @@ __global__ void __launch_bounds__(AJ_THREADS) adjust_kernel(AdjustArgs a, int pa
   const ChunkRows rows = request_rows(a, b);
   const int j0 = blockIdx.z * part, j1 = min(j0 + part, rows.n);
   if (j0 >= j1) return;
-  const Tin* src = static_cast<const Tin*>(a.logits) + (size_t)(rows.row0 + j0) * a.V;
-  Tout* dst = static_cast<Tout*>(a.out) + (size_t)(rows.row0 + j0) * a.V;
-  const int words = (a.V + 31) / 32;
-  int v[G], left[G];   // first token of a group, and how many of the row are left there
-#pragma unroll
-  for (int g = 0; g < G; ++g) {
-    v[g] = v0 + g * GS + tid * AJ_VEC;
-    left[g] = a.V - v[g];
-  }
-  float n[G][AJ_VEC];        // the next row's logits and mask, on their way
-  unsigned nbits[G];
-  auto fetch = [&](int j) {
-    const int r = rows.row0 + j;
-    int m = -1;
-    if (a.mask) m = a.mask_rows ? a.mask_rows[r] : r;
-    const bool masked = m >= 0 && m < a.masks;
-#pragma unroll
-    for (int g = 0; g < G; ++g) {
-      nbits[g] = 0xff;
-      if (left[g] <= 0) continue;
-      load8(src + (size_t)(j - j0) * a.V + v[g], left[g], n[g]);
-      if (masked) nbits[g] = reinterpret_cast<const uint8_t*>(a.mask + (size_t)m * words)[v[g] / 8];
-    }
-  };
-  fetch(j0);
+  const Tin* src = static_cast<const Tin*>(a.logits) + (size_t)(rows.row0 + j0) * a.V + v0 + tid * AJ_VEC;
+  Tout* dst = static_cast<Tout*>(a.out) + (size_t)(rows.row0 + j0) * a.V + v0 + tid * AJ_VEC;
+  const int left = a.V - v0 - tid * AJ_VEC;   // tokens from this thread's first one on
+  const bool whole = v0 + S <= a.V;           // (uniform)
 
-  for (int i = tid; i < S; i += AJ_THREADS) {
-    s_cnt[i] = 0;
-    s_bias[i] = 0;
+  for (int i = tid; i < S / 4; i += AJ_THREADS) {
+    reinterpret_cast<u32x4*>(s_cnt)[i] = u32x4{0u, 0u, 0u, 0u};
+    reinterpret_cast<u32x4*>(s_bias)[i] = u32x4{0u, 0u, 0u, 0u};
+  }
+  for (int j = j0 + tid; j < j1; j += AJ_THREADS) {
+    s_draft[j - j0] = a.draft_tokens && j + 1 < rows.n ? draft_id(a, b, j) : -1;
+    int m = -1;
+    if (a.mask) m = a.mask_rows ? a.mask_rows[rows.row0 + j] : rows.row0 + j;
+    s_mask[j - j0] = m < a.masks ? m : -1;
   }
   const History h = history(a, b);
   const Penalties pen = penalties(a, b);
   __syncthreads();
   const int32_t* said = a.history + (size_t)b * a.max_hist;
-  constexpr int U = 8;
-  for (int i0 = 0; i0 < h.n; i0 += U * AJ_THREADS) {
+  auto count = [&](int id, int i) {
+    const unsigned at = (unsigned)id - (unsigned)v0;
+    if (id >= 0 && at < S) {
+      if (i < h.old) atomicOr(&s_cnt[at], AJ_PROMPT);
+      else atomicAdd(&s_cnt[at], 1u);
+    }
+  };
+  typedef int Int4 __attribute__((ext_vector_type(4), aligned(4)));
+  constexpr int U = 4;
+  int at0 = 0;
+  for (; at0 + 4 * U * AJ_THREADS <= h.n; at0 += 4 * U * AJ_THREADS) {
+    Int4 id[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) id[u] = *reinterpret_cast<const Int4*>(said + at0 + (u * AJ_THREADS + tid) * 4);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) count(id[u][e], at0 + (u * AJ_THREADS + tid) * 4 + e);
+  }
+  for (; at0 < h.n; at0 += U * AJ_THREADS) {
     int id[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int i = i0 + u * AJ_THREADS + tid;
-      id[u] = i < h.n ? said[i] : -1;
-    }
+    for (int u = 0; u < U; ++u) id[u] = said[min(at0 + u * AJ_THREADS + tid, h.n - 1)];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int i = i0 + u * AJ_THREADS + tid;
-      const unsigned at = (unsigned)id[u] - (unsigned)v0;
-      if (id[u] >= 0 && at < S) {
-        if (i < h.old) atomicOr(&s_cnt[at], AJ_PROMPT);
-        else atomicAdd(&s_cnt[at], 1u);
-      }
+      const int i = at0 + u * AJ_THREADS + tid;
+      if (i < h.n) count(id[u], i);
     }
   }
-  for (int j = tid; j < j0; j += AJ_THREADS) {   // (k = 0: j0 = 0)
-    if (!a.draft_tokens) break;
-    const int t = draft_id(a, b, j);
-    const unsigned at = (unsigned)t - (unsigned)v0;
-    if (t >= 0 && at < S) atomicAdd(&s_cnt[at], 1u);
+  if (a.draft_tokens) {   // the drafts of the parts before
+    for (int j = tid; j < j0; j += AJ_THREADS) {
+      const int t = draft_id(a, b, j);
+      const unsigned at = (unsigned)t - (unsigned)v0;
+      if (t >= 0 && at < S) atomicAdd(&s_cnt[at], 1u);
+    }
   }
   for (int i = tid; i < a.n_bias; i += AJ_THREADS) {
     const int t = a.bias_ids[(size_t)b * a.n_bias + i];
@@ -206,57 +218,95 @@ __global__ void __launch_bounds__(AJ_THREADS) adjust_kernel(AdjustArgs a, int pa
     const unsigned said_n = c & ~AJ_PROMPT;
     return said_n ? fmaf(pen.phi, (float)said_n, pen.pi) : 0.f;
   };
-  float bias[G][AJ_VEC], less[G][AJ_VEC];
-  unsigned seen[G];
+  TokenRegs<G> k;
 #pragma unroll
   for (int g = 0; g < G; ++g) {
-    seen[g] = 0;
+    k.seen[g] = 0;
 #pragma unroll
     for (int e = 0; e < AJ_VEC; ++e) {
       const int at = g * GS + tid * AJ_VEC + e;
       const unsigned c = s_cnt[at];
       const int i = s_bias[at];
-      seen[g] |= (c ? 1u : 0u) << e;
-      less[g][e] = cost(c);
-      bias[g][e] = i ? a.bias[(size_t)b * a.n_bias + i - 1] : 0.f;
+      k.seen[g] |= (c ? 1u : 0u) << e;
+      k.less[g][e] = cost(c);
+      k.bias[g][e] = i ? a.bias[(size_t)b * a.n_bias + i - 1] : 0.f;
     }
   }
-  for (int j = j0; j < j1; ++j) {
-    float x[G][AJ_VEC];
-    unsigned bits[G];
+  const int words = (a.V + 31) / 32;
+  const uint8_t* mask = reinterpret_cast<const uint8_t*>(a.mask);
+  // this thread's mask byte of row j, group g; where there is no mask, some byte that is there
+  auto mask_at = [&](int m, int g) -> const uint8_t* {
+    return m >= 0 ? mask + (size_t)m * words * 4 + (v0 + g * GS) / 8 + tid : reinterpret_cast<const uint8_t*>(a.logits);
+  };
+  auto adjusted = [&](RowRegs<G>& r) {
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-      bits[g] = nbits[g];
-#pragma unroll
-      for (int e = 0; e < AJ_VEC; ++e) x[g][e] = n[g][e];
-    }
-    if (j + 1 < j1) fetch(j + 1);
-#pragma unroll
-    for (int g = 0; g < G; ++g) {
+    for (int g = 0; g < G; ++g)
 #pragma unroll
       for (int e = 0; e < AJ_VEC; ++e) {
-        float y = x[g][e] + bias[g][e];
-        y *= seen[g] >> e & 1 ? (y > 0.f ? pen.inv_rho : pen.rho) : 1.f;
-        y -= less[g][e];
-        x[g][e] = bits[g] >> e & 1 ? y : -INFINITY;
+        float y = r.x[g][e] + k.bias[g][e];
+        y *= k.seen[g] >> e & 1 ? (y > 0.f ? pen.inv_rho : pen.rho) : 1.f;
+        y -= k.less[g][e];
+        r.x[g][e] = r.bits[g] >> e & 1 ? y : -INFINITY;
       }
-      if (left[g] > 0) store8(dst + (size_t)(j - j0) * a.V + v[g], left[g], x[g]);
+  };
+  auto said_next = [&](int t) {   // the draft behind a row joins what was said
+    const unsigned at = (unsigned)t - (unsigned)v0;
+    if (t >= 0 && at < S && (int)(at % GS / AJ_VEC) == tid) {   // (this thread alone reads the token's count from here on)
+      const float c = cost(s_cnt[at] += 1);
+#pragma unroll
+      for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int e = 0; e < AJ_VEC; ++e)
+          if (at == (unsigned)(g * GS + tid * AJ_VEC + e)) {
+            k.less[g][e] = c;
+            k.seen[g] |= 1u << e;
+          }
     }
-    if (a.draft_tokens && j + 1 < j1) {
-      const int t = draft_id(a, b, j);
-      const unsigned at = (unsigned)t - (unsigned)v0;
-      if (t >= 0 && at < S && (int)(at % GS / AJ_VEC) == tid) {   // (this thread alone reads the token's count from here on)
-        const float c = cost(s_cnt[at] += 1);
+  };
+  if (whole) {
+    // No branch around a load or store, so that a row's waits are for its own: with them 64 requests of 17 rows of 131072
+    // take 195 us.
+    auto fetch = [&](int j, RowRegs<G>& r) {
+      const int i = min(j, j1 - 1) - j0, m = __builtin_amdgcn_readfirstlane(s_mask[i]);
 #pragma unroll
-        for (int g = 0; g < G; ++g)
-#pragma unroll
-          for (int e = 0; e < AJ_VEC; ++e)
-            if (at == (unsigned)(g * GS + tid * AJ_VEC + e)) {
-              less[g][e] = c;
-              seen[g] |= 1u << e;
-            }
+      for (int g = 0; g < G; ++g) {
+        load8(src + (size_t)i * a.V + g * GS, AJ_VEC, r.x[g]);
+        r.bits[g] = *mask_at(m, g) | (m >= 0 ? 0u : 0xffu);
       }
+    };
+    auto row = [&](int j, RowRegs<G>& r) {
+      adjusted(r);
+#pragma unroll
+      for (int g = 0; g < G; ++g) store8(dst + (size_t)(j - j0) * a.V + g * GS, AJ_VEC, r.x[g]);
+      said_next(__builtin_amdgcn_readfirstlane(s_draft[j - j0]));
+    };
+    RowRegs<G> r0, r1;
+    fetch(j0, r0);
+    for (int j = j0; j < j1; j += 2) {
+      fetch(j + 1, r1);
+      row(j, r0);
+      if (j + 1 >= j1) break;
+      fetch(j + 2, r0);
+      row(j + 1, r1);
     }
+    return;
+  }
+  // the last slice
+  for (int j = j0; j < j1; ++j) {
+    RowRegs<G> r;
+    const int m = __builtin_amdgcn_readfirstlane(s_mask[j - j0]);
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      r.bits[g] = 0xff;
+      if (left <= g * GS) continue;
+      load8(src + (size_t)(j - j0) * a.V + g * GS, left - g * GS, r.x[g]);
+      if (m >= 0) r.bits[g] = *mask_at(m, g);
+    }
+    adjusted(r);
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+      if (left > g * GS) store8(dst + (size_t)(j - j0) * a.V + g * GS, left - g * GS, r.x[g]);
+    said_next(s_draft[j - j0]);
   }
 }
 
@@ -265,7 +315,7 @@ hipError_t launch_g(const AdjustArgs& a, hipStream_t s) {
   const int slices = (a.V + AJ_THREADS * AJ_VEC * G - 1) / (AJ_THREADS * AJ_VEC * G);
   // workgroups enough for the chip: the rows of a request are split where slices and requests make too few
   const long long wgs = (long long)slices * a.B;
-  const int parts = (int)std::max(1LL, std::min<long long>(a.k + 1, 1024 / wgs));
+  const int parts = (int)std::max<long long>((a.k + AJ_PART) / AJ_PART, std::min<long long>(a.k + 1, 1024 / wgs));
   const int part = (a.k + parts) / parts;
   const dim3 grid(slices + 1, a.B, (a.k + part) / part);
   hipLaunchKernelGGL((adjust_kernel<Tin, Tout, G>), grid, dim3(AJ_THREADS), 0, s, a, part);
