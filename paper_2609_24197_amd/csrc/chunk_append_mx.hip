@@ -207,7 +207,7 @@ hipError_t launch_typed(const ChunkAppendArgs& a, hipStream_t s) {
 constexpr int RD_ROWS = 4;
 
 // RD_ROWS rows per workgroup; a lane takes a word of 8 channels at a time, so that a wave's stores are whole lines.
-template <class T>
+template <class T, int D>
 __global__ void __launch_bounds__(AP_THREADS) chunk_read_mx_kernel(ChunkAppendArgs a, T* k, T* v) {
   if (blockIdx.x == gridDim.x - 1) {
     check_call(a);
@@ -224,28 +224,44 @@ __global__ void __launch_bounds__(AP_THREADS) chunk_read_mx_kernel(ChunkAppendAr
     }
   }
   __syncthreads();
-  const int D = a.D, wpr = a.Hkv * D / 8;   // words of a row and tensor
+  const int wpr = a.Hkv * D / 8;   // words of a row and tensor
   const size_t head_bytes = mx_head_bytes(a.ps, D);
-  for (int i = tid; i < 2 * RD_ROWS * wpr; i += AP_THREADS) {
-    const int t = i / (2 * wpr), w = i % wpr;
-    const bool is_k = i / wpr % 2 == 0;
-    const int pos = s_pos[t], page = s_page[t];
-    if (pos < 0) continue;
-    const int h = w / (D / 8), d = w % (D / 8) * 8, row = pos & (a.ps - 1);
-    unsigned code = 0, scale = 0;   // (a position that is not mapped reads as zeros)
-    if (page >= 0) {
-      const uint8_t* p = static_cast<const uint8_t*>(is_k ? a.k_cache : a.v_cache) + ((size_t)page * a.Hkv + h) * head_bytes;
-      code = *reinterpret_cast<const unsigned*>(p + row * (D / 2) + d / 2);
-      scale = p[a.ps * (D / 2) + row * (D / MX_BLOCK) + d / MX_BLOCK];
+  // a thread's next word, and which of the rows' k and v in turn it is of; counted on, not divided anew
+  int q = tid / wpr, w = tid % wpr;
+  const int dq = AP_THREADS / wpr, dw = AP_THREADS % wpr;
+  constexpr int U = 4;   // words of a thread on their way together
+  for (int i0 = tid; i0 < 2 * RD_ROWS * wpr; i0 += U * AP_THREADS) {
+    unsigned code[U], scale[U];
+    T* dst[U];
+#pragma unroll
+    for (int x = 0; x < U; ++x) {
+      const int t = min(q >> 1, RD_ROWS - 1);
+      const bool is_k = (q & 1) == 0;
+      const int pos = s_pos[t], page = s_page[t];
+      const int h = w / (D / 8), d = w % (D / 8) * 8, row = pos & (a.ps - 1);
+      const uint8_t* p = static_cast<const uint8_t*>(is_k ? a.k_cache : a.v_cache) + ((size_t)max(page, 0) * a.Hkv + h) * head_bytes;
+      code[x] = *reinterpret_cast<const unsigned*>(p + row * (D / 2) + d / 2);
+      scale[x] = p[a.ps * (D / 2) + row * (D / MX_BLOCK) + d / MX_BLOCK];
+      if (page < 0) code[x] = scale[x] = 0;   // (a position that is not mapped reads as zeros)
+      dst[x] = q < 2 * RD_ROWS && pos >= 0 ? (is_k ? k : v) + ((size_t)(r0 + t) * a.Hkv + h) * D + d : nullptr;
+      q += dq;
+      w += dw;
+      if (w >= wpr) {
+        w -= wpr;
+        ++q;
+      }
     }
-    T* dst = (is_k ? k : v) + ((size_t)(r0 + t) * a.Hkv + h) * D + d;
-    if constexpr (sizeof(T) == 4) {
-      f32x4 lo, hi;
-      mx_widen(code, scale, lo, hi);
-      *reinterpret_cast<f32x4*>(dst) = lo;
-      *reinterpret_cast<f32x4*>(dst + 4) = hi;
-    } else {
-      *reinterpret_cast<bf16x8*>(dst) = mx_widen(code, scale);
+#pragma unroll
+    for (int x = 0; x < U; ++x) {
+      if (!dst[x]) continue;
+      if constexpr (sizeof(T) == 4) {
+        f32x4 lo, hi;
+        mx_widen(code[x], scale[x], lo, hi);
+        *reinterpret_cast<f32x4*>(dst[x]) = lo;
+        *reinterpret_cast<f32x4*>(dst[x] + 4) = hi;
+      } else {
+        *reinterpret_cast<bf16x8*>(dst[x]) = mx_widen(code[x], scale[x]);
+      }
     }
   }
 }
@@ -259,12 +275,15 @@ hipError_t launch_chunk_append_mx(const ChunkAppendArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_chunk_read_mx(const ChunkAppendArgs& a, void* k, void* v, hipStream_t s) {
-  const dim3 grid((a.T + RD_ROWS - 1) / RD_ROWS + 1);
-  if (a.out_f32)
-    hipLaunchKernelGGL(chunk_read_mx_kernel<float>, grid, dim3(AP_THREADS), 0, s, a, static_cast<float*>(k), static_cast<float*>(v));
-  else
-    hipLaunchKernelGGL(chunk_read_mx_kernel<bf16>, grid, dim3(AP_THREADS), 0, s, a, static_cast<bf16*>(k), static_cast<bf16*>(v));
-  return hipGetLastError();
+  if (a.D != 64 && a.D != 128) return hipErrorInvalidValue;
+  auto launch = [&](auto t, auto d) {
+    typedef typename decltype(t)::type T;
+    hipLaunchKernelGGL((chunk_read_mx_kernel<T, decltype(d)::value>), dim3((a.T + RD_ROWS - 1) / RD_ROWS + 1), dim3(AP_THREADS), 0, s,
+                       a, static_cast<T*>(k), static_cast<T*>(v));
+    return hipGetLastError();
+  };
+  if (a.out_f32) return a.D == 128 ? launch(std::common_type<float>{}, Int<128>{}) : launch(std::common_type<float>{}, Int<64>{});
+  return a.D == 128 ? launch(std::common_type<bf16>{}, Int<128>{}) : launch(std::common_type<bf16>{}, Int<64>{});
 }
 
 }  // namespace hspec
