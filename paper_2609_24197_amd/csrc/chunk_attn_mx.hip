@@ -34,8 +34,10 @@ hipError_t launch_few_rows(const ChunkAttnArgs& a, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_chunk_attn_mx(const ChunkAttnArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL(chunk_plan, dim3(1), dim3(PL_THREADS), 0, s, a);
-  if (hipError_t e = hipGetLastError()) return e;
+  if (!a.columns || a.first) {
+    hipLaunchKernelGGL(chunk_plan, dim3(1), dim3(PL_THREADS), 0, s, a);
+    if (hipError_t e = hipGetLastError()) return e;
+  }
   if (a.columns) return a.D == 128 ? launch_few_rows<128>(a, s) : launch_few_rows<64>(a, s);
   return with_variant(a, [&](auto c) { return launch_units<decltype(c)>(a, s); });
 }

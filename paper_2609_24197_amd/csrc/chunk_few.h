@@ -11,6 +11,7 @@
 // the waves of a workgroup share what they widen: RW of them divide the rows, KW the keys of a step, and the KW results
 // are put together at the unit's end.
 #pragma once
+#include "chunk_columns.h"
 #include "chunk_tile.h"
 
 namespace hspec {
@@ -653,48 +654,77 @@ __device__ __forceinline__ ChunkUnit uniform(ChunkUnit u) {   // (the same in ev
   return ChunkUnit{f(u.b), f(u.tile), f(u.k0), f(u.k1), f(u.slot), f(u.row0), f(u.n), f(u.L)};
 }
 
-// Workgroup (column, head) does the units of its column one after the other.  (256 threads at least: see chunk_attn_kernel)
+// Units of a column: the plan's, or found here.  Every wave of the workgroup calls it.
+struct ColumnUnits {
+  const ChunkUnit* at;
+  int n;
+};
+__device__ __forceinline__ ColumnUnits units_of(const ChunkAttnArgs& a, int w, ChunkUnit* found) {
+  if (a.first) {
+    const int i = a.first[w];
+    return ColumnUnits{a.units + i, a.first[w + 1] - i};
+  }
+  const LanePlan p = lane_plan(a);
+  const int n = column_units(a, p, w, threadIdx.x < 64 ? found : nullptr);
+  __syncthreads();
+  return ColumnUnits{found, n};
+}
+
+// Workgroup (column, head) does the units of its column one after the other, and leaves what each of its waves found.  The
+// last workgroup writes the plan down where no kernel has before.  (256 threads at least: see chunk_attn_kernel)
 template <class C>
 __global__ void __launch_bounds__(C::NT > 256 ? C::NT : 256) __attribute__((amdgpu_waves_per_eu(C::WPE))) few_kernel(ChunkAttnArgs a) {
   __shared__ __align__(16) bf16 lds[C::LDS];
-  const int h = blockIdx.x % a.Hkv, w = blockIdx.x / a.Hkv;
-  const int end = a.first[w + 1];
-  for (int i = a.first[w]; i < end; ++i) {
-    const ChunkUnit u = uniform(a.units[i]);
-    const int found = run_unit<false>(C{}, a, u, h, lds);
-    // (one entry a wave at most: the same item twice is done twice, with the same result)
-    const bool odd = __any(found & UNIT_ODD);
-    if ((threadIdx.x & 63) == 0) {
-      if (found & UNIT_BAD_PAGE) set_status(a.status, ST_BAD_PAGE);
-      if (a.redo && odd) {
-        const int at = atomicAdd(a.status + 3, 1);
-        if (at < a.max_redo) a.redo[at] = i * a.Hkv + h;
-      }
-    }
+  __shared__ ChunkUnit s_units[CO_REQUESTS];
+  if (blockIdx.x == (unsigned)a.columns * a.Hkv) {
+    if (threadIdx.x < 64) write_plan(a, lane_plan(a));
+    return;
   }
+  const int h = blockIdx.x % a.Hkv, w = blockIdx.x / a.Hkv;
+  const ColumnUnits us = units_of(a, w, s_units);
+  int found = 0;
+  for (int i = 0; i < us.n; ++i) {
+    const ChunkUnit u = uniform(us.at[i]);
+    found |= run_unit<false>(C{}, a, u, h, lds);
+  }
+  const int bits = (__any(found & UNIT_ODD) ? UNIT_ODD : 0) | (__any(found & UNIT_BAD_PAGE) ? UNIT_BAD_PAGE : 0);
+  if ((threadIdx.x & 63) == 0) a.flags[blockIdx.x * C::NW + threadIdx.x / 64] = bits;
 }
-// The units some row of which came out infinite or NaN, once more with masked values kept apart.
+// The columns some row of which came out infinite or NaN, once more with masked values kept apart (rare).
 template <class C>
 __global__ void __launch_bounds__(C::NT) few_redo_kernel(ChunkAttnArgs a) {
   __shared__ __align__(16) bf16 lds[C::LDS];
-  const int n = min(a.status[3], a.max_redo);
-  for (int i = blockIdx.x; i < n; i += gridDim.x) {
-    const int item = a.redo[i];
-    const ChunkUnit u = uniform(a.units[item / a.Hkv]);
-    run_unit<true>(C{}, a, u, item % a.Hkv, lds);
+  __shared__ ChunkUnit s_units[CO_REQUESTS];
+  const int items = a.columns * a.Hkv, lane = threadIdx.x & 63;
+  for (int i0 = blockIdx.x; i0 < items; i0 += gridDim.x * 64) {   // 64 items a round, a lane looks at one
+    const long long mine = i0 + (long long)gridDim.x * lane;
+    int odd = 0;
+    if (mine < items) {
+#pragma unroll
+      for (int k = 0; k < C::NW; ++k) odd |= a.flags[mine * C::NW + k] & UNIT_ODD;
+    }
+    for (unsigned long long left = __ballot(odd != 0); left; left &= left - 1) {   // (the same in every wave)
+      const int item = i0 + gridDim.x * __builtin_ctzll(left);
+      __syncthreads();   // (the last column's units are read)
+      const ColumnUnits us = units_of(a, item / a.Hkv, s_units);
+      for (int i = 0; i < us.n; ++i) {
+        const ChunkUnit u = uniform(us.at[i]);
+        run_unit<true>(C{}, a, u, item % a.Hkv, lds);
+      }
+    }
   }
 }
 
 template <class C>
 hipError_t launch_few(const ChunkAttnArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL(few_kernel<C>, dim3((unsigned)a.columns * a.Hkv), dim3(C::NT), 0, s, a);
+  const unsigned items = (unsigned)a.columns * a.Hkv;
+  hipLaunchKernelGGL(few_kernel<C>, dim3(items + (a.first ? 0 : 1)), dim3(C::NT), 0, s, a);
   if (hipError_t e = hipGetLastError()) return e;
-  if (a.redo) {
-    const unsigned items = (unsigned)std::min(256LL, (long long)a.max_units * a.Hkv);
-    hipLaunchKernelGGL(few_redo_kernel<C>, dim3(items), dim3(C::NT), 0, s, a);
+  if (a.max_new > 1) {   // (one new token: its rows see the same keys)
+    hipLaunchKernelGGL(few_redo_kernel<C>, dim3(std::min(256u, items)), dim3(C::NT), 0, s, a);
     if (hipError_t e = hipGetLastError()) return e;
   }
-  return launch_merge<bf16, C::D>(a, s);
+  return launch_merge<bf16, C::D>(a, s, C::NW);
 }
 
 }  // namespace

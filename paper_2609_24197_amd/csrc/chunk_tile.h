@@ -592,22 +592,32 @@ __device__ __forceinline__ void merge_store(const ChunkAttnArgs& a, const ChunkS
   if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(dst) = acc;
   else *reinterpret_cast<bf16x4*>(dst) = bf16x4{f2bf(acc[0]), f2bf(acc[1]), f2bf(acc[2]), f2bf(acc[3])};
 }
+// In columns, the last workgroup puts what the units' waves found into the status, which nothing else writes by then.
+__device__ __forceinline__ bool merge_status(const ChunkAttnArgs& a, int waves) {   // whether this workgroup is that one
+  if (!a.flags || blockIdx.x != gridDim.x - 1) return false;
+  int bits = 0;
+  for (int i = threadIdx.x; i < a.columns * a.Hkv * waves; i += MG_THREADS) bits |= a.flags[i];
+  if (bits & 2) set_status(a.status, ST_BAD_PAGE);
+  return true;
+}
 // (A piece that a row sees nothing of has m = -inf, l = 0 and O = 0; no piece is left out for its weight, so that a NaN
 // among the scores or values of one shows as it does where a cache is not split.)
 __device__ __forceinline__ float piece_weight(float m, float m_use) { return __builtin_amdgcn_exp2f(m - m_use); }
 
 template <class T, int D>
-__global__ void __launch_bounds__(MG_THREADS) chunk_merge_rows(ChunkAttnArgs a, int blocks) {
+__global__ void __launch_bounds__(MG_THREADS) chunk_merge_rows(ChunkAttnArgs a, int blocks, int waves) {
+  if (merge_status(a, waves)) return;
+  const int wgs = gridDim.x - (a.flags ? 1 : 0);
   constexpr int PR = MG_THREADS * 4 / D;   // rows per workgroup
   constexpr int U = 4;
   const int g = a.Hq / a.Hkv;
   const int n = a.status[2] * a.Hkv * blocks;
-  for (int w = blockIdx.x; w < n; w += gridDim.x) {
+  for (int w = blockIdx.x; w < n; w += wgs) {
     const int e = w / (a.Hkv * blocks), h = w / blocks % a.Hkv;
     const ChunkSplit s = a.splits[e];
     const int rr = w % blocks * PR + threadIdx.x / (D / 4);   // row of the tile
     const int c = s.tile * a.tile_rows + rr;
-    if (rr >= a.tile_rows || c >= s.n * g) continue;
+    if (s.pieces < 2 || rr >= a.tile_rows || c >= s.n * g) continue;
     const int d = threadIdx.x % (D / 4) * 4;
     const size_t p0 = ((size_t)s.slot * a.Hkv + h) * a.tile_rows + rr, step = (size_t)a.Hkv * a.tile_rows;
     float m = -INFINITY;
@@ -643,18 +653,20 @@ __global__ void __launch_bounds__(MG_THREADS) chunk_merge_rows(ChunkAttnArgs a, 
 }
 
 template <class T, int D>
-__global__ void __launch_bounds__(MG_THREADS) chunk_merge_row(ChunkAttnArgs a, int rows) {
+__global__ void __launch_bounds__(MG_THREADS) chunk_merge_row(ChunkAttnArgs a, int rows, int waves) {
+  if (merge_status(a, waves)) return;
+  const int wgs = gridDim.x - (a.flags ? 1 : 0);
   constexpr int TPR = D / 4, G = MG_THREADS / TPR;   // threads of a row, groups of pieces
   constexpr int U = 4, CH = MG_THREADS;              // pieces in flight per group, pieces per round
   __shared__ float s_w[CH], s_m[MG_THREADS / 64], s_l[MG_THREADS / 64];
   __shared__ __align__(16) f32x4 s_o[MG_THREADS];
   const int g = a.Hq / a.Hkv, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int n = a.status[2] * a.Hkv * rows;
-  for (int w = blockIdx.x; w < n; w += gridDim.x) {
+  for (int w = blockIdx.x; w < n; w += wgs) {
     const int e = w / (a.Hkv * rows), h = w / rows % a.Hkv, rr = w % rows;
     const ChunkSplit s = a.splits[e];
     const int c = s.tile * a.tile_rows + rr;
-    if (c >= s.n * g) continue;   // (uniform)
+    if (s.pieces < 2 || c >= s.n * g) continue;   // (uniform)
     const size_t p0 = ((size_t)s.slot * a.Hkv + h) * a.tile_rows + rr, step = (size_t)a.Hkv * a.tile_rows;
     const int grp = tid / TPR, d = tid % TPR * 4;
     auto piece_o = [&](int i) { return *reinterpret_cast<const f32x4*>(a.part_o + (p0 + min(i, s.pieces - 1) * step) * D + d); };
@@ -710,16 +722,17 @@ __global__ void __launch_bounds__(MG_THREADS) chunk_merge_row(ChunkAttnArgs a, i
 // ----------------------------------------------------------------------------- launch
 
 template <class T, int D>
-hipError_t launch_merge(const ChunkAttnArgs& a, hipStream_t s) {
-  if (a.max_splits > 0) {
+hipError_t launch_merge(const ChunkAttnArgs& a, hipStream_t s, int waves = 0) {
+  const unsigned more = a.flags ? 1 : 0;   // the workgroup of merge_status
+  if (a.max_splits > 0 || a.flags) {
     const long long rows = std::min((long long)a.tile_rows, (long long)a.max_new * (a.Hq / a.Hkv));
     const long long singles = (long long)a.max_splits * a.Hkv * rows;
     if (singles <= MG_FEW) {
-      hipLaunchKernelGGL((chunk_merge_row<T, D>), dim3((unsigned)singles), dim3(MG_THREADS), 0, s, a, (int)rows);
+      hipLaunchKernelGGL((chunk_merge_row<T, D>), dim3((unsigned)singles + more), dim3(MG_THREADS), 0, s, a, (int)rows, waves);
     } else {
       const int blocks = (int)((rows * D / 4 + MG_THREADS - 1) / MG_THREADS);
       const long long wgs = std::min((long long)a.max_splits * a.Hkv * blocks, 2048LL);
-      hipLaunchKernelGGL((chunk_merge_rows<T, D>), dim3((unsigned)wgs), dim3(MG_THREADS), 0, s, a, blocks);
+      hipLaunchKernelGGL((chunk_merge_rows<T, D>), dim3((unsigned)wgs + more), dim3(MG_THREADS), 0, s, a, blocks, waves);
     }
   }
   return hipGetLastError();

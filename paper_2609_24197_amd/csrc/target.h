@@ -60,14 +60,15 @@ struct ChunkAttnArgs {
   int* queue = nullptr;               // [kChunkClasses * kChunkQueueStride]
   ChunkUnit* units = nullptr;
   ChunkSplit* splits = nullptr;
-  int* first = nullptr;               // [columns + 1] the first unit of each column
+  int* first = nullptr;               // [columns + 1] the first unit of each column; null: each finds its own
+  int* flags = nullptr;               // [columns][Hkv][waves] what a column's waves found; null: no columns
   int* redo = nullptr;                // items to do again, status[3] of them; null: rows of a request see the same keys
   float* part_o = nullptr;            // [slots][Hkv][tile rows][D]
   float* part_ml = nullptr;           // [slots][Hkv][tile rows][2]
   // chunk_bounds
   int tile_rows = 0, key_tile = 0, once = 0, slots = 0, target = 0, min_split = 0;
   int columns = 0;                    // 0: units go by a queue
-  int max_units = 0, max_slots = 0, max_splits = 0, max_redo = 0;
+  int max_units = 0, max_slots = 0, max_splits = 0, max_redo = 0, max_flags = 0;
 };
 // Keys per tile, and waves per SIMD the registers are sized for, of a workgroup of `waves` waves.
 constexpr int chunk_key_tile(int waves, bool f32) { return f32 || waves == 1 ? 32 : 64; }
@@ -154,6 +155,11 @@ inline void mx_bounds(ChunkAttnArgs& a) {
   a.columns = (int)std::max(1LL, std::min<long long>(a.slots / a.Hkv, most));
   a.target = a.columns * a.Hkv;
   plan_bounds(a, waves);
+  a.max_flags = a.columns * a.Hkv * waves;
+  if (a.B <= 64) {   // no plan: a slot for every unit, an entry for every request
+    a.max_slots = a.max_units = a.B + a.columns;
+    a.max_splits = a.B;
+  }
 }
 hipError_t launch_chunk_attn(const ChunkAttnArgs& a, hipStream_t s);
 hipError_t launch_chunk_attn_mx(const ChunkAttnArgs& a, hipStream_t s);

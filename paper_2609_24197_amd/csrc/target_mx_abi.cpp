@@ -94,10 +94,13 @@ static void plan_chunk_attn_mx(Arena& ar, const hspec_chunk_cfg& c, int max_len,
   hspec::mx_bounds(a);
   a.status = ar.take<int>(64);
   a.queue = ar.take<int>(hspec::kChunkClasses * hspec::kChunkQueueStride);
-  if (a.columns) a.first = ar.take<int>((size_t)a.columns + 1);
-  a.units = ar.take<hspec::ChunkUnit>(a.max_units);
+  if (a.columns) a.flags = ar.take<int>(a.max_flags);
+  if (!a.columns || a.B > 64) {
+    if (a.columns) a.first = ar.take<int>((size_t)a.columns + 1);
+    a.units = ar.take<hspec::ChunkUnit>(a.max_units);
+  }
   a.splits = ar.take<hspec::ChunkSplit>(a.max_splits);
-  if (a.max_new > 1) a.redo = ar.take<int>(a.max_redo);   // (one new token: its rows see the same keys)
+  if (!a.columns && a.max_new > 1) a.redo = ar.take<int>(a.max_redo);   // (one new token: its rows see the same keys)
   const size_t rows = (size_t)a.max_slots * c.Hkv * a.tile_rows;
   a.part_o = ar.take<float>(rows * c.D);
   a.part_ml = ar.take<float>(rows * 2);

@@ -27,4 +27,5 @@ def driver(tmp_path_factory):
 def test_plans(driver, mode):
     r = subprocess.run([driver, mode], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, (r.returncode, r.stderr[-2000:])
-    assert int(re.search(r"(\d+) plans in columns", r.stdout).group(1)) >= 3
+    columns, lanes = map(int, re.search(r"(\d+) plans in columns, (\d+) of lanes", r.stdout).groups())
+    assert columns >= 3 and (lanes >= 50 or mode == "longest")
