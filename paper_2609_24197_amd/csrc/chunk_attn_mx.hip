@@ -28,7 +28,7 @@ template <int D>
 hipError_t launch_few_rows(const ChunkAttnArgs& a, hipStream_t s) {
   const MxTile t = mx_tile(a);
   if (t.rw == 1) return t.ct == 1 ? launch_few<Few<D, 1>>(a, s) : launch_few<Few<D, 2>>(a, s);
-  return t.rw == 2 ? launch_few<Share<D, 2, 2>>(a, s) : t.rw == 3 ? launch_few<Share<D, 3, 2>>(a, s) : launch_few<Share<D, 4, 2>>(a, s);
+  return t.rw == 2 ? launch_few<Share<D, 2, 2>>(a, s) : launch_few<Share<D, 4, 1>>(a, s);
 }
 
 }  // namespace

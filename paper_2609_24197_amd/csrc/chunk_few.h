@@ -470,72 +470,83 @@ __device__ __forceinline__ int share_unit(C, const ChunkAttnArgs& a, const Chunk
   auto compute = [&](int base, int end, const bf16* stage) {
     const int hi = min(hi0, end), all_hi = min(all_hi0, end), any_hi = min(any_hi0, end);
     const unsigned span = (unsigned)max(hi - lo, 0);
+    const int key0 = 32 * NKB * kw, mine = base + key0;   // this wave's keys
+    if (!live || mine >= any_hi || mine + 32 * NKB <= any_lo) return;   // (uniform)
+    f32x16 st[NKB];
 #pragma unroll
     for (int kb = 0; kb < NKB; ++kb) {
-      const int key0 = 32 * (kw * NKB + kb), mine = base + key0;
-      if (!live || mine >= any_hi || mine + 32 <= any_lo) continue;   // (uniform)
       bf16x8 kf[NQ];
 #pragma unroll
-      for (int s = 0; s < NQ; ++s) kf[s] = ld8(stage + kv_off<bf16, CPR>(key0 + l32, 16 * s + 8 * hf));
-      f32x16 st = zero16();
+      for (int s = 0; s < NQ; ++s) kf[s] = ld8(stage + kv_off<bf16, CPR>(key0 + 32 * kb + l32, 16 * s + 8 * hf));
+      st[kb] = zero16();
 #pragma unroll
-      for (int s = 0; s < NQ; ++s) st = mma32(kf[s], qf[s], st);
-      // V is on its way from LDS beside the products and the softmax (the scheduler would have each read right before its use)
-      bf16x8 vv[2][NDB];
+      for (int s = 0; s < NQ; ++s) st[kb] = mma32(kf[s], qf[s], st[kb]);
+    }
+    // V is on its way from LDS beside the products and the softmax, 32 keys ahead (the scheduler would have each read right
+    // before its use)
+    bf16x8 vv[2][NDB];
+    auto fetch = [&](int s) {
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
+      for (int db = 0; db < NDB; ++db) vv[s % 2][db] = v_frag<CPR>(stage + TILE, key0 / 16 + s, db, lane);
+    };
+    fetch(0);
+    fetch(1);
+    __builtin_amdgcn_sched_barrier(0);
+    if (!(mine + 32 * NKB <= all_hi && mine >= all_lo)) {
 #pragma unroll
-        for (int db = 0; db < NDB; ++db) vv[s][db] = v_frag<CPR>(stage + TILE, key0 / 16 + s, db, lane);
-      __builtin_amdgcn_sched_barrier(0);
-      if (!(mine + 32 <= all_hi && mine >= all_lo)) {
+      for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          if ((unsigned)(mine + 8 * (i / 4) + 4 * hf + i % 4 - lo) >= span) st[i] = -INFINITY;
-      }
-      float mx = -INFINITY;
+          if ((unsigned)(mine + 32 * kb + 8 * (i / 4) + 4 * hf + i % 4 - lo) >= span) st[kb][i] = -INFINITY;
+    }
+    float mx = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, st[i]);
-      mx = half_max(mx) * a.scale_log2;
-      if (__any(mx > m_run + CHUNK_SLACK)) {   // (a row's own scores alone decide)
-        const float m_new = mx > m_run + CHUNK_SLACK ? mx : m_run;
-        const float alpha = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
-        l_run *= alpha;
+    for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
-        for (int db = 0; db < NDB; ++db) o[db] *= alpha;
-        m_run = m_new;
-      }
-      const float m_use = m_run == -INFINITY ? 0.f : m_run;
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, st[kb][i]);
+    mx = half_max(mx) * a.scale_log2;
+    if (__any(mx > m_run + CHUNK_SLACK)) {   // (a row's own scores alone decide)
+      const float m_new = mx > m_run + CHUNK_SLACK ? mx : m_run;
+      const float alpha = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
+      l_run *= alpha;
+#pragma unroll
+      for (int db = 0; db < NDB; ++db) o[db] *= alpha;
+      m_run = m_new;
+    }
+    const float m_use = m_run == -INFINITY ? 0.f : m_run;
+#pragma unroll
+    for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        st[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[i], a.scale_log2, -m_use));
-        l_run += st[i];
+        st[kb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kb][i], a.scale_log2, -m_use));
+        l_run += st[kb][i];
       }
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {   // (P as bf16: see FewRows)
-        bf16x8 pf;
+    for (int s = 0; s < 2 * NKB; ++s) {   // (P as bf16: see FewRows)
+      bf16x8 pf;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) pf[j] = f2bf(st[8 * s + j]);
+      for (int j = 0; j < 8; ++j) pf[j] = f2bf(st[s / 2][8 * (s & 1) + j]);
 #pragma unroll
-        for (int db = 0; db < NDB; ++db) {
-          bf16x8 vf = vv[s][db];
-          if constexpr (ODD) {   // (see FewRows)
-            s16x8 bits = __builtin_bit_cast(s16x8, vf), up, dn, sees;
+      for (int db = 0; db < NDB; ++db) {
+        bf16x8 vf = vv[s % 2][db];
+        if constexpr (ODD) {   // (see FewRows)
+          s16x8 bits = __builtin_bit_cast(s16x8, vf), up, dn, sees;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const bool fin = (bits[j] & 0x7f80) != 0x7f80, nan = !fin && (bits[j] & 0x7f);
-              const int key = mine + 16 * s + 8 * (j / 4) + 4 * hf + j % 4;
-              up[j] = (short)(!fin && (nan || bits[j] >= 0) ? 0x7f7f : 0);
-              dn[j] = (short)(!fin && (nan || bits[j] < 0) ? 0xff7f : 0);
-              sees[j] = (short)(key >= lo && key < hi ? 0x7f7f : 0);
-              if (!fin) bits[j] = 0;
-            }
-            o[db] += mma32(__builtin_bit_cast(bf16x8, up), __builtin_bit_cast(bf16x8, sees), zero16());
-            o[db] += mma32(__builtin_bit_cast(bf16x8, dn), __builtin_bit_cast(bf16x8, sees), zero16());
-            vf = __builtin_bit_cast(bf16x8, bits);
+          for (int j = 0; j < 8; ++j) {
+            const bool fin = (bits[j] & 0x7f80) != 0x7f80, nan = !fin && (bits[j] & 0x7f);
+            const int key = mine + 16 * s + 8 * (j / 4) + 4 * hf + j % 4;
+            up[j] = (short)(!fin && (nan || bits[j] >= 0) ? 0x7f7f : 0);
+            dn[j] = (short)(!fin && (nan || bits[j] < 0) ? 0xff7f : 0);
+            sees[j] = (short)(key >= lo && key < hi ? 0x7f7f : 0);
+            if (!fin) bits[j] = 0;
           }
-          o[db] = mma32(vf, pf, o[db]);
+          o[db] += mma32(__builtin_bit_cast(bf16x8, up), __builtin_bit_cast(bf16x8, sees), zero16());
+          o[db] += mma32(__builtin_bit_cast(bf16x8, dn), __builtin_bit_cast(bf16x8, sees), zero16());
+          vf = __builtin_bit_cast(bf16x8, bits);
         }
+        o[db] = mma32(vf, pf, o[db]);
       }
+      if (s + 2 < 2 * NKB) fetch(s + 2);
     }
   };
   bf16 *st0 = lds, *st1 = lds + 2 * TILE;

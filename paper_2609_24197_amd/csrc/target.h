@@ -141,7 +141,7 @@ struct MxTile {
 inline MxTile mx_tile(const ChunkAttnArgs& a) {
   const long long R = (long long)a.max_new * (a.Hq / a.Hkv);
   if (a.f32 || R > 128) return MxTile{0, 0, 0};
-  return R <= 16 ? MxTile{1, 1, 1} : R <= 32 ? MxTile{2, 1, 1} : R <= 64 ? MxTile{2, 2, 2} : R <= 96 ? MxTile{2, 3, 2} : MxTile{2, 4, 2};
+  return R <= 16 ? MxTile{1, 1, 1} : R <= 32 ? MxTile{2, 1, 1} : R <= 64 ? MxTile{2, 2, 2} : MxTile{2, 4, 1};
 }
 inline void mx_bounds(ChunkAttnArgs& a) {
   const MxTile t = mx_tile(a);
