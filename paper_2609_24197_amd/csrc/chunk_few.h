@@ -34,15 +34,62 @@ __device__ __forceinline__ s16x4 few_v(const bf16* sV, int key0, int db, int lan
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(sV + few_off<D>(key, db * 16 + 4 * (lane & 3))));
 }
 
-// A wave's rows: what they see, Q, and the softmax's running maximum, sum and output.
-template <int D, int NCT, bool ODD>
+// An fp32 value as the sum of three bf16, by cutting off bits: 8 + 8 + 8 of its 24, so that nothing is lost.  (What is not
+// finite is the first of them.)
+struct Planes {
+  unsigned bits[3];   // bf16 in the upper half
+};
+__device__ __forceinline__ Planes planes(float v) {
+  Planes p;
+  const bool fin = fabsf(v) < INFINITY;
+  p.bits[0] = v == v ? __float_as_uint(v) & 0xffff0000u : 0x7fc00000u;
+  const float r = fin ? v - __uint_as_float(p.bits[0]) : 0.f;
+  p.bits[1] = __float_as_uint(r) & 0xffff0000u;
+  p.bits[2] = __float_as_uint(r - __uint_as_float(p.bits[1]));
+  return p;
+}
+// Of 8 of them, the PL-th bf16 of each (PL = 1: bf16 as it is).
+template <int PL>
+__device__ __forceinline__ void split8(const float* v, bf16x8 (&f)[PL]) {
+  u32x4 w[PL];
+#pragma unroll
+  for (int j = 0; j < 8; j += 2) {
+    const Planes a = planes(v[j]), b = planes(v[j + 1]);
+#pragma unroll
+    for (int i = 0; i < PL; ++i) w[i][j / 2] = __builtin_amdgcn_perm(b.bits[i], a.bits[i], 0x07060302);
+  }
+#pragma unroll
+  for (int i = 0; i < PL; ++i) f[i] = __builtin_bit_cast(bf16x8, w[i]);
+}
+// 8 values from memory as operands of products, or zeros.
+template <class T, int PL>
+__device__ __forceinline__ void operands(const void* p, size_t at, bool in, bf16x8 (&f)[PL]) {
+  if constexpr (sizeof(T) == 2) {
+    f[0] = in ? ld8(static_cast<const bf16*>(p) + at) : zero8();
+  } else {
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = 0.f;
+    if (in) {
+      *reinterpret_cast<f32x4*>(v) = *reinterpret_cast<const f32x4*>(static_cast<const float*>(p) + at);
+      *reinterpret_cast<f32x4*>(v + 4) = *reinterpret_cast<const f32x4*>(static_cast<const float*>(p) + at + 4);
+    }
+    split8<PL>(v, f);
+  }
+}
+
+// A wave's rows: what they see, Q, and the softmax's running maximum, sum and output.  With fp32 rows Q and the weights
+// enter as three bf16 each: the 4-bit values are bf16 exactly, so three products with 32-bit sums lose no more than one in 32
+// bits does, at a fifth of its time.
+template <class T, int D, int NCT, bool ODD>
 struct FewRows {
+  static constexpr int PL = sizeof(T) == 4 ? 3 : 1;
   static constexpr int CH = D / 4, NS = CH / 8, NB = D / 16;   // channels of a lane, products per 16 keys, d blocks
   int lo[NCT], hi[NCT];       // keys that this lane's column of each 16 sees
   int any_lo, any_hi, all_lo, all_hi;   // keys that any and that all rows of the wave see
   size_t at_q[NCT];
   bool real[NCT];
-  bf16x8 qf[NCT][NS];
+  bf16x8 qf[NCT][NS][PL];
   f32x4 o[NCT][NB];
   float m_run[NCT], l_run[NCT];
   int c0, R, lane, c;
@@ -69,7 +116,7 @@ struct FewRows {
       hi[ct] = real[ct] ? sees_to(tok) : 0;
 #pragma unroll
       for (int s = 0; s < NS; ++s)
-        qf[ct][s] = real[ct] ? ld8(static_cast<const bf16*>(a.q) + at_q[ct] + CH * c + 8 * s) : zero8();
+        operands<T>(a.q, at_q[ct] + CH * c + 8 * s, real[ct], qf[ct][s]);
 #pragma unroll
       for (int db = 0; db < NB; ++db) o[ct][db] = f32x4{0.f, 0.f, 0.f, 0.f};
       m_run[ct] = -INFINITY;
@@ -118,15 +165,33 @@ struct FewRows {
     }
   }
 
-  // O += of the 32 keys from base on, whose weights are st[.][t] and st[.][t + 1] and whose V begins at sV.  P enters as
-  // bf16: half a step is 2^-8 of each weight, as large as the output's own rounding; the sum takes the unrounded weights.
+  // st[.][t] += scores of 16 keys, of which kf is the s-th 8 channels a lane.
   template <int NK>
-  __device__ __forceinline__ void values(const f32x4 (&st)[NCT][NK], int t, const bf16* sV, int base, int end) {
-    bf16x8 pf[NCT];
+  __device__ __forceinline__ void scores(f32x4 (&st)[NCT][NK], int t, int s, bf16x8 kf) const {
 #pragma unroll
     for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) pf[ct][j] = f2bf(st[ct][t + j / 4][j % 4]);
+      for (int i = 0; i < PL; ++i) st[ct][t] = mma16(kf, qf[ct][s][i], st[ct][t]);
+  }
+
+  // O += of the 32 keys from base on, whose weights are st[.][t] and st[.][t + 1] and whose V begins at sV.  With bf16
+  // rows P enters as bf16: half a step is 2^-8 of each weight, as large as the output's own rounding; the sum takes the
+  // unrounded weights.
+  template <int NK>
+  __device__ __forceinline__ void values(const f32x4 (&st)[NCT][NK], int t, const bf16* sV, int base, int end) {
+    bf16x8 pf[NCT][PL];
+#pragma unroll
+    for (int ct = 0; ct < NCT; ++ct) {
+      if constexpr (PL == 1) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) pf[ct][0][j] = f2bf(st[ct][t + j / 4][j % 4]);
+      } else {
+        float w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = st[ct][t + j / 4][j % 4];
+        split8<PL>(w, pf[ct]);
+      }
+    }
 #pragma unroll
     for (int db = 0; db < NB; ++db) {
       const s16x4 v0 = few_v<D>(sV, 0, db, lane), v1 = few_v<D>(sV, 16, db, lane);
@@ -158,7 +223,8 @@ struct FewRows {
       }
 #pragma unroll
       for (int ct = 0; ct < NCT; ++ct)
-        o[ct][db] = mma16(vf, pf[ct], o[ct][db]);
+#pragma unroll
+        for (int i = 0; i < PL; ++i) o[ct][db] = mma16(vf, pf[ct][i], o[ct][db]);
     }
   }
 
@@ -177,11 +243,12 @@ struct FewRows {
       if (!real[ct]) continue;
       if (u.slot < 0) {
         const float inv = hi[ct] > lo[ct] ? 1.f / l : 0.f;   // (a row that sees no key is zero)
-        bf16* dst = static_cast<bf16*>(a.o) + at_q[ct] + 4 * c;
+        T* dst = static_cast<T*>(a.o) + at_q[ct] + 4 * c;
 #pragma unroll
         for (int db = 0; db < NB; ++db) {
           const f32x4 v = o[ct][db] * inv;
-          *reinterpret_cast<bf16x4*>(dst + 16 * db) = bf16x4{f2bf(v[0]), f2bf(v[1]), f2bf(v[2]), f2bf(v[3])};
+          if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(dst + 16 * db) = v;
+          else *reinterpret_cast<bf16x4*>(dst + 16 * db) = bf16x4{f2bf(v[0]), f2bf(v[1]), f2bf(v[2]), f2bf(v[3])};
         }
       } else {
         const size_t pr = ((size_t)u.slot * a.Hkv + h) * rows + part + 16 * ct + (lane & 15);
@@ -230,25 +297,31 @@ struct FewPages {
 
 // ---------------------------------------------------------------- a wave by itself
 
-template <int D_, int NCT_>
+// (fp32 rows past 16 are divided over NW such waves, which have more to multiply than to widen.)
+template <class T_, int D_, int NCT_, int NW_>
 struct Few {
-  static constexpr int D = D_, NCT = NCT_;
-  static constexpr int NW = 1, KT = 64, NT = 64, ROWS = 16 * NCT;
-  static constexpr int WPE = NCT == 1 ? 3 : 2;    // waves per SIMD the registers are sized for
-  static constexpr int VK = NCT == 1 ? 32 : KT;   // keys of V in LDS at a time
-  static constexpr int LDS = VK * D;              // elements
+  typedef T_ T;
+  static constexpr int D = D_, NCT = NCT_, NW = NW_;
+  static constexpr int KT = 64, NT = 64 * NW, ROWS = 16 * NCT * NW;
+  static constexpr int WPE = NCT == 1 && sizeof(T) == 2 ? 3 : 2;   // waves per SIMD the registers are sized for
+  static constexpr int VK = NCT == 1 ? 32 : KT;                    // keys of V in LDS at a time
+  static constexpr int LDS = NW * VK * D;                          // elements
 };
 
 template <bool ODD, class C>
-__device__ __forceinline__ int few_unit(C, const ChunkAttnArgs& a, const ChunkUnit& u, int h, bf16* sV) {
+__device__ __forceinline__ int few_unit(C, const ChunkAttnArgs& a, const ChunkUnit& u, int h, bf16* lds) {
+  typedef typename C::T T;
   constexpr int D = C::D, KT = C::KT, NCT = C::NCT, NK = KT / 16, VK = C::VK;
-  typedef FewRows<D, NCT, ODD> Rows;
-  constexpr int CH = Rows::CH, NS = Rows::NS;
+  typedef FewRows<T, D, NCT, ODD> Rows;
+  constexpr int CH = Rows::CH, NS = Rows::NS, PL = Rows::PL;
   typedef typename std::conditional<D == 128, u32x4, uint2>::type Codes;
   const int lane = threadIdx.x & 63, c = lane >> 4, l16 = lane & 15;
+  const int wave = C::NW > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0, c0 = wave * 16 * NCT;
+  if (c0 >= u.n * (a.Hq / a.Hkv)) return 0;
+  bf16* sV = lds + wave * VK * D;
   const int held = a.k_new ? min(u.L, u.k1) : u.k1;
   Rows x;
-  x.init(a, u, h, 0);
+  x.init(a, u, h, c0);
   const int k_min = max(u.k0, x.any_lo);   // the first key that a row sees: those before it are not read
   const int from = k_min / KT * KT;        // (u.k0 is a multiple of 64 too, so that 16 keys lie in one page)
   FewPages pages;
@@ -339,12 +412,7 @@ __device__ __forceinline__ int few_unit(C, const ChunkAttnArgs& a, const ChunkUn
 #pragma unroll
       for (int t = 0; t < NK; ++t)
 #pragma unroll
-        for (int s = 0; s < NS; ++s) {
-          const bf16x8 kf = wide(rk, t, s);
-#pragma unroll
-          for (int ct = 0; ct < NCT; ++ct)
-            st[ct][t] = mma16(kf, x.qf[ct][s], st[ct][t]);
-        }
+        for (int s = 0; s < NS; ++s) x.scores(st, t, s, wide(rk, t, s));
       load(a.k_cache, base + KT, p, rk);
       attend(base, held, value);
       if constexpr (VK < KT) load(a.v_cache, base + KT, p, rv);
@@ -354,25 +422,35 @@ __device__ __forceinline__ int few_unit(C, const ChunkAttnArgs& a, const ChunkUn
   if (a.k_new && u.k1 > u.L) {
     const size_t stride = (size_t)a.Hkv * D, at_new = (size_t)u.row0 * stride + h * D + CH * c;
     for (int base = max(k_min, u.L); base < x.any_hi; base += KT) {
-      auto row = [&](const void* p, int t, int s) -> bf16x8 {
+      auto row = [&](const void* p, int t, int s, bf16x8 (&f)[PL]) {
         const int key = base + 16 * t + l16;
-        return key < u.k1 ? ld8(static_cast<const bf16*>(p) + at_new + (size_t)(key - u.L) * stride + 8 * s) : zero8();
+        operands<T>(p, at_new + (size_t)(key - u.L) * stride + 8 * s, key < u.k1, f);
       };
       clear();
 #pragma unroll
       for (int t = 0; t < NK; ++t)
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
-          const bf16x8 kf = row(a.k_new, t, s);
+          bf16x8 kf[PL];
+          row(a.k_new, t, s, kf);
 #pragma unroll
-          for (int ct = 0; ct < NCT; ++ct) st[ct][t] = mma16(kf, x.qf[ct][s], st[ct][t]);
+          for (int i = 0; i < PL; ++i) x.scores(st, t, s, kf[i]);
         }
-      auto value = [&](int t, int s) { return row(a.v_new, t, s); };
-      if constexpr (VK == KT) put(0, NK, value);
-      attend(base, INT_MAX, value);
+      x.weights(a, st, base, INT_MAX);
+#pragma unroll
+      for (int t = 0; t < NK; t += 2)
+#pragma unroll
+        for (int i = 0; i < PL; ++i) {
+          put(t, t + 2, [&](int t2, int s) {
+            bf16x8 vf[PL];
+            row(a.v_new, t2, s, vf);
+            return vf[i];
+          });
+          x.values(st, t, sV + 16 * t % VK * D, base + 16 * t, INT_MAX);
+        }
     }
   }
-  return found | x.finish(a, u, h, C::ROWS, 0);
+  return found | x.finish(a, u, h, C::ROWS, c0);
 }
 
 // ------------------------------------------------------------- waves share a step
@@ -381,6 +459,7 @@ __device__ __forceinline__ int few_unit(C, const ChunkAttnArgs& a, const ChunkUn
 // chunk_unit's, whose operands' layouts these are).
 template <int D_, int RW_, int KW_>
 struct Share {
+  typedef bf16 T;
   static constexpr int D = D_, RW = RW_, KW = KW_;
   static constexpr int NW = RW * KW, KT = 64, NT = 64 * NW, ROWS = 32 * RW;
   static constexpr int WPE = 2;
@@ -651,8 +730,8 @@ __device__ __forceinline__ int share_unit(C, const ChunkAttnArgs& a, const Chunk
 
 // ----------------------------------------------------------------------------- launch
 
-template <bool ODD, int D, int NCT>
-__device__ __forceinline__ int run_unit(Few<D, NCT> v, const ChunkAttnArgs& a, const ChunkUnit& u, int h, bf16* lds) {
+template <bool ODD, class T, int D, int NCT, int NW>
+__device__ __forceinline__ int run_unit(Few<T, D, NCT, NW> v, const ChunkAttnArgs& a, const ChunkUnit& u, int h, bf16* lds) {
   return few_unit<ODD>(v, a, u, h, lds);
 }
 template <bool ODD, int D, int RW, int KW>
@@ -735,7 +814,7 @@ hipError_t launch_few(const ChunkAttnArgs& a, hipStream_t s) {
     hipLaunchKernelGGL(few_redo_kernel<C>, dim3(std::min(256u, items)), dim3(C::NT), 0, s, a);
     if (hipError_t e = hipGetLastError()) return e;
   }
-  return launch_merge<bf16, C::D>(a, s, C::NW);
+  return launch_merge<typename C::T, C::D>(a, s, C::NW);
 }
 
 }  // namespace

@@ -133,25 +133,27 @@ inline void chunk_bounds(ChunkAttnArgs& a) {
   plan_bounds(a, waves);
 }
 
-// Over the 4-bit cache, bf16 rows up to 128 of a request take the tiles of chunk_few.h: 16 or 32 rows are a wave's, more are
-// divided over the waves of a workgroup.
+// Over the 4-bit cache, up to 128 rows of a request take the tiles of chunk_few.h: bf16 rows up to 32 are a wave's, more
+// are divided over the waves of a workgroup; fp32 rows are 16 a wave.
 struct MxTile {
-  int ct, rw, kw;   // 16-row blocks of a wave, waves that divide the rows and a step's keys; ct = 0: the tiles of chunk_bounds
+  int rows, rw, kw;   // of a wave, waves that divide the rows and a step's keys; rows = 0: the tiles of chunk_bounds
 };
 inline MxTile mx_tile(const ChunkAttnArgs& a) {
   const long long R = (long long)a.max_new * (a.Hq / a.Hkv);
-  if (a.f32 || R > 128) return MxTile{0, 0, 0};
-  return R <= 16 ? MxTile{1, 1, 1} : R <= 32 ? MxTile{2, 1, 1} : R <= 64 ? MxTile{2, 2, 2} : MxTile{2, 4, 1};
+  if (R > 128) return MxTile{0, 0, 0};
+  if (R <= 16) return MxTile{16, 1, 1};
+  if (a.f32) return MxTile{16, R <= 32 ? 2 : R <= 64 ? 4 : 8, 1};
+  return R <= 32 ? MxTile{32, 1, 1} : R <= 64 ? MxTile{32, 2, 2} : MxTile{32, 4, 1};
 }
 inline void mx_bounds(ChunkAttnArgs& a) {
   const MxTile t = mx_tile(a);
-  if (!t.ct) return chunk_bounds(a);
-  a.tile_rows = 16 * t.ct * t.rw;
+  if (!t.rows) return chunk_bounds(a);
+  a.tile_rows = t.rows * t.rw;
   a.key_tile = 64;
   // as many columns as workgroups run at once, and no more than there can be steps
   const long long most = std::min<long long>(a.T, a.B) * ((a.cap + 63LL) / 64 + 1);
   const int waves = t.rw * t.kw;
-  a.slots = std::max((t.ct == 1 ? 12 : 8) / waves, 1) * 256;
+  a.slots = (t.rows == 16 && !a.f32 ? 12 : 8) / waves * 256;
   a.columns = (int)std::max(1LL, std::min<long long>(a.slots / a.Hkv, most));
   a.target = a.columns * a.Hkv;
   plan_bounds(a, waves);
