@@ -38,6 +38,31 @@ def test_many_requests_of_long_caches(new, dense):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new,dense", [(1, None), (5, None), (9, "block"), (17, None), (16, "causal"), (29, None)])
+def test_more_requests_than_a_wave_has_lanes(new, dense, dtype):
+    """Past 64 requests a plan's launch comes first."""
+    n = [new if i % 5 else 0 for i in range(130)]
+    check_attend(batch([(37 * i) % 700 for i in range(130)], n, 8, 2, 128, dtype=dtype, dense=dense, seed=new + 70))
+
+
+@pytest.mark.parametrize("count", [64, 65])
+def test_bad_pages_and_rows_of_many_requests(count):
+    x = batch([40] * count, [3] * count, 4, 1, 64, seed=20)
+    want, ws = attend(x)
+    assert hspec.read_status(ws) == 0
+    y = dict(x, table=x["table"].clone())
+    y["table"][count - 1, 1] = -5
+    got, ws = attend(y)
+    assert hspec.read_status(ws) == hspec.DEV_BAD_PAGE and torch.equal(got[:-5], want[:-5])
+    cu = x["cu"].clone()
+    cu[count // 2] = 1
+    _, ws = attend(dict(x, cu=cu))
+    assert hspec.read_status(ws) & hspec.DEV_BAD_ROWS
+    _, ws = attend(x, ws=ws)                        # (a workspace that held another call's findings)
+    assert hspec.read_status(ws) == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("window", [1, 2, 15, 64, 65, 200])
 @pytest.mark.parametrize("dense", [None, "causal"])
 def test_windows(window, dense, dtype):
@@ -70,9 +95,10 @@ def test_blocks_need_no_page(dense):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("dense", [None, "causal"])
-def test_values_that_a_row_does_not_see(dense, dtype):
+@pytest.mark.parametrize("Hq", [2, 4, 8, 16])
+def test_values_that_a_row_does_not_see(Hq, dense, dtype):
     """A token's NaN or infinite K and V reach the rows that see it, and change nothing, not a bit, in the others."""
-    x = batch([40, 0], [30, 9], 8, 2, 64, dtype=dtype, dense=dense, seed=6)
+    x = batch([40, 0], [30, 9], Hq, 2, 64, dtype=dtype, dense=dense, seed=6)
     want, _ = attend(x)
     for odd in ([math.nan] if dense is None else [math.nan, math.inf, -math.inf]):
         y = dict(x)
