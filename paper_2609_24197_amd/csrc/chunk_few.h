@@ -361,11 +361,11 @@ __device__ __forceinline__ int few_unit(C, const ChunkAttnArgs& a, const ChunkUn
       const auto r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(static_cast<const uint8_t*>(cache) + p.off[t]), 0,
                                                        p.bytes[t], BUFFER_FLAGS);
       if constexpr (D == 128) {
-        w.code[t] = __builtin_bit_cast(Codes, __builtin_amdgcn_raw_buffer_load_b128(r, in ? at_code : BUF_OOB, row0 * (D / 2), 0));
+        w.code[t] = __builtin_bit_cast(Codes, __builtin_amdgcn_raw_buffer_load_b128(r, in ? at_code : BUF_OOB, row0 * (D / 2), 2));
       } else {
-        w.code[t] = __builtin_bit_cast(Codes, __builtin_amdgcn_raw_buffer_load_b64(r, in ? at_code : BUF_OOB, row0 * (D / 2), 0));
+        w.code[t] = __builtin_bit_cast(Codes, __builtin_amdgcn_raw_buffer_load_b64(r, in ? at_code : BUF_OOB, row0 * (D / 2), 2));
       }
-      w.scale[t] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(r, in ? at_scale : BUF_OOB, row0 * (D / MX_BLOCK), 0);
+      w.scale[t] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(r, in ? at_scale : BUF_OOB, row0 * (D / MX_BLOCK), 2);
     }
   };
   auto wide = [](const Raw& w, int t, int s) { return mx_widen(reinterpret_cast<const unsigned*>(&w.code[t])[s], w.scale[t]); };
@@ -528,11 +528,11 @@ __device__ __forceinline__ int share_unit(C, const ChunkAttnArgs& a, const Chunk
       const uint8_t* p = static_cast<const uint8_t*>(i ? a.v_cache : a.k_cache) + at_h + (size_t)max(id, 0) * page_bytes;
       const auto r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, mine && id >= 0 ? head_bytes : 0u, BUFFER_FLAGS);
       if constexpr (D == 128) {
-        w.code[i] = __builtin_bit_cast(Codes, __builtin_amdgcn_raw_buffer_load_b128(r, in ? at_code : BUF_OOB, row0 * (D / 2), 0));
+        w.code[i] = __builtin_bit_cast(Codes, __builtin_amdgcn_raw_buffer_load_b128(r, in ? at_code : BUF_OOB, row0 * (D / 2), 2));
       } else {
-        w.code[i] = __builtin_bit_cast(Codes, __builtin_amdgcn_raw_buffer_load_b64(r, in ? at_code : BUF_OOB, row0 * (D / 2), 0));
+        w.code[i] = __builtin_bit_cast(Codes, __builtin_amdgcn_raw_buffer_load_b64(r, in ? at_code : BUF_OOB, row0 * (D / 2), 2));
       }
-      w.scale[i] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(r, in ? at_scale : BUF_OOB, row0 * (D / MX_BLOCK), 0);
+      w.scale[i] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(r, in ? at_scale : BUF_OOB, row0 * (D / MX_BLOCK), 2);
     }
   };
   auto store = [&](const Raw& w, bf16* st) {

@@ -367,54 +367,58 @@ __device__ __forceinline__ bool chunk_unit(const ChunkAttnArgs& a, const ChunkUn
   if constexpr (!C::MX) {
     stream(u.k0, ntiles);
   } else {
-    // 4-bit tiles: the blocks of 32 channels of tile t + 2 are on their way in registers while tile t + 1's, widened,
-    // go into the other stage and tile t is multiplied.
-    constexpr int BPR = D / MX_BLOCK, TB = KT * BPR, NB = (2 * TB + C::NT - 1) / C::NT;
-    constexpr int LROWS = 64 / BPR;   // rows that 64 blocks in a row cover: one or two groups of one page
-    static_assert(TB % 64 == 0 && (LROWS == 16 || LROWS == 32), "blocks of a wave");
-    MxBlock raw[NB];
-    const size_t head_bytes = mx_head_bytes(a.ps, D);
+    // 4-bit tiles: tile t + 2 is on its way in registers while tile t + 1, widened, goes into the other stage and tile t is
+    // multiplied.  A wave takes 16 keys of K or V at a time, a lane channels [CH c4, CH (c4 + 1)) of one key.  Loads go through
+    // buffers, without branches: behind those the compiler would wait for every load under way.
+    constexpr int CH = D / 4, G16 = KT / 16, NB = 2 * G16 / C::NW;
+    static_assert(2 * G16 % C::NW == 0, "groups of 16 keys");
+    typedef typename std::conditional<D == 128, u32x4, uint2>::type Codes;
+    const int l16 = lane & 15, c4 = lane >> 4;
+    const unsigned head_bytes = (unsigned)mx_head_bytes(a.ps, D), page_bytes = head_bytes * (unsigned)a.Hkv;
+    const size_t at_h = (size_t)h * head_bytes;
+    const unsigned at_code = l16 * (D / 2) + c4 * (CH / 2), at_scale = a.ps * (D / 2) + l16 * (D / MX_BLOCK) + c4 * CH / MX_BLOCK;
+    struct Raw {
+      Codes code[NB];
+      unsigned scale[NB];
+    } raw;
     auto load = [&](int ti) {
+      const int base = u.k0 + ti * KT;
+      if ((base + KT - 1) >> lps >= pg0 + 256) load_ids(base >> lps);
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
-        const int idx0 = i * C::NT + wave * 64;
-        raw[i] = MxBlock{u32x4{0u, 0u, 0u, 0u}, 0u};
-        if (idx0 >= 2 * TB) continue;   // (uniform) more lanes than blocks
-        const int bi = idx0 % TB + lane, row = bi / BPR, c = bi % BPR;
-        const int key = u.k0 + ti * KT + row, key0 = u.k0 + ti * KT + idx0 % TB / BPR;
-        int pid = -1;
-#pragma unroll
-        for (int n = 0; n < LROWS / 16; ++n) {
-          const int kn = key0 + 16 * n;
-          const bool any = kn + 16 > k_min && kn < held;   // (a group with nothing visible has no page)
-          if (any && (kn >> lps) >= pg0 + 256) load_ids(kn >> lps);
-          const int id = any ? page_id(kn >> lps) : -1;
-          if (any && (unsigned)id >= (unsigned)a.num_pages && lane == 0) set_status(a.status, ST_BAD_PAGE);
-          if (n == 0 || lane >= 32) pid = id;
+        const int item = i * C::NW + wave, key0 = base + 16 * (item % G16);
+        const bool any = key0 + 16 > k_min && key0 < held;   // (16 keys with nothing visible have no page)
+        const int id = page_id(key0 >> lps);
+        const bool good = any && (unsigned)id < (unsigned)a.num_pages;
+        if (any && !good && lane == 0) set_status(a.status, ST_BAD_PAGE);
+        const unsigned row0 = (unsigned)key0 & (unsigned)(a.ps - 1);
+        // (a key that no row sees reads as zeros, by an offset past the buffer)
+        const bool in = (unsigned)(key0 + l16 - k_min) < (unsigned)(held - k_min);
+        const uint8_t* p = static_cast<const uint8_t*>(item < G16 ? a.k_cache : a.v_cache) + at_h + (size_t)(good ? id : 0) * page_bytes;
+        const auto r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, good ? head_bytes : 0u, BUFFER_FLAGS);
+        if constexpr (D == 128) {
+          raw.code[i] = __builtin_bit_cast(Codes, __builtin_amdgcn_raw_buffer_load_b128(r, in ? at_code : BUF_OOB, row0 * (D / 2), 0));
+        } else {
+          raw.code[i] = __builtin_bit_cast(Codes, __builtin_amdgcn_raw_buffer_load_b64(r, in ? at_code : BUF_OOB, row0 * (D / 2), 0));
         }
-        if (key >= k_min && key < held && (unsigned)pid < (unsigned)a.num_pages) {
-          const uint8_t* p = static_cast<const uint8_t*>(idx0 < TB ? a.k_cache : a.v_cache) +
-                             ((size_t)pid * a.Hkv + h) * head_bytes;
-          raw[i] = mx_load(p, a.ps, D, key & (a.ps - 1), c);
-        }
+        raw.scale[i] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(r, in ? at_scale : BUF_OOB, row0 * (D / MX_BLOCK), 0);
       }
     };
     auto store = [&](T* sb) {
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
-        const int idx = i * C::NT + tid;
-        if (idx >= 2 * TB) continue;
-        const int bi = idx % TB, row = bi / BPR, d0 = bi % BPR * MX_BLOCK;
-        T* dst = sb + (idx < TB ? 0 : C::TILE);
+        const int item = i * C::NW + wave, row = 16 * (item % G16) + l16;
+        T* dst = sb + (item < G16 ? 0 : C::TILE);
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < CH / 8; ++w) {
+          const unsigned code = reinterpret_cast<const unsigned*>(&raw.code[i])[w];
           if constexpr (F32) {
             f32x4 lo4, hi4;
-            mx_widen(raw[i].code[w], raw[i].scale, lo4, hi4);
-            *reinterpret_cast<f32x4*>(dst + kv_off<T, C::CPR>(row, d0 + 8 * w)) = lo4;
-            *reinterpret_cast<f32x4*>(dst + kv_off<T, C::CPR>(row, d0 + 8 * w + 4)) = hi4;
+            mx_widen(code, raw.scale[i], lo4, hi4);
+            *reinterpret_cast<f32x4*>(dst + kv_off<T, C::CPR>(row, CH * c4 + 8 * w)) = lo4;
+            *reinterpret_cast<f32x4*>(dst + kv_off<T, C::CPR>(row, CH * c4 + 8 * w + 4)) = hi4;
           } else {
-            *reinterpret_cast<bf16x8*>(dst + kv_off<T, C::CPR>(row, d0 + 8 * w)) = mx_widen(raw[i].code[w], raw[i].scale);
+            *reinterpret_cast<bf16x8*>(dst + kv_off<T, C::CPR>(row, CH * c4 + 8 * w)) = mx_widen(code, raw.scale[i]);
           }
         }
       }
@@ -422,13 +426,13 @@ __device__ __forceinline__ bool chunk_unit(const ChunkAttnArgs& a, const ChunkUn
     if (ntiles > 0) {
       load(0);
       store(st0);
-      if (ntiles > 1) load(1);
+      load(1);   // (keys past the last read as zeros)
     }
     auto step = [&](int ti, T* mine, T* other) {
       wait_vm_lgkm0<63>();
       wg_barrier();   // every wave's part of tile ti is in LDS, and every wave has left the other stage
-      if (ti + 1 < ntiles) store(other);
-      if (ti + 2 < ntiles) load(ti + 2);
+      store(other);
+      load(ti + 2);
       compute(u.k0 + ti * KT, held, mine);
       __builtin_amdgcn_s_setprio(0);
     };
