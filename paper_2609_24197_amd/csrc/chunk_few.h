@@ -306,6 +306,7 @@ struct Few {
   static constexpr int WPE = NCT == 1 && sizeof(T) == 2 ? 3 : 2;   // waves per SIMD the registers are sized for
   static constexpr int VK = NCT == 1 ? 32 : KT;                    // keys of V in LDS at a time
   static constexpr int LDS = NW * VK * D;                          // elements
+  static constexpr int AUX = NW == 1 ? 2 : 0;                      // loads past the L2 where no other wave wants the keys
 };
 
 template <bool ODD, class C>
@@ -361,11 +362,11 @@ __device__ __forceinline__ int few_unit(C, const ChunkAttnArgs& a, const ChunkUn
       const auto r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(static_cast<const uint8_t*>(cache) + p.off[t]), 0,
                                                        p.bytes[t], BUFFER_FLAGS);
       if constexpr (D == 128) {
-        w.code[t] = __builtin_bit_cast(Codes, __builtin_amdgcn_raw_buffer_load_b128(r, in ? at_code : BUF_OOB, row0 * (D / 2), 2));
+        w.code[t] = __builtin_bit_cast(Codes, __builtin_amdgcn_raw_buffer_load_b128(r, in ? at_code : BUF_OOB, row0 * (D / 2), C::AUX));
       } else {
-        w.code[t] = __builtin_bit_cast(Codes, __builtin_amdgcn_raw_buffer_load_b64(r, in ? at_code : BUF_OOB, row0 * (D / 2), 2));
+        w.code[t] = __builtin_bit_cast(Codes, __builtin_amdgcn_raw_buffer_load_b64(r, in ? at_code : BUF_OOB, row0 * (D / 2), C::AUX));
       }
-      w.scale[t] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(r, in ? at_scale : BUF_OOB, row0 * (D / MX_BLOCK), 2);
+      w.scale[t] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(r, in ? at_scale : BUF_OOB, row0 * (D / MX_BLOCK), C::AUX);
     }
   };
   auto wide = [](const Raw& w, int t, int s) { return mx_widen(reinterpret_cast<const unsigned*>(&w.code[t])[s], w.scale[t]); };
@@ -466,7 +467,7 @@ struct Share {
   static constexpr int TILE = KT * D, CPR = D / 8;
   static constexpr int MERGE = KW > 1 ? ROWS * (D + 4) * 2 : 0;     // elements that results take on their way between waves
   static constexpr int LDS = 4 * TILE > MERGE ? 4 * TILE : MERGE;   // two stages of K and V
-  static_assert(KW <= 2 && NW >= 4 && NW <= 8, "waves");
+  static_assert(KW <= 2 && NW == 4, "waves");
 };
 
 template <bool ODD, class C>
@@ -502,11 +503,9 @@ __device__ __forceinline__ int share_unit(C, const ChunkAttnArgs& a, const Chunk
   for (int db = 0; db < NDB; ++db) o[db] = zero16();
   float m_run = -INFINITY, l_run = 0.f;
 
-  // A wave takes 16 keys of K, and of V, a step (of one of them with more than four waves), a lane channels
-  // [CH c4, CH (c4 + 1)) of one key.  Loads go through buffers, without branches: behind those the compiler would wait for every load
-  // under way.
-  const int l16 = lane & 15, c4 = lane >> 4;
-  const int k16[2] = {16 * wave, 16 * (wave - (C::NW - 4))};   // outside [0, 64): none
+  // A wave takes 16 keys of K and of V a step, a lane channels [CH c4, CH (c4 + 1)) of one key.  Loads go through buffers,
+  // without branches: behind those the compiler would wait for every load under way.
+  const int l16 = lane & 15, c4 = lane >> 4, k16 = 16 * wave;
   struct Raw {
     Codes code[2];   // K, V
     unsigned scale[2];
@@ -516,17 +515,16 @@ __device__ __forceinline__ int share_unit(C, const ChunkAttnArgs& a, const Chunk
   const unsigned at_code = l16 * (D / 2) + c4 * (CH / 2), at_scale = a.ps * (D / 2) + l16 * (D / MX_BLOCK) + c4 * CH / MX_BLOCK;
   auto load = [&](int base, Raw& w) {
     pages.step(base);
+    const int key0 = base + k16, id = pages.page(key0);
+    if (id < 0 && key0 < held && key0 + 16 > k_min) found = UNIT_BAD_PAGE;
+    const unsigned row0 = (unsigned)key0 & (unsigned)(a.ps - 1);
+    const size_t off = at_h + (size_t)max(id, 0) * page_bytes;
+    // (a key that no row sees reads as zeros, by an offset past the buffer)
+    const bool in = (unsigned)(key0 + l16 - k_min) < (unsigned)(held - k_min);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const int key0 = base + (k16[i] & (KT - 1));
-      const bool mine = C::NW == 4 || (unsigned)k16[i] < (unsigned)KT;
-      const int id = pages.page(key0);
-      if (mine && id < 0 && key0 < held && key0 + 16 > k_min) found = UNIT_BAD_PAGE;
-      const unsigned row0 = (unsigned)key0 & (unsigned)(a.ps - 1);
-      // (a key that no row sees reads as zeros, by an offset past the buffer)
-      const bool in = (unsigned)(key0 + l16 - k_min) < (unsigned)(held - k_min);
-      const uint8_t* p = static_cast<const uint8_t*>(i ? a.v_cache : a.k_cache) + at_h + (size_t)max(id, 0) * page_bytes;
-      const auto r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, mine && id >= 0 ? head_bytes : 0u, BUFFER_FLAGS);
+      const uint8_t* p = static_cast<const uint8_t*>(i ? a.v_cache : a.k_cache) + off;
+      const auto r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, id >= 0 ? head_bytes : 0u, BUFFER_FLAGS);
       if constexpr (D == 128) {
         w.code[i] = __builtin_bit_cast(Codes, __builtin_amdgcn_raw_buffer_load_b128(r, in ? at_code : BUF_OOB, row0 * (D / 2), 2));
       } else {
@@ -537,13 +535,11 @@ __device__ __forceinline__ int share_unit(C, const ChunkAttnArgs& a, const Chunk
   };
   auto store = [&](const Raw& w, bf16* st) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      if (C::NW != 4 && (unsigned)k16[i] >= (unsigned)KT) continue;   // (uniform)
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int s = 0; s < NS; ++s)
-        *reinterpret_cast<bf16x8*>(st + i * TILE + kv_off<bf16, CPR>(k16[i] + l16, CH * c4 + 8 * s)) =
+        *reinterpret_cast<bf16x8*>(st + i * TILE + kv_off<bf16, CPR>(k16 + l16, CH * c4 + 8 * s)) =
             mx_widen(reinterpret_cast<const unsigned*>(&w.code[i])[s], w.scale[i]);
-    }
   };
   // keys [base, base + KT) below end of a stage
   auto compute = [&](int base, int end, const bf16* stage) {
