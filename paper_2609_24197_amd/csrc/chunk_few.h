@@ -6,6 +6,10 @@
 // c = l / 16, of key l % 16 of every 16 (the channels are summed over, so any order of them serves, if Q has the same); V^T
 // is read transposed from LDS in the order in which S^T leaves a lane its keys.
 //
+// Bound by HBM where a request has a token (64 of them, 512..8192 cached, 32 and 8 heads of 128: 63 us, 5.1 TB/s), past 32 rows
+// by a step's chain of LDS, products and softmax, with two waves a SIMD (block of 16: 138 us, 17 tokens: 165; the matrix
+// units are busy a quarter of the time).
+//
 // Up to 32 rows (Few) a wave walks its keys by itself: K is the product's operand as it was loaded, widened in
 // registers, V goes through a piece of LDS of the wave's own, and there is no barrier in a unit.  Past that (Share)
 // the waves of a workgroup share what they widen: RW of them divide the rows, KW the keys of a step, and the KW results

@@ -162,7 +162,8 @@ static hspec_status check_adjust(const hspec_adjust_cfg* c) {
       c->masks < 0)
     return fail(HSPEC_ERR_SHAPE, "a dimension of the adjustment is negative, or B, rows or vocab is 0");
   if (c->vocab > (1 << 19) || c->draft_vocab > (1 << 19) || c->B > 32767 || c->k > 4096 ||
-      (long long)c->B * (c->k + 1) > (1 << 22) || c->rows > (1 << 22))
+      (long long)c->B * (c->k + 1) > (1 << 22) || c->rows > (1 << 22) || c->max_hist > (1 << 24) || c->n_bias > (1 << 20) ||
+      c->masks > (1 << 22))
     return fail(HSPEC_ERR_UNSUPPORTED, "adjustment too large");
   return HSPEC_OK;
 }

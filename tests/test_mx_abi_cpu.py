@@ -126,7 +126,8 @@ def _adjust(c=None, ws=WS, n=256, **kw):
     (dict(max_hist=-1), SHAPE), (dict(n_bias=-1), SHAPE), (dict(masks=-1), SHAPE), (dict(dtype=2), DTYPE),
     (dict(out_dtype=-1), DTYPE), (dict(vocab=1 << 20), UNSUPPORTED), (dict(draft_vocab=1 << 20), UNSUPPORTED),
     (dict(B=40000), UNSUPPORTED), (dict(k=5000), UNSUPPORTED), (dict(B=32767, k=4096), UNSUPPORTED),
-    (dict(rows=1 << 23), UNSUPPORTED)])
+    (dict(rows=1 << 23), UNSUPPORTED), (dict(max_hist=(1 << 24) + 1), UNSUPPORTED), (dict(n_bias=(1 << 20) + 1), UNSUPPORTED),
+    (dict(masks=(1 << 22) + 1), UNSUPPORTED)])
 def test_adjust_configs_refused(kw, want):
     assert _adjust(**kw) == want
     assert _lib().hspec_adjust_logits_workspace(C.byref(_adjust_cfg(**kw))) == 0
