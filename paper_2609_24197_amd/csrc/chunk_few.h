@@ -356,12 +356,14 @@ __device__ __forceinline__ int few_unit(C, const ChunkAttnArgs& a, const ChunkUn
     Codes code[NK];
     unsigned scale[NK];
   };
-  const unsigned at_code = l16 * (D / 2) + c * (CH / 2), at_scale = a.ps * (D / 2) + l16 * (D / MX_BLOCK) + c * CH / MX_BLOCK;
-  auto load = [&](const void* cache, int base, const Place& p, Raw& w) {
+  // the key of 16 whose V this lane takes (a wave's 16 rows wait for HBM, not for LDS: with its own key 74 us, 76 with this)
+  const int v16 = NCT == 1 && sizeof(T) == 2 ? l16 : D == 128 ? spread16<0, 1, 3, 2>(l16) : spread16<1, 2, 3, 0>(l16);
+  auto load = [&](const void* cache, int key16, int base, const Place& p, Raw& w) {
+    const unsigned at_code = key16 * (D / 2) + c * (CH / 2), at_scale = a.ps * (D / 2) + key16 * (D / MX_BLOCK) + c * CH / MX_BLOCK;
 #pragma unroll
     for (int t = 0; t < NK; ++t) {
       // (a key that no row sees reads as zeros, by an offset past the buffer)
-      const bool in = (unsigned)(base + 16 * t + l16 - k_min) < (unsigned)(held - k_min);
+      const bool in = (unsigned)(base + 16 * t + key16 - k_min) < (unsigned)(held - k_min);
       const unsigned row0 = (unsigned)(base + 16 * t) & (unsigned)(a.ps - 1);
       const auto r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(static_cast<const uint8_t*>(cache) + p.off[t]), 0,
                                                        p.bytes[t], BUFFER_FLAGS);
@@ -382,13 +384,13 @@ __device__ __forceinline__ int few_unit(C, const ChunkAttnArgs& a, const ChunkUn
 #pragma unroll
       for (int t = 0; t < NK; ++t) st[ct][t] = f32x4{0.f, 0.f, 0.f, 0.f};
   };
-  // Groups [t0, t1) of V into LDS; value(t, s): channels 8 s .. of this lane's of its key of the t-th 16.
+  // Groups [t0, t1) of V into LDS; value(t, s): channels 8 s .. of this lane's of its key (v16) of the t-th 16.
   auto put = [&](int t0, int t1, auto value) {
 #pragma unroll
     for (int t = t0; t < t1; ++t)
 #pragma unroll
       for (int s = 0; s < NS; ++s)
-        *reinterpret_cast<bf16x8*>(sV + few_off<D>(16 * t % VK + l16, CH * c + 8 * s)) = value(t, s);
+        *reinterpret_cast<bf16x8*>(sV + few_off<D>(16 * t % VK + v16, CH * c + 8 * s)) = value(t, s);
   };
   // (VK < KT: V goes into LDS here, 32 keys at a time)
   auto attend = [&](int base, int end, auto value) {
@@ -404,31 +406,31 @@ __device__ __forceinline__ int few_unit(C, const ChunkAttnArgs& a, const ChunkUn
   if (from < held) {
     Raw rk, rv;
     Place p = place(from);
-    load(a.k_cache, from, p, rk);
-    load(a.v_cache, from, p, rv);
+    load(a.k_cache, l16, from, p, rk);
+    load(a.v_cache, v16, from, p, rv);
     for (int base = from; base < held; base += KT) {
       auto value = [&](int t, int s) { return wide(rv, t, s); };
       p = place(base + KT);   // (keys past the last read as zeros; a branch around a load would have the next one wait for all)
       if constexpr (VK == KT) {
         put(0, NK, value);
-        load(a.v_cache, base + KT, p, rv);
+        load(a.v_cache, v16, base + KT, p, rv);
       }
       clear();
 #pragma unroll
       for (int t = 0; t < NK; ++t)
 #pragma unroll
         for (int s = 0; s < NS; ++s) x.scores(st, t, s, wide(rk, t, s));
-      load(a.k_cache, base + KT, p, rk);
+      load(a.k_cache, l16, base + KT, p, rk);
       attend(base, held, value);
-      if constexpr (VK < KT) load(a.v_cache, base + KT, p, rv);
+      if constexpr (VK < KT) load(a.v_cache, v16, base + KT, p, rv);
     }
   }
   // the new tokens' keys beside the cache, as they are
   if (a.k_new && u.k1 > u.L) {
     const size_t stride = (size_t)a.Hkv * D, at_new = (size_t)u.row0 * stride + h * D + CH * c;
     for (int base = max(k_min, u.L); base < x.any_hi; base += KT) {
-      auto row = [&](const void* p, int t, int s, bf16x8 (&f)[PL]) {
-        const int key = base + 16 * t + l16;
+      auto row = [&](const void* p, int key16, int t, int s, bf16x8 (&f)[PL]) {
+        const int key = base + 16 * t + key16;
         operands<T>(p, at_new + (size_t)(key - u.L) * stride + 8 * s, key < u.k1, f);
       };
       clear();
@@ -437,7 +439,7 @@ __device__ __forceinline__ int few_unit(C, const ChunkAttnArgs& a, const ChunkUn
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
           bf16x8 kf[PL];
-          row(a.k_new, t, s, kf);
+          row(a.k_new, l16, t, s, kf);
 #pragma unroll
           for (int i = 0; i < PL; ++i) x.scores(st, t, s, kf[i]);
         }
@@ -448,7 +450,7 @@ __device__ __forceinline__ int few_unit(C, const ChunkAttnArgs& a, const ChunkUn
         for (int i = 0; i < PL; ++i) {
           put(t, t + 2, [&](int t2, int s) {
             bf16x8 vf[PL];
-            row(a.v_new, t2, s, vf);
+            row(a.v_new, v16, t2, s, vf);
             return vf[i];
           });
           x.values(st, t, sV + 16 * t % VK * D, base + 16 * t, INT_MAX);
@@ -509,7 +511,7 @@ __device__ __forceinline__ int share_unit(C, const ChunkAttnArgs& a, const Chunk
 
   // A wave takes 16 keys of K and of V a step, a lane channels [CH c4, CH (c4 + 1)) of one key.  Loads go through buffers,
   // without branches: behind those the compiler would wait for every load under way.
-  const int l16 = lane & 15, c4 = lane >> 4, k16 = 16 * wave;
+  const int l16 = kv_lane<CPR>(lane & 15), c4 = lane >> 4, k16 = 16 * wave;
   struct Raw {
     Codes code[2];   // K, V
     unsigned scale[2];

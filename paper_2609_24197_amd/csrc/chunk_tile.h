@@ -66,6 +66,14 @@ __device__ __forceinline__ int kv_off(int row, int d) {
   return (row * CPR + ((d / EPC) ^ f)) * EPC + d % EPC;
 }
 
+// The key of a lane of 16 that writes rows of kv_off's.
+template <int CPR>
+__device__ __forceinline__ int kv_lane(int l) {
+  if constexpr (CPR == 16) return spread16<0, 2, 3, 1>(l);
+  else if constexpr (CPR == 8) return spread16<1, 2, 3, 0>(l);
+  else return l;
+}
+
 // max over the two lanes l, l ^ 32
 __device__ __forceinline__ float half_max(float v) {
   auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -373,7 +381,7 @@ __device__ __forceinline__ bool chunk_unit(const ChunkAttnArgs& a, const ChunkUn
     constexpr int CH = D / 4, G16 = KT / 16, NB = 2 * G16 / C::NW;
     static_assert(2 * G16 % C::NW == 0, "groups of 16 keys");
     typedef typename std::conditional<D == 128, u32x4, uint2>::type Codes;
-    const int l16 = lane & 15, c4 = lane >> 4;
+    const int l16 = kv_lane<C::CPR>(lane & 15), c4 = lane >> 4;
     const unsigned head_bytes = (unsigned)mx_head_bytes(a.ps, D), page_bytes = head_bytes * (unsigned)a.Hkv;
     const size_t at_h = (size_t)h * head_bytes;
     const unsigned at_code = l16 * (D / 2) + c4 * (CH / 2), at_scale = a.ps * (D / 2) + l16 * (D / MX_BLOCK) + c4 * CH / MX_BLOCK;
