@@ -7,8 +7,8 @@
 // is read transposed from LDS in the order in which S^T leaves a lane its keys.
 //
 // Bound by HBM where a request has a token (64 of them, 512..8192 cached, 32 and 8 heads of 128: 63 us, 5.1 TB/s), past 32 rows
-// by a step's chain of LDS, products and softmax, with two waves a SIMD (block of 16: 138 us, 17 tokens: 165; the matrix
-// units are busy a quarter of the time).
+// by a step's chain of LDS, products and softmax, with two waves a SIMD (the whole call, a block of 16: 137 to 147 us by the card,
+// 17 tokens: 172 to 176; the matrix units are busy a quarter of the time).
 //
 // Up to 32 rows (Few) a wave walks its keys by itself: K is the product's operand as it was loaded, widened in
 // registers, V goes through a piece of LDS of the wave's own, and there is no barrier in a unit.  Past that (Share)
@@ -356,23 +356,27 @@ __device__ __forceinline__ int few_unit(C, const ChunkAttnArgs& a, const ChunkUn
     Codes code[NK];
     unsigned scale[NK];
   };
-  // the key of 16 whose V this lane takes (a wave's 16 rows wait for HBM, not for LDS: with its own key 74 us, 76 with this)
-  const int v16 = NCT == 1 && sizeof(T) == 2 ? l16 : D == 128 ? spread16<0, 1, 3, 2>(l16) : spread16<1, 2, 3, 0>(l16);
-  auto load = [&](const void* cache, int key16, int base, const Place& p, Raw& w) {
-    const unsigned at_code = key16 * (D / 2) + c * (CH / 2), at_scale = a.ps * (D / 2) + key16 * (D / MX_BLOCK) + c * CH / MX_BLOCK;
+  // the key of 16 whose V this lane takes (16 bf16 rows wait for HBM, not for LDS, and have no register to spare: 74 us for 64
+  // requests of a token with the lane's own key, 76 with this)
+  constexpr bool OWN = NCT == 1 && sizeof(T) == 2;
+  const int v16 = OWN ? l16 : D == 128 ? spread16<0, 1, 3, 2>(l16) : spread16<1, 2, 3, 0>(l16);
+  const unsigned at_code = l16 * (D / 2) + c * (CH / 2), at_scale = a.ps * (D / 2) + l16 * (D / MX_BLOCK) + c * CH / MX_BLOCK;
+  const unsigned at_code_v = v16 * (D / 2) + c * (CH / 2), at_scale_v = a.ps * (D / 2) + v16 * (D / MX_BLOCK) + c * CH / MX_BLOCK;
+  auto load = [&](auto v, const void* cache, int base, const Place& p, Raw& w) {
+    constexpr bool V = decltype(v)::value && !OWN;
 #pragma unroll
     for (int t = 0; t < NK; ++t) {
       // (a key that no row sees reads as zeros, by an offset past the buffer)
-      const bool in = (unsigned)(base + 16 * t + key16 - k_min) < (unsigned)(held - k_min);
+      const bool in = (unsigned)(base + 16 * t + (V ? v16 : l16) - k_min) < (unsigned)(held - k_min);
       const unsigned row0 = (unsigned)(base + 16 * t) & (unsigned)(a.ps - 1);
       const auto r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(static_cast<const uint8_t*>(cache) + p.off[t]), 0,
                                                        p.bytes[t], BUFFER_FLAGS);
       if constexpr (D == 128) {
-        w.code[t] = __builtin_bit_cast(Codes, __builtin_amdgcn_raw_buffer_load_b128(r, in ? at_code : BUF_OOB, row0 * (D / 2), C::AUX));
+        w.code[t] = __builtin_bit_cast(Codes, __builtin_amdgcn_raw_buffer_load_b128(r, in ? (V ? at_code_v : at_code) : BUF_OOB, row0 * (D / 2), C::AUX));
       } else {
-        w.code[t] = __builtin_bit_cast(Codes, __builtin_amdgcn_raw_buffer_load_b64(r, in ? at_code : BUF_OOB, row0 * (D / 2), C::AUX));
+        w.code[t] = __builtin_bit_cast(Codes, __builtin_amdgcn_raw_buffer_load_b64(r, in ? (V ? at_code_v : at_code) : BUF_OOB, row0 * (D / 2), C::AUX));
       }
-      w.scale[t] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(r, in ? at_scale : BUF_OOB, row0 * (D / MX_BLOCK), C::AUX);
+      w.scale[t] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(r, in ? (V ? at_scale_v : at_scale) : BUF_OOB, row0 * (D / MX_BLOCK), C::AUX);
     }
   };
   auto wide = [](const Raw& w, int t, int s) { return mx_widen(reinterpret_cast<const unsigned*>(&w.code[t])[s], w.scale[t]); };
@@ -390,7 +394,7 @@ __device__ __forceinline__ int few_unit(C, const ChunkAttnArgs& a, const ChunkUn
     for (int t = t0; t < t1; ++t)
 #pragma unroll
       for (int s = 0; s < NS; ++s)
-        *reinterpret_cast<bf16x8*>(sV + few_off<D>(16 * t % VK + v16, CH * c + 8 * s)) = value(t, s);
+        *reinterpret_cast<bf16x8*>(sV + few_off<D>(16 * t % VK + (OWN ? l16 : v16), CH * c + 8 * s)) = value(t, s);
   };
   // (VK < KT: V goes into LDS here, 32 keys at a time)
   auto attend = [&](int base, int end, auto value) {
@@ -406,31 +410,31 @@ __device__ __forceinline__ int few_unit(C, const ChunkAttnArgs& a, const ChunkUn
   if (from < held) {
     Raw rk, rv;
     Place p = place(from);
-    load(a.k_cache, l16, from, p, rk);
-    load(a.v_cache, v16, from, p, rv);
+    load(std::false_type{}, a.k_cache, from, p, rk);
+    load(std::true_type{}, a.v_cache, from, p, rv);
     for (int base = from; base < held; base += KT) {
       auto value = [&](int t, int s) { return wide(rv, t, s); };
       p = place(base + KT);   // (keys past the last read as zeros; a branch around a load would have the next one wait for all)
       if constexpr (VK == KT) {
         put(0, NK, value);
-        load(a.v_cache, v16, base + KT, p, rv);
+        load(std::true_type{}, a.v_cache, base + KT, p, rv);
       }
       clear();
 #pragma unroll
       for (int t = 0; t < NK; ++t)
 #pragma unroll
         for (int s = 0; s < NS; ++s) x.scores(st, t, s, wide(rk, t, s));
-      load(a.k_cache, l16, base + KT, p, rk);
+      load(std::false_type{}, a.k_cache, base + KT, p, rk);
       attend(base, held, value);
-      if constexpr (VK < KT) load(a.v_cache, v16, base + KT, p, rv);
+      if constexpr (VK < KT) load(std::true_type{}, a.v_cache, base + KT, p, rv);
     }
   }
   // the new tokens' keys beside the cache, as they are
   if (a.k_new && u.k1 > u.L) {
     const size_t stride = (size_t)a.Hkv * D, at_new = (size_t)u.row0 * stride + h * D + CH * c;
     for (int base = max(k_min, u.L); base < x.any_hi; base += KT) {
-      auto row = [&](const void* p, int key16, int t, int s, bf16x8 (&f)[PL]) {
-        const int key = base + 16 * t + key16;
+      auto row = [&](auto v, const void* p, int t, int s, bf16x8 (&f)[PL]) {
+        const int key = base + 16 * t + (decltype(v)::value && !OWN ? v16 : l16);
         operands<T>(p, at_new + (size_t)(key - u.L) * stride + 8 * s, key < u.k1, f);
       };
       clear();
@@ -439,7 +443,7 @@ __device__ __forceinline__ int few_unit(C, const ChunkAttnArgs& a, const ChunkUn
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
           bf16x8 kf[PL];
-          row(a.k_new, l16, t, s, kf);
+          row(std::false_type{}, a.k_new, t, s, kf);
 #pragma unroll
           for (int i = 0; i < PL; ++i) x.scores(st, t, s, kf[i]);
         }
@@ -450,7 +454,7 @@ __device__ __forceinline__ int few_unit(C, const ChunkAttnArgs& a, const ChunkUn
         for (int i = 0; i < PL; ++i) {
           put(t, t + 2, [&](int t2, int s) {
             bf16x8 vf[PL];
-            row(a.v_new, v16, t2, s, vf);
+            row(std::true_type{}, a.v_new, t2, s, vf);
             return vf[i];
           });
           x.values(st, t, sV + 16 * t % VK * D, base + 16 * t, INT_MAX);

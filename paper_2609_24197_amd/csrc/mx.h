@@ -25,8 +25,8 @@ __device__ __forceinline__ MxBlock mx_load(const uint8_t* p, int ps, int D, int 
 }
 
 // The key, of 16, that lane l of 16 takes into LDS: bits of l at places A, B, C, E.  A 16-byte write is done 8 lanes at a time
-// over 128 bytes, so the keys of 8 lanes side by side differ in the bits that choose the place within those (a third of the
-// LDS cycles are conflicts with keys in order).
+// over 128 bytes, so the keys of 8 lanes side by side differ in the bits that choose the place within those (with
+// keys in order a quarter to a third of the LDS cycles are conflicts, and prompts and 17 tokens take 2 % more on the same card).
 template <int A, int B, int C, int E>
 __device__ __forceinline__ int spread16(int l) {
   return (l & 1) << A | (l >> 1 & 1) << B | (l >> 2 & 1) << C | (l >> 3 & 1) << E;
