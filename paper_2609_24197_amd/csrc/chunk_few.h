@@ -338,7 +338,8 @@ __device__ __forceinline__ int few_unit(C, const ChunkAttnArgs& a, const ChunkUn
     size_t off[NK];       // of the head's part of the page
     unsigned bytes[NK];   // 0: no such page
   };
-  const unsigned head_bytes = (unsigned)mx_head_bytes(a.ps, D), page_bytes = head_bytes * (unsigned)a.Hkv;
+  const unsigned head_bytes = (unsigned)mx_head_bytes(a.ps, D);
+  const size_t page_bytes = mx_page_bytes(a.ps, D, a.Hkv);
   const size_t at_h = (size_t)h * head_bytes;
   auto place = [&](int base) {
     Place p;
@@ -520,7 +521,8 @@ __device__ __forceinline__ int share_unit(C, const ChunkAttnArgs& a, const Chunk
     Codes code[2];   // K, V
     unsigned scale[2];
   };
-  const unsigned head_bytes = (unsigned)mx_head_bytes(a.ps, D), page_bytes = head_bytes * (unsigned)a.Hkv;
+  const unsigned head_bytes = (unsigned)mx_head_bytes(a.ps, D);
+  const size_t page_bytes = mx_page_bytes(a.ps, D, a.Hkv);
   const size_t at_h = (size_t)h * head_bytes;
   const unsigned at_code = l16 * (D / 2) + c4 * (CH / 2), at_scale = a.ps * (D / 2) + l16 * (D / MX_BLOCK) + c4 * CH / MX_BLOCK;
   auto load = [&](int base, Raw& w) {

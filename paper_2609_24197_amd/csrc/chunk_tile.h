@@ -382,7 +382,8 @@ __device__ __forceinline__ bool chunk_unit(const ChunkAttnArgs& a, const ChunkUn
     static_assert(2 * G16 % C::NW == 0, "groups of 16 keys");
     typedef typename std::conditional<D == 128, u32x4, uint2>::type Codes;
     const int l16 = kv_lane<C::CPR>(lane & 15), c4 = lane >> 4;
-    const unsigned head_bytes = (unsigned)mx_head_bytes(a.ps, D), page_bytes = head_bytes * (unsigned)a.Hkv;
+    const unsigned head_bytes = (unsigned)mx_head_bytes(a.ps, D);
+    const size_t page_bytes = mx_page_bytes(a.ps, D, a.Hkv);
     const size_t at_h = (size_t)h * head_bytes;
     const unsigned at_code = l16 * (D / 2) + c4 * (CH / 2), at_scale = a.ps * (D / 2) + l16 * (D / MX_BLOCK) + c4 * CH / MX_BLOCK;
     struct Raw {

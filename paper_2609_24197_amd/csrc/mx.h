@@ -1,16 +1,11 @@
 // The 4-bit cache: K and V as 4-bit floats (sign, 0 0.5 1 1.5 2 3 4 6) in blocks of 32 channels that share a power of
-// two.  For each page and KV head: page_size rows of D / 2 bytes (channel 2i in the low half of byte i), then page_size
-// rows of D / 32 scale bytes s, 2^(s - 127), 255 for a block that is NaN.  A head's part of a page is one run of memory,
-// so that a unit of attention, which takes one head, reads whole lines.
+// two (mx_layout.h).
 #pragma once
 #include "common.h"
+#include "mx_layout.h"
 
 namespace hspec {
 namespace {
-
-constexpr int MX_BLOCK = 32;
-
-__host__ __device__ inline size_t mx_head_bytes(int ps, int D) { return (size_t)ps * (D / 2 + D / MX_BLOCK); }
 
 struct MxBlock {
   u32x4 code;        // 8 channels a word
