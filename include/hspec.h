@@ -533,7 +533,8 @@ size_t hspec_verify_workspace(const hspec_verify_cfg* cfg);
  * page_size rows of D/2 bytes (channel 2i in the low half of byte i, code = index of the magnitude + 8
  * if negative) and then page_size rows of D/32 scale bytes s: 2^(s - 127), 255 for a block of NaN.
  * Pages, page tables, the batch's arrays, their checks and the errors are those of the target's side
- * above; cfg.dtype is the type of q, o and the dense rows.
+ * above; cfg.dtype is the type of q, o and the dense rows.  A head's part of a page is below 2^31 bytes
+ * (page_size at most 2^24 with D = 128, 2^25 with 64), else HSPEC_ERR_UNSUPPORTED.
  */
 size_t hspec_mx_cache_bytes(const hspec_chunk_cfg* cfg);
 

@@ -1,8 +1,17 @@
 // C ABI of the 4-bit cache (append, read, attention) and of the logits' adjustment: argument checks, workspace layout
 // and launches.  Host code only.
+#include "mx_layout.h"
 #include "target_check.h"
 
 namespace {
+
+// Kernels address a head's part of a page with 31 bits, and what they leave out with an offset past its end (BUF_OOB).
+hspec_status check_mx(const hspec_chunk_cfg* c) {
+  if (hspec_status s = check_chunk(c)) return s;
+  if (hspec::mx_head_bytes(c->page_size, c->D) >= 1ull << 31)
+    return fail(HSPEC_ERR_UNSUPPORTED, "a head's part of a page must be below 2^31 bytes (page_size=%d)", c->page_size);
+  return HSPEC_OK;
+}
 
 Span mx_span(const hspec_chunk_cfg& c, const void* p) {
   return span(p, {(size_t)c.num_pages, (size_t)c.page_size, (size_t)c.Hkv, (size_t)c.D / 32 * 17});
@@ -27,7 +36,7 @@ hspec::ChunkAppendArgs batch_args(const hspec_chunk_cfg& c, const int32_t* cu, c
 }  // namespace
 
 HSPEC_API size_t hspec_mx_cache_bytes(const hspec_chunk_cfg* cfg) {
-  return !cfg || check_chunk(cfg) ? 0 : mx_span(*cfg, nullptr).n;
+  return !cfg || check_mx(cfg) ? 0 : mx_span(*cfg, nullptr).n;
 }
 
 // ------------------------------------------------------------------------------ append
@@ -39,7 +48,7 @@ HSPEC_API hspec_status hspec_chunk_append_mx(const hspec_chunk_cfg* cfg, hspec_d
                                              const int32_t* ctx_lens, void* q, void* k_cache, void* v_cache,
                                              const int32_t* page_table, void* workspace, size_t ws_bytes, void* stream) {
   clear_err();
-  if (hspec_status s = check_chunk(cfg)) return s;
+  if (hspec_status s = check_mx(cfg)) return s;
   if (!dtype_ok(qkv_dtype)) return fail(HSPEC_ERR_DTYPE, "unknown qkv dtype %d", (int)qkv_dtype);
   if (!qkv || !cu_new || !ctx_lens || !q || !k_cache || !v_cache || !page_table)
     return fail(HSPEC_ERR_NULL, "an input or output pointer is NULL");
@@ -68,7 +77,7 @@ HSPEC_API hspec_status hspec_chunk_read_mx(const hspec_chunk_cfg* cfg, const int
                                            const void* k_cache, const void* v_cache, const int32_t* page_table, void* k,
                                            void* v, void* workspace, size_t ws_bytes, void* stream) {
   clear_err();
-  if (hspec_status s = check_chunk(cfg)) return s;
+  if (hspec_status s = check_mx(cfg)) return s;
   if (!cu_new || !ctx_lens || !k_cache || !v_cache || !page_table || !k || !v)
     return fail(HSPEC_ERR_NULL, "an input or output pointer is NULL");
   if (hspec_status s = check_aligned({k_cache, v_cache, k, v})) return s;
@@ -107,7 +116,7 @@ static void plan_chunk_attn_mx(Arena& ar, const hspec_chunk_cfg& c, int max_len,
 }
 
 HSPEC_API size_t hspec_chunk_attn_mx_workspace(const hspec_chunk_cfg* cfg, int max_len) {
-  if (!cfg || max_len <= 0 || check_chunk(cfg)) return 0;
+  if (!cfg || max_len <= 0 || check_mx(cfg)) return 0;
   Arena ar;
   hspec::ChunkAttnArgs a;
   plan_chunk_attn_mx(ar, *cfg, max_len, a);
@@ -119,7 +128,7 @@ HSPEC_API hspec_status hspec_chunk_attn_mx(const hspec_chunk_cfg* cfg, const voi
                                            const void* v_cache, const int32_t* page_table, const int32_t* ctx_lens,
                                            int max_len, void* o, void* workspace, size_t ws_bytes, void* stream) {
   clear_err();
-  if (hspec_status s = check_chunk(cfg)) return s;
+  if (hspec_status s = check_mx(cfg)) return s;
   if (max_len <= 0) return fail(HSPEC_ERR_SHAPE, "max_len must be positive");
   if (!(cfg->scale >= 0.f && cfg->scale <= 1e30f)) return fail(HSPEC_ERR_SHAPE, "scale must be finite and not negative");
   if (!q || !cu_new || !k_cache || !v_cache || !page_table || !ctx_lens || !o)
