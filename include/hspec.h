@@ -598,7 +598,7 @@ size_t hspec_chunk_attn_mx_workspace(const hspec_chunk_cfg* cfg, int max_len);
  *   [rows]: the row's line of it, below 0: none (NULL: row r has line r, masks = rows).
  * NULL with a count of 0 leaves history, drafts, bias or mask out.  out may be logits (same dtype), and
  * otherwise lies over no other argument.  Rows past cu_rows[B] are left as they were.  Checked on the device:
- * cu_rows as in hspec_verify (HSPEC_DEV_BAD_ROWS; a row of several ranges is one of their requests'); a length
+ * cu_rows as in hspec_verify (HSPEC_DEV_BAD_ROWS; a row of several ranges is the first request's); a length
  * outside [0, max_hist], or a prompt's outside [0, its history's], is clamped (HSPEC_DEV_BAD_CTX_LEN); a draft
  * ahead of some row without a target id is not counted (HSPEC_DEV_BAD_TOKEN); mask_rows >= masks is none
  * (HSPEC_DEV_BAD_ROWS); a repetition outside [2^-64, 2^64], or another penalty that is NaN or beyond +-2^64,

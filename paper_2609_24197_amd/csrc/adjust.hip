@@ -142,9 +142,11 @@ struct TokenRegs {
 template <class Tin, class Tout, int G>
 __global__ void __launch_bounds__(AJ_THREADS) adjust_kernel(AdjustArgs a, int part) {
   constexpr int S = AJ_THREADS * AJ_VEC * G, GS = AJ_THREADS * AJ_VEC;
+  static_assert(AJ_THREADS == 256 && AJ_PART <= 64, "waves of s_before, bits of taken");
   __shared__ __align__(16) unsigned s_cnt[S];
   __shared__ __align__(16) int s_bias[S];   // entry of the bias list, from 1 on
   __shared__ int s_draft[AJ_PART], s_mask[AJ_PART];   // of each row: the draft that comes after it (-1: none), its line of the mask
+  __shared__ int s_before[AJ_THREADS / 64];           // whether some of the rows are of a request before this one, too
   const int tid = threadIdx.x, b = blockIdx.y;
   if (blockIdx.x == gridDim.x - 1) {
     if (b == 0 && blockIdx.z == 0) check_call(a);
@@ -169,9 +171,24 @@ __global__ void __launch_bounds__(AJ_THREADS) adjust_kernel(AdjustArgs a, int pa
     if (a.mask) m = a.mask_rows ? a.mask_rows[rows.row0 + j] : rows.row0 + j;
     s_mask[j - j0] = m < a.masks ? m : -1;
   }
+  // Where cu is bad, a row of several ranges is the first request's, so that one workgroup alone writes it (and, in place,
+  // reads it).
+  if (a.cu) {
+    bool before = false;
+#pragma unroll 4
+    for (int i = tid; i < b; i += AJ_THREADS) {
+      const RowsBefore r = rows_before(a.cu, i, b, a.rows, a.k + 1, rows.row0 + j0, j1 - j0);
+      before |= r.from < r.to;
+    }
+    before = __any(before);
+    if (tid % 64 == 0) s_before[tid / 64] = before;
+  }
   const History h = history(a, b);
   const Penalties pen = penalties(a, b);
   __syncthreads();
+  unsigned long long taken = 0;   // bit j - j0 of row j: another request's
+  if (a.cu && (s_before[0] | s_before[1] | s_before[2] | s_before[3]))
+    taken = rows_taken(a.cu, b, a.rows, a.k + 1, rows.row0 + j0, j1 - j0);
   const int32_t* said = a.history + (size_t)b * a.max_hist;
   auto count = [&](int id, int i) {
     const unsigned at = (unsigned)id - (unsigned)v0;
@@ -264,7 +281,7 @@ __global__ void __launch_bounds__(AJ_THREADS) adjust_kernel(AdjustArgs a, int pa
           }
     }
   };
-  if (whole) {
+  if (whole && !taken) {
     // No branch around a load or store, so that a row's waits are for its own: with them 64 requests of 17 rows of 131072
     // take 195 us.
     auto fetch = [&](int j, RowRegs<G>& r) {
@@ -292,8 +309,12 @@ __global__ void __launch_bounds__(AJ_THREADS) adjust_kernel(AdjustArgs a, int pa
     }
     return;
   }
-  // the last slice
+  // the last slice, or rows that are not all this request's
   for (int j = j0; j < j1; ++j) {
+    if (taken >> (j - j0) & 1) {
+      said_next(s_draft[j - j0]);
+      continue;
+    }
     RowRegs<G> r;
     const int m = __builtin_amdgcn_readfirstlane(s_mask[j - j0]);
 #pragma unroll

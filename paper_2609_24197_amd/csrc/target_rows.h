@@ -26,6 +26,33 @@ __device__ __forceinline__ ChunkRows chunk_rows(const int32_t* cu, int b, int T,
   return r;
 }
 
+// Whether the range of request i, of those before request b, holds some of the n rows from r0 on: [from, to) of them.
+struct RowsBefore {
+  int from, to;
+};
+__device__ __forceinline__ RowsBefore rows_before(const int32_t* cu, int i, int b, int T, int max_n, int r0, int n) {
+  RowsBefore r{0, 0};
+  if (i < b) {
+    const ChunkRows c = clamp_rows(cu[i], cu[i + 1], T, max_n);
+    r.from = max(c.row0 - r0, 0);
+    r.to = min(c.row0 + c.n - r0, n);
+  }
+  return r;
+}
+// Of the n <= 64 rows from r0 on of request b, those that are also of a request before it (where cu is bad): bit i for
+// row r0 + i.  Every lane of a wave calls it.
+__device__ __forceinline__ unsigned long long rows_taken(const int32_t* cu, int b, int T, int max_n, int r0, int n) {
+  unsigned long long taken = 0;
+  for (int at = 0; at < b; at += 64) {
+    const RowsBefore r = rows_before(cu, at + (int)(threadIdx.x & 63), b, T, max_n, r0, n);
+    for (unsigned long long left = __ballot(r.from < r.to); left; left &= left - 1) {
+      const int lane = __builtin_ctzll(left), from = __shfl(r.from, lane), to = __shfl(r.to, lane);
+      taken |= ~0ULL >> (64 - (to - from)) << from;
+    }
+  }
+  return taken;
+}
+
 // Cached length of a request that takes n new tokens: at most cap positions in all, and `held` of them cached.
 struct ChunkPos {
   int L;
