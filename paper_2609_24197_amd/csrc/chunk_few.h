@@ -659,6 +659,9 @@ __device__ __forceinline__ int share_unit(C, const ChunkAttnArgs& a, const Chunk
       step(t, st0, st1, r1);
       if (t + 1 < n) step(t + 1, st1, st0, r0);
     }
+    // the last step has written a stage that nothing reads, and a wave without rows or visible keys comes straight from that:
+    // a barrier waits for no write, and what lies behind the next one puts other things there
+    wait_vm_lgkm0<63>();
   }
   // the new tokens' keys beside the cache, as they are
   if (a.k_new && u.k1 > u.L) {

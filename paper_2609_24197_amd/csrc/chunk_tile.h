@@ -449,6 +449,7 @@ __device__ __forceinline__ bool chunk_unit(const ChunkAttnArgs& a, const ChunkUn
       step(t0, st0, st1);
       if (t0 + 1 < ntiles) step(t0 + 1, st1, st0);
     }
+    wait_vm_lgkm0<63>();   // the last step has written a stage that nothing reads: done before the stages hold something else
     if (a.k_new) {
       const int from = max(u.k0, u.L);
       wg_barrier();   // (every wave has left both stages)
