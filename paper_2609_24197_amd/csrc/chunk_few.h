@@ -407,8 +407,9 @@ __device__ __forceinline__ int few_unit(C, const ChunkAttnArgs& a, const ChunkUn
     }
   };
 
-  // cached keys: the next step's are on their way from where this one's are multiplied (K) or have gone into LDS (V)
-  if (from < held) {
+  // cached keys, if a row sees one: the next step's are on their way from where this one's are multiplied (K) or have gone
+  // into LDS (V)
+  if (k_min < held) {
     Raw rk, rv;
     Place p = place(from);
     load(std::false_type{}, a.k_cache, from, p, rk);
@@ -640,7 +641,7 @@ __device__ __forceinline__ int share_unit(C, const ChunkAttnArgs& a, const Chunk
 
   // cached keys: step t is multiplied while step t + 1 goes into the other stage and the two behind it are on their way
   // (keys past the last read as zeros)
-  const int n = held > from ? (held - from + KT - 1) / KT : 0;
+  const int n = held > k_min ? (held - from + KT - 1) / KT : 0;   // (0 where no row sees a cached key)
   if (n > 0) {
     Raw r0, r1;
     load(from, r0);

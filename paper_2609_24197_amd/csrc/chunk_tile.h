@@ -153,9 +153,9 @@ __device__ __forceinline__ bool chunk_unit(const ChunkAttnArgs& a, const ChunkUn
     }
   }
 
-  // MX with the new tokens beside the cache: keys from `held` on are theirs
+  // MX with the new tokens beside the cache: keys from `held` on are theirs, and a window may leave no cached one
   const int held = C::MX && a.k_new ? min(u.L, u.k1) : u.k1;
-  const int ntiles = held > u.k0 ? (held - u.k0 + KT - 1) / KT : 0;
+  const int ntiles = held > (C::MX ? k_min : u.k0) ? (held - u.k0 + KT - 1) / KT : 0;
   const int32_t* ptab = a.page_table + (size_t)u.b * a.max_pages;
   // Page ids [pg0, pg0 + 256) of the table, lane by lane in four registers (-1 past the unit's last page): a tile's
   // ids cost no load of their own, which would have to wait for the DMA that went out before it.
