@@ -7,21 +7,10 @@
 namespace hspec {
 namespace {
 
-struct MxBlock {
-  u32x4 code;        // 8 channels a word
-  unsigned scale;    // the byte
-};
-// Block c of row `row` of a head's part of a page.
-__device__ __forceinline__ MxBlock mx_load(const uint8_t* p, int ps, int D, int row, int c) {
-  MxBlock b;
-  b.code = *reinterpret_cast<const u32x4*>(p + row * (D / 2) + c * (MX_BLOCK / 2));
-  b.scale = p[ps * (D / 2) + row * (D / MX_BLOCK) + c];
-  return b;
-}
-
 // The key, of 16, that lane l of 16 takes into LDS: bits of l at places A, B, C, E.  A 16-byte write is done 8 lanes at a time
 // over 128 bytes, so the keys of 8 lanes side by side differ in the bits that choose the place within those (with
-// keys in order a quarter to a third of the LDS cycles are conflicts, and prompts and 17 tokens take 2 % more on the same card).
+// keys in order a quarter to a third of the LDS cycles are conflicts, so none, and prompts and 17 tokens take 2 % more on the
+// same card).
 template <int A, int B, int C, int E>
 __device__ __forceinline__ int spread16(int l) {
   return (l & 1) << A | (l >> 1 & 1) << B | (l >> 2 & 1) << C | (l >> 3 & 1) << E;
