@@ -569,7 +569,7 @@ size_t hspec_chunk_read_mx_workspace(const hspec_chunk_cfg* cfg);
  * HSPEC_CHUNK_BLOCK, every new token of a request sees all of them, as the block of
  * hspec_paged_attn does (needs k_new, v_new, and max_new <= window where there is one).  Precision, masked
  * slots, rows that see nothing and the other arguments as hspec_chunk_attn: with bf16 storage the 4-bit values are
- * widened exactly and multiplied as bf16; with fp32 no factor of a product loses a bit, and sums are of 32 bits.
+ * widened exactly and multiplied as bf16; with fp32 no factor of a product loses a bit (above 2^-133), and sums are of 32 bits.
  */
 enum { HSPEC_CHUNK_BLOCK = 1u << 0 };
 hspec_status hspec_chunk_attn_mx(const hspec_chunk_cfg* cfg, const void* q, const int32_t* cu_new, const void* k_new,

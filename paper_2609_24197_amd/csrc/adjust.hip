@@ -8,7 +8,7 @@
 // of one request in turn: it counts the request's history into LDS for its slice alone (whole-number additions, so any
 // order serves), keeps what a token's row-independent part comes to in registers, and each row is then one load, a few
 // operations and one store per token, with the next row's loads under way.  64 requests of 17 rows of 131072 bf16 logits:
-// 103 us in the kernel, 5.6 TB/s; one row of 32000: 4.4.
+// 120 us in the kernel, 4.8 TB/s (105 at its shortest); one row of 32000: 4.8.
 #include "common.h"
 #include "target.h"
 #include "target_rows.h"
@@ -343,6 +343,10 @@ hipError_t launch_g(const AdjustArgs& a, hipStream_t s) {
   hipLaunchKernelGGL((adjust_kernel<Tin, Tout, G>), grid, dim3(AJ_THREADS), 0, s, a, part);
   return hipGetLastError();
 }
+// One group of 8 tokens a thread where slices and requests are few: shorter workgroups, and more of them (one row of 32000:
+// 3.6 us in a graph, 4.7 with two groups; 32 of them 5.0 and 6.1; 17 rows of each 17.6 and 18.3).  Two where they fill the
+// chip anyway, which halves the counting of a history for each token (17 rows of 131072 of 16 requests: 26.7 us, 27.4 with
+// one; of 32, 52.3 and 53.5; of 64, 113 either way; a row each of 16 requests, though, 7.4 and 6.2, of 64, 15.8 and 15.0).
 template <class Tin, class Tout>
 hipError_t launch_typed(const AdjustArgs& a, hipStream_t s) {
   return (long long)a.V * a.B <= (1 << 20) ? launch_g<Tin, Tout, 1>(a, s) : launch_g<Tin, Tout, 2>(a, s);

@@ -1,7 +1,8 @@
 // Attention of a ragged chunk of new tokens over the 4-bit paged cache (mx.h).  Up to 128 rows of a request: chunk_few.h.  Past
 // that, the units, queue and merge of the other caches (chunk_tile.h), with K and V widened to the type of q on their way
-// into LDS: three prompts of about 6000 tokens, 32 and 8 heads of 128, 1383 to 1474 us by the card, 981 to 921 TFLOP/s (1286 over a bf16 cache).  The new
-// tokens' own K and V are in the cache, or beside it as they are, where their keys follow the cached ones.
+// into LDS: three prompts of about 6000 tokens, 32 and 8 heads of 128, take 1383 to 1474 us by the card (981 to 921 TFLOP/s),
+// over a bf16 cache 1286.  The new tokens' own K and V are in the cache, or beside it as they are, where their keys follow the
+// cached ones.
 #include "chunk_few.h"
 #include "chunk_tile.h"
 

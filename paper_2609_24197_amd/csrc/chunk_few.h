@@ -6,7 +6,7 @@
 // c = l / 16, of key l % 16 of every 16 (the channels are summed over, so any order of them serves, if Q has the same); V^T
 // is read transposed from LDS in the order in which S^T leaves a lane its keys.
 //
-// Bound by HBM where a request has a token (64 of them, 512..8192 cached, 32 and 8 heads of 128: 63 us, 5.1 TB/s), past 32 rows
+// Bound by HBM where a request has a token (64 of them, 512..8192 cached, 32 and 8 heads of 128: 67 us, 4.8 TB/s), past 32 rows
 // by a step's chain of LDS, products and softmax, with two waves a SIMD (the whole call, a block of 16: 137 to 147 us by the card,
 // 17 tokens: 172 to 176; the matrix units are busy a quarter of the time).
 //
@@ -38,8 +38,8 @@ __device__ __forceinline__ s16x4 few_v(const bf16* sV, int key0, int db, int lan
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(sV + few_off<D>(key, db * 16 + 4 * (lane & 3))));
 }
 
-// An fp32 value as the sum of three bf16, by cutting off bits: 8 + 8 + 8 of its 24, so that nothing is lost.  (What is not
-// finite is the first of them.)
+// An fp32 value as the sum of three bf16, by cutting off bits: 8 + 8 + 8 of its 24, so that nothing is lost but what lies
+// below 2^-133, bf16's smallest step.  (What is not finite is the first of them.)
 struct Planes {
   unsigned bits[3];   // bf16 in the upper half
 };
