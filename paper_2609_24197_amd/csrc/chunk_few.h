@@ -491,7 +491,6 @@ __device__ __forceinline__ int share_unit(C, const ChunkAttnArgs& a, const Chunk
   const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5, l32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rw = wave / C::KW, kw = wave % C::KW;
-  const int held = a.k_new ? min(u.L, u.k1) : u.k1;
   const int g = a.Hq / a.Hkv, R = u.n * g, c0 = rw * 32, c = c0 + l32;
   const bool live = c0 < R, real = c < R;
   const int tok = real ? c / g : u.n - 1, hq = h * g + (real ? c - tok * g : 0);
@@ -503,6 +502,7 @@ __device__ __forceinline__ int share_unit(C, const ChunkAttnArgs& a, const Chunk
   const int t_first = min(c0, R - 1) / g, t_last = min(c0 + 31, R - 1) / g;
   const int any_lo = sees_from(t_first), any_hi0 = sees_to(t_last), all_lo = sees_from(t_last), all_hi0 = sees_to(t_first);
   const int k_min = max(u.k0, sees_from(0));   // the first key that a row of the unit sees
+  const int cached = a.k_new ? min(u.L, u.k1) : u.k1, held = cached > k_min ? cached : 0;   // (0: no row sees a cached key)
   const int from = k_min / KT * KT;
   FewPages pages;
   pages.init(a, u.b, from, held);
@@ -641,7 +641,7 @@ __device__ __forceinline__ int share_unit(C, const ChunkAttnArgs& a, const Chunk
 
   // cached keys: step t is multiplied while step t + 1 goes into the other stage and the two behind it are on their way
   // (keys past the last read as zeros)
-  const int n = held > k_min ? (held - from + KT - 1) / KT : 0;   // (0 where no row sees a cached key)
+  const int n = held > from ? (held - from + KT - 1) / KT : 0;
   if (n > 0) {
     Raw r0, r1;
     load(from, r0);
