@@ -1,4 +1,4 @@
-"""The 4-bit cache with pages of more than 2^32 bytes."""
+"""The 4-bit cache with pages of more than 2^32 bytes, and with the largest that the calls take."""
 import pytest
 import torch
 
@@ -46,6 +46,40 @@ def test_pages_past_32_bits(wide, dtype, new):
         o = torch.empty(new, H, D, dtype=st, device="cuda")
         ws = hspec.workspace(hspec.chunk_attn_mx_workspace(a, N))
         hspec.chunk_attn_mx(a, q[held:].contiguous(), ints(0, new), *caches, table, ints(held), N, o, ws)
+        assert hspec.read_status(ws) == 0
+        got.append((q, k, v, o))
+    for x, y in zip(*got):
+        assert torch.isfinite(x).all() and torch.equal(x, y)
+
+
+@pytest.mark.parametrize("new", [1, 9, 17, 50, 150])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("ps,D", [(1 << 24, 128), (1 << 25, 64)])
+def test_the_end_of_the_largest_page(ps, D, dtype, new):
+    """The last 200 positions of a page of 1.1 GB, behind a window: as on pages of 16, of which the last are mapped."""
+    T, Hq, st = 200, 4, ST[dtype]
+    g = torch.Generator(device="cuda").manual_seed(new)
+    qkv = torch.randn(T, (Hq + 2) * D, generator=g, device="cuda").to(st)
+    ints = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    got = []
+    for size in (16, ps):
+        n = ps // size
+        pages = 15 if n > 1 else 1
+        table = torch.full((1, n), -1, dtype=torch.int32, device="cuda")
+        table[0, -min(n, 13):] = ints(*range(pages - min(n, 13), pages))
+        c = hspec.chunk_cfg(1, T, T, Hq, 1, D, size, n, pages, code(dtype))
+        caches = [torch.empty(hspec.mx_cache_shape(c), dtype=torch.uint8, device="cuda") for _ in range(2)]
+        q = torch.empty(T, Hq, D, dtype=st, device="cuda")
+        ws = hspec.workspace(hspec.chunk_append_mx_workspace(c))
+        hspec.chunk_append_mx(c, qkv, ints(0, T), ints(ps - T), q, *caches, table, ws)
+        assert hspec.read_status(ws) == 0
+        k, v = (torch.empty(T, 1, D, dtype=st, device="cuda") for _ in range(2))
+        hspec.chunk_read_mx(c, ints(0, T), ints(ps - T), *caches, table, k, v, ws)
+        assert hspec.read_status(ws) == 0
+        a = hspec.chunk_cfg(1, new, new, Hq, 1, D, size, n, pages, code(dtype), window=45)
+        o = torch.empty(new, Hq, D, dtype=st, device="cuda")
+        ws = hspec.workspace(hspec.chunk_attn_mx_workspace(a, ps))
+        hspec.chunk_attn_mx(a, q[T - new:].contiguous(), ints(0, new), *caches, table, ints(ps - new), ps, o, ws)
         assert hspec.read_status(ws) == 0
         got.append((q, k, v, o))
     for x, y in zip(*got):
