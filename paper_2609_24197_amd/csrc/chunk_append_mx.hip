@@ -19,8 +19,9 @@
 namespace hspec {
 namespace {
 
-// Rows a workgroup.  With the norm, in a graph, for 1, 2 and 4 of them: 64 rows of 48 heads 6.2, 9.6 and 16.1 us; 1088 of them
-// 13.7, 13.1 and 19.3; 2000 from bf16 25.8, 17.9 and 15.6; 8000 of 80 heads 131, 98 and 89.
+// Rows a workgroup, two at every size: fewer suit few rows, more suit many.  With the norm, in a graph, for 1, 2 and 4 of
+// them: 64 rows of 48 heads 6.2, 9.6 and 16.1 us; 1088 of them 13.7, 13.1 and 19.3; 2000 from bf16 25.8, 17.9 and 15.6; 8000
+// of 80 heads 131, 98 and 89.
 constexpr int AM_ROWS = 2;
 
 // Codes of one lane's E channels of a block, and the block's scale byte; 32 / E neighbouring lanes share the block.

@@ -7,8 +7,8 @@
 // is read transposed from LDS in the order in which S^T leaves a lane its keys.
 //
 // Bound by HBM where a request has a token (64 of them, 512..8192 cached, 32 and 8 heads of 128: 67 us, 4.8 TB/s), past 32 rows
-// by a step's chain of LDS, products and softmax, with two waves a SIMD (the whole call, a block of 16: 137 to 147 us by the card,
-// 17 tokens: 172 to 176; the matrix units are busy a quarter of the time).
+// by a step's chain of LDS, products and softmax, with two waves a SIMD (the whole call, a block of 16: 135 to 147 us by the card,
+// 17 tokens: 169 to 176; the matrix units are busy a quarter of the time).
 //
 // Up to 32 rows (Few) a wave walks its keys by itself: K is the product's operand as it was loaded, widened in
 // registers, V goes through a piece of LDS of the wave's own, and there is no barrier in a unit.  Past that (Share)
